@@ -552,6 +552,124 @@ CPA_API int cpa_event_host(cpa_plan* plan, const void* h_q, const void* h_k, con
 CPA_API int cpa_decode_static(const cpa_plan* plan, const void* q, const void* k_pool, const void* v_pool,
                               void* o, void* stream);
 
+/*
+ * The KV cache in 8 bits, with tables built on the device.  A decode step reads the whole cache and little else, so a
+ * cache of one byte per element halves its time, and a pool of given size holds twice the history.  The paper says
+ * nothing about the cache's format (Section 4.2 names the serving engine that has it underneath); everything below is
+ * this library's own.  The calls need no plan: lengths, page lists and slots live on the device, no call reads them back,
+ * and every launch depends on its arguments alone, so that a sequence of them can be captured into a CUDA graph.
+ *
+ *   kv_pool   : device [num_pages, num_kv_heads, 2, 16, head_dim] e4m3 codes, index 0 = K and 1 = V, rows in order;
+ *               16-byte aligned (cpa_decode_q8 reads it through a tensor map)
+ *   kv_scales : device fp32 [num_pages, num_kv_heads, 2], 16-byte aligned
+ *   value     = code * scale
+ * The append calls give a (page, kv head, K or V) the smallest power of two s >= 2^-126 for which no finite magnitude
+ * that the page has held exceeds 448 s; code = x / s rounded to nearest even.  An infinity is stored as +-448, a NaN as
+ * NaN.  When a later row needs a larger scale, the codes that the page holds are rounded again (code * s_old / s_new),
+ * which only changes codes that become subnormal.  A block's first row in a page starts the page's scale afresh.  The
+ * calls that read take any scale, the append calls any positive scale they find.  Slots behind a block's length may hold
+ * anything, their page's scale counts only once a row is there.
+ *
+ * cpa_config: num_q_heads, num_kv_heads, head_dim (64, 128), page_size (16), scale and num_sms as for a plan (the SMs a
+ * decode launch may fill, 0 = all); group size G <= 8, at most 1024 kv heads; the other fields are not used.
+ *
+ * Streams: all work is enqueued on `stream`, on the current device.  Calls on the same tables must not overlap on the
+ * device (the decode's merge counters and the status word live there), nor calls on the same workspace.
+ */
+typedef struct cpa_table_dims {
+    int32_t num_blocks;      /* B >= 1, at most 2^20 */
+    int32_t max_new_tokens;  /* tokens to reserve pages for behind every block's length, >= 0 */
+    int32_t num_pages;       /* pages of the pool: page ids lie in [0, num_pages); num_pages * 32 * num_kv_heads < 2^31 */
+    int32_t page_capacity;   /* entries of the page list, >= the pages that the blocks take */
+    int32_t token_capacity;  /* entries of the slot map, >= the blocks' tokens; 0 = no slot map is made */
+} cpa_table_dims;
+
+/* Size in bytes of the device tables of these dimensions, or a negative cpa_status. */
+CPA_API int64_t cpa_tables_bytes(const cpa_config* cfg, const cpa_table_dims* dims);
+
+/* Byte offset of an int32 array inside the tables: CPA_ARR_CU_SEQLENS [B+1], CPA_ARR_PAGE_INDPTR [B+1],
+ * CPA_ARR_PAGE_INDICES [page_capacity], CPA_ARR_SLOT_MAPPING [token_capacity]; or a negative cpa_status. */
+CPA_API int64_t cpa_tables_offset(const cpa_config* cfg, const cpa_table_dims* dims, int which);
+
+/*
+ * cpa_tables_build -- block tables and slot map from request lengths on the device: the arrays that cpa_plan_create
+ * computes on the host, with the same rules and values (block b takes ceil((L_b + max_new_tokens) / 16) pages in order
+ * from the free list; slot of token i = page * 16 + i % 16), for lengths that only the device knows.
+ *   d_block_lens : device int32 [B], >= 0 (a block of length 0 is an empty place of a padded batch)
+ *   d_free_pages : device int32 [num_free], distinct ids in [0, num_pages) (distinctness is the caller's contract)
+ *   d_tables     : device, cpa_tables_bytes bytes, 16-byte aligned; needs no initialisation
+ * One launch; entries behind the last page and the last token stay as they were.  What only the device can see is
+ * recorded in the tables and read with cpa_tables_status: a negative length (CPA_EINVAL), more pages than num_free or
+ * page_capacity or more tokens than token_capacity (CPA_ENOSPC) leave tables of B empty blocks, which every call below
+ * accepts; a page id out of range (CPA_EINVAL) is replaced by page 0, and results on such tables are void.
+ * Errors: CPA_EINVAL, CPA_EUNSUPPORTED, CPA_ECUDA.
+ */
+CPA_API int cpa_tables_build(const cpa_config* cfg, const cpa_table_dims* dims, const int32_t* d_block_lens,
+                             const int32_t* d_free_pages, int32_t num_free, void* d_tables, void* stream);
+
+/* Synchronise `stream` and read the status of the tables: what the build recorded, else the first that a later call did
+ * (CPA_ENOSPC: rows beyond a block's pages; CPA_EINVAL: a negative length or a range outside the packed rows;
+ * CPA_ETIMEOUT: a device-side wait gave up).  cpa_tables_build clears it. */
+CPA_API int cpa_tables_status(const void* d_tables, void* stream);
+
+/*
+ * cpa_kv_append_q8 -- quantise new K/V rows into the blocks' pages, behind the tokens that they have.
+ *   k_new, v_new : device bf16 [num_rows, num_kv_heads, head_dim], packed, block-major
+ *   d_cu_new     : device int32 [B+1], block b's rows are [cu[b], cu[b+1]), at most num_rows in all (rows behind the
+ *                  last are not read); the tables' cu_seqlens for whole prompts.  NULL = one row per block
+ *                  (num_rows = B)
+ *   d_lens       : device int32 [B] tokens cached before the call, NULL = 0 everywhere
+ *   d_lens_out   : device int32 [B], written with the tokens cached after it; not d_lens itself; may be NULL
+ * A block whose rows do not fit its pages is left out (its length stays, CPA_ENOSPC in the status), as is one with a
+ * bad range (CPA_EINVAL in the status).  The same call repeated stores the same cache.  Errors: CPA_EINVAL,
+ * CPA_EUNSUPPORTED, CPA_ECUDA.
+ */
+CPA_API int cpa_kv_append_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const void* k_new,
+                             const void* v_new, const int32_t* d_cu_new, int32_t num_rows, const int32_t* d_lens,
+                             int32_t* d_lens_out, void* kv_pool, float* kv_scales, void* stream);
+
+/* Size of the decode calls' device workspace in bytes, or a negative cpa_status.  Depends on cfg alone. */
+CPA_API int64_t cpa_decode_q8_workspace_bytes(const cpa_config* cfg);
+
+/*
+ * cpa_decode_q8 -- one batched decode step over the 8-bit cache: the query token of block b attends over the block's
+ * first d_lens[b] tokens.  The split over the KV length is made on the device from the lengths.
+ *   q, o        : device bf16 [B, num_q_heads, head_dim]
+ *   d_lens      : device int32 [B]; 0 gives a row of zeros
+ *   d_active    : device int32 [B] or NULL = all; a block with flag 0 sits out, its rows of o are not written
+ *   d_workspace : device scratch, cpa_decode_q8_workspace_bytes, 16-byte aligned, needs no initialisation
+ * A block whose length is negative or beyond its pages sits out too (status CPA_EINVAL, CPA_ENOSPC).  Errors:
+ * CPA_EINVAL, CPA_EUNSUPPORTED, CPA_ECUDA.
+ */
+CPA_API int cpa_decode_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const void* q,
+                          const int32_t* d_lens, const int32_t* d_active, const void* kv_pool, const float* kv_scales,
+                          void* o, void* d_workspace, void* stream);
+
+/*
+ * cpa_decode_append_q8 -- one decode step with its append fused in: cpa_kv_append_q8 of one row per block, then
+ * cpa_decode_q8 over the cache with that row in it (as it was stored), in one launch.
+ *   k_new, v_new : device bf16 [B, num_kv_heads, head_dim]
+ *   d_lens       : device int32 [B] tokens cached before the step;  d_lens_out: [B] after it, not d_lens itself; a
+ *                  block that sits out keeps its length.  A caller keeps two arrays and swaps them from step to step.
+ * Everything else as for cpa_decode_q8.
+ */
+CPA_API int cpa_decode_append_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const void* q,
+                                 const void* k_new, const void* v_new, const int32_t* d_lens, int32_t* d_lens_out,
+                                 const int32_t* d_active, void* kv_pool, float* kv_scales, void* o, void* d_workspace,
+                                 void* stream);
+
+/*
+ * cpa_kv_read_q8 -- rows of the 8-bit cache as bf16: positions d_first[b] + i of block b to packed rows d_cu[b] + i,
+ * i < d_cu[b+1] - d_cu[b] (to hand a history on to calls that take bf16 rows).
+ *   d_first      : device int32 [B], NULL = 0 everywhere;  d_cu: device int32 [B+1], at most num_rows rows in all
+ *   k_out, v_out : device bf16 [num_rows, num_kv_heads, head_dim]; rows behind the last stay as they were
+ * A block whose range leaves its pages is left out (status as for the append); that the positions have been written is
+ * the caller's contract.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED, CPA_ECUDA.
+ */
+CPA_API int cpa_kv_read_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const int32_t* d_first,
+                           const int32_t* d_cu, int32_t num_rows, const void* kv_pool, const float* kv_scales,
+                           void* k_out, void* v_out, void* stream);
+
 /* Static text for a cpa_status value. */
 CPA_API const char* cpa_strerror(int status);
 

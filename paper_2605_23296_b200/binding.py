@@ -45,6 +45,12 @@ class cpa_config(ctypes.Structure):
                 ("pages_per_split", ctypes.c_int32), ("num_sms", ctypes.c_int32)]
 
 
+class cpa_table_dims(ctypes.Structure):
+    _fields_ = [("num_blocks", ctypes.c_int32), ("max_new_tokens", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("page_capacity", ctypes.c_int32),
+                ("token_capacity", ctypes.c_int32)]
+
+
 class CpaError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -114,6 +120,25 @@ _lib.cpa_decode_append.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.cpa_decode_append.restype = ctypes.c_int
 _lib.cpa_decode_static.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp]
 _lib.cpa_decode_static.restype = ctypes.c_int
+_cfgp, _dimsp, _c32 = ctypes.POINTER(cpa_config), ctypes.POINTER(cpa_table_dims), ctypes.c_int32
+_lib.cpa_tables_bytes.argtypes = [_cfgp, _dimsp]
+_lib.cpa_tables_bytes.restype = ctypes.c_int64
+_lib.cpa_tables_offset.argtypes = [_cfgp, _dimsp, ctypes.c_int]
+_lib.cpa_tables_offset.restype = ctypes.c_int64
+_lib.cpa_tables_build.argtypes = [_cfgp, _dimsp, _vp, _vp, _c32, _vp, _vp]
+_lib.cpa_tables_build.restype = ctypes.c_int
+_lib.cpa_tables_status.argtypes = [_vp, _vp]
+_lib.cpa_tables_status.restype = ctypes.c_int
+_lib.cpa_kv_append_q8.argtypes = [_cfgp, _dimsp, _vp, _vp, _vp, _vp, _c32] + [_vp] * 5
+_lib.cpa_kv_append_q8.restype = ctypes.c_int
+_lib.cpa_decode_q8_workspace_bytes.argtypes = [_cfgp]
+_lib.cpa_decode_q8_workspace_bytes.restype = ctypes.c_int64
+_lib.cpa_decode_q8.argtypes = [_cfgp, _dimsp] + [_vp] * 9
+_lib.cpa_decode_q8.restype = ctypes.c_int
+_lib.cpa_decode_append_q8.argtypes = [_cfgp, _dimsp] + [_vp] * 12
+_lib.cpa_decode_append_q8.restype = ctypes.c_int
+_lib.cpa_kv_read_q8.argtypes = [_cfgp, _dimsp, _vp, _vp, _vp, _c32] + [_vp] * 5
+_lib.cpa_kv_read_q8.restype = ctypes.c_int
 _lib.cpa_strerror.argtypes = [ctypes.c_int]
 _lib.cpa_strerror.restype = ctypes.c_char_p
 
@@ -347,3 +372,53 @@ def cpa_decode_static(plan: int, q, k_pool, v_pool, o, stream: int = 0) -> int:
     stream capture.
     """
     return _lib.cpa_decode_static(plan, _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(o), stream or None)
+
+
+# ---- the KV cache in 8 bits: device tables, quantising append, decode, read-back (no plan)
+
+def cpa_tables_bytes(cfg: cpa_config, dims: cpa_table_dims) -> int:
+    return int(_lib.cpa_tables_bytes(ctypes.byref(cfg), ctypes.byref(dims)))
+
+
+def cpa_tables_offset(cfg: cpa_config, dims: cpa_table_dims, which: int) -> int:
+    return int(_lib.cpa_tables_offset(ctypes.byref(cfg), ctypes.byref(dims), int(which)))
+
+
+def cpa_tables_build(cfg: cpa_config, dims: cpa_table_dims, d_block_lens, d_free_pages, num_free: int, d_tables,
+                     stream: int = 0) -> int:
+    return _lib.cpa_tables_build(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_block_lens), _ptr(d_free_pages),
+                                 int(num_free), _ptr(d_tables), stream or None)
+
+
+def cpa_tables_status(d_tables, stream: int = 0) -> int:
+    return _lib.cpa_tables_status(_ptr(d_tables), stream or None)
+
+
+def cpa_kv_append_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, k_new, v_new, d_cu_new, num_rows: int, d_lens,
+                     d_lens_out, kv_pool, kv_scales, stream: int = 0) -> int:
+    return _lib.cpa_kv_append_q8(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_tables), _ptr(k_new), _ptr(v_new),
+                                 _ptr(d_cu_new), int(num_rows), _ptr(d_lens), _ptr(d_lens_out), _ptr(kv_pool),
+                                 _ptr(kv_scales), stream or None)
+
+
+def cpa_decode_q8_workspace_bytes(cfg: cpa_config) -> int:
+    return int(_lib.cpa_decode_q8_workspace_bytes(ctypes.byref(cfg)))
+
+
+def cpa_decode_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, q, d_lens, d_active, kv_pool, kv_scales, o, d_workspace,
+                  stream: int = 0) -> int:
+    return _lib.cpa_decode_q8(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_tables), _ptr(q), _ptr(d_lens),
+                              _ptr(d_active), _ptr(kv_pool), _ptr(kv_scales), _ptr(o), _ptr(d_workspace), stream or None)
+
+
+def cpa_decode_append_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, q, k_new, v_new, d_lens, d_lens_out, d_active,
+                         kv_pool, kv_scales, o, d_workspace, stream: int = 0) -> int:
+    return _lib.cpa_decode_append_q8(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_tables), _ptr(q), _ptr(k_new),
+                                     _ptr(v_new), _ptr(d_lens), _ptr(d_lens_out), _ptr(d_active), _ptr(kv_pool),
+                                     _ptr(kv_scales), _ptr(o), _ptr(d_workspace), stream or None)
+
+
+def cpa_kv_read_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, d_first, d_cu, num_rows: int, kv_pool, kv_scales,
+                   k_out, v_out, stream: int = 0) -> int:
+    return _lib.cpa_kv_read_q8(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_tables), _ptr(d_first), _ptr(d_cu),
+                               int(num_rows), _ptr(kv_pool), _ptr(kv_scales), _ptr(k_out), _ptr(v_out), stream or None)

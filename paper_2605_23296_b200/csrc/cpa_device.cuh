@@ -8,6 +8,7 @@
 // (atomicCAS from 0); cpa_plan_status maps them to a cpa_status.
 constexpr int32_t kStatusWaitGaveUp = 1;   // a bounded wait ran out           -> CPA_ETIMEOUT
 constexpr int32_t kStatusNoSpace = 2;      // an append found no page/slot left -> CPA_ENOSPC
+constexpr int32_t kStatusInvalid = 3;      // a length or page id on the device is out of range -> CPA_EINVAL (tables)
 
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" :: "r"(bar), "r"(count) : "memory");

@@ -1,0 +1,219 @@
+// Block tables and slot maps built on the device from request lengths: the device counterpart of the index arrays that
+// cpa_plan_create computes on the host, for lengths that only the device knows.
+//
+//   cu_seqlens[b+1]  = sum_{a<=b} L_a            page_indptr[b+1] = sum_{a<=b} ceil((L_a + T) / 16)
+//   page list        = the first page_indptr[B] free pages (blocks take them in order)
+//   slot(b, i)       = free[page_indptr[b] + i / 16] * 16 + i % 16
+//
+// The work is two prefix sums over B and a fill of the slot map: bytes are few (4 per token and page), so a call is
+// bound by latency.  Hence one launch without any communication between its CTAs: every CTA sums all lengths (they come
+// from L2, B words) and scans them chunk by chunk, and fills those tiles of the slot map that are its own.  A second
+// launch for the fill, or a scan handed on from CTA to CTA, would each cost more than the repeated sum.
+#include <algorithm>
+
+#include "cache_q8.cuh"
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kPerThread = 4;                     // blocks of a chunk per thread
+constexpr int kChunk = kThreads * kPerThread;
+constexpr int kTile = 4096;                       // tokens (or pages) per tile of the fills
+
+struct pair64 { int64_t tokens, pages; };
+
+// Sum over the CTA, given to every thread.
+__device__ __forceinline__ pair64 cta_sum(pair64 v, pair64* sm) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        v.tokens += __shfl_xor_sync(0xffffffffu, v.tokens, o);
+        v.pages += __shfl_xor_sync(0xffffffffu, v.pages, o);
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+    __syncthreads();
+    pair64 t{0, 0};
+    for (int w = 0; w < kThreads / 32; ++w) { t.tokens += sm[w].tokens; t.pages += sm[w].pages; }
+    return t;
+}
+
+__global__ void __launch_bounds__(kThreads)
+tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t* __restrict__ free_pages, int B, int T,
+                    int num_pages, int page_limit, int token_limit, int n_tickets) {
+    __shared__ int sm_cu[kChunk + 1], sm_ip[kChunk + 1];
+    __shared__ pair64 sm_warp[kThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    // totals, in 64 bits; a negative length or too many pages or tokens leaves empty tables and a status
+    pair64 sum{0, 0};
+    bool bad = false;
+    for (int b = tid; b < B; b += kThreads) {
+        const int64_t L = lens[b];
+        bad |= L < 0;
+        sum.tokens += L;
+        sum.pages += (L + T + kPage - 1) / kPage;
+    }
+    bad = __syncthreads_or((int)bad);
+    const pair64 total = cta_sum(sum, sm_warp);
+    const int32_t status = bad ? kStatusInvalid
+                               : total.pages > page_limit || total.tokens > token_limit ? kStatusNoSpace : 0;
+    for (int i = blockIdx.x * kThreads + tid; i < n_tickets; i += gridDim.x * kThreads) t.tickets[i] = 0;
+    if (status) {
+        for (int b = blockIdx.x * kThreads + tid; b <= B; b += gridDim.x * kThreads) t.cu_seqlens[b] = t.page_indptr[b] = 0;
+        if (blockIdx.x == 0 && tid < kHeaderWords) t.header[tid] = tid == kBuildWords ? status : 0;
+        return;
+    }
+    // every CTA writes its own word of the header, so nothing has to be cleared in front of the launch
+    if (blockIdx.x == 0 && tid < kHeaderWords && (tid < kBuildWords || tid >= kBuildWords + (int)gridDim.x))
+        t.header[tid] = tid == 1 ? (int)total.tokens : tid == 2 ? (int)total.pages : 0;
+
+    // the page list; an id outside the pool is replaced by page 0, so that no later call leaves the pool
+    bool bad_id = false;
+    for (int i = blockIdx.x * kThreads + tid; i < (int)total.pages; i += gridDim.x * kThreads) {
+        const int id = free_pages[i];
+        const bool out = (unsigned)id >= (unsigned)num_pages;
+        bad_id |= out;
+        t.page_indices[i] = out ? 0 : id;
+    }
+    bad_id = __syncthreads_or((int)bad_id);
+    if (tid == 0) t.header[kBuildWords + blockIdx.x] = bad_id ? kStatusInvalid : 0;
+
+    pair64 run{0, 0};
+    for (int at = 0; at < B; at += kChunk) {
+        // exclusive scan of this chunk's lengths and pages on top of `run`
+        int tok[kPerThread], pg[kPerThread], mine_t = 0, mine_p = 0;
+        const int b0 = at + tid * kPerThread;
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+            const int L = b0 + i < B ? lens[b0 + i] : 0;
+            tok[i] = mine_t;
+            pg[i] = mine_p;
+            mine_t += L;
+            mine_p += b0 + i < B ? (int)(((int64_t)L + T + kPage - 1) / kPage) : 0;
+        }
+        int inc_t = mine_t, inc_p = mine_p;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int a = __shfl_up_sync(0xffffffffu, inc_t, o), c = __shfl_up_sync(0xffffffffu, inc_p, o);
+            if (lane >= o) { inc_t += a; inc_p += c; }
+        }
+        __syncthreads();       // the previous chunk's fill and the totals are through with shared memory
+        if (lane == 31) sm_warp[warp] = {inc_t, inc_p};
+        __syncthreads();
+        int base_t = (int)run.tokens, base_p = (int)run.pages;
+        pair64 chunk{0, 0};
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) { base_t += (int)sm_warp[w].tokens; base_p += (int)sm_warp[w].pages; }
+            chunk.tokens += sm_warp[w].tokens;
+            chunk.pages += sm_warp[w].pages;
+        }
+        base_t += inc_t - mine_t;
+        base_p += inc_p - mine_p;
+        const int n = min(kChunk, B - at);
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+            const int j = tid * kPerThread + i;
+            if (j > n) continue;
+            sm_cu[j] = base_t + tok[i];
+            sm_ip[j] = base_p + pg[i];
+            if (blockIdx.x == 0 && j < n) { t.cu_seqlens[at + j] = sm_cu[j]; t.page_indptr[at + j] = sm_ip[j]; }
+        }
+        const int t0 = (int)run.tokens, t1 = (int)(run.tokens + chunk.tokens);
+        run.tokens += chunk.tokens;
+        run.pages += chunk.pages;
+        if (tid == 0) { sm_cu[n] = t1; sm_ip[n] = (int)run.pages; }
+        if (blockIdx.x == 0 && tid == 0 && at + n == B) { t.cu_seqlens[B] = t1; t.page_indptr[B] = (int)run.pages; }
+        __syncthreads();
+        if (t.slot_mapping == nullptr) continue;
+        // slots of the chunk's tokens, in tiles that go round the CTAs
+        for (int tile = t0 / kTile; (int64_t)tile * kTile < t1; ++tile) {
+            if (tile % (int)gridDim.x != (int)blockIdx.x) continue;
+            for (int j = tid * 4; j < kTile; j += kThreads * 4) {
+                const int64_t g = (int64_t)tile * kTile + j;      // four tokens, 16-byte aligned in the map
+                const int first = (int)max((int64_t)t0, g), last = (int)min((int64_t)t1, g + 4);
+                if (first >= last) continue;
+                int lo = 0, hi = n - 1;                            // last block of the chunk that starts at or before it
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (sm_cu[mid] <= first) lo = mid; else hi = mid - 1;
+                }
+                int out[4], page_at = -1, page = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t token = g + i;
+                    out[i] = 0;
+                    if (token < first || token >= last) continue;
+                    while (sm_cu[lo + 1] <= token) ++lo;           // blocks of length zero are stepped over
+                    const int pos = (int)token - sm_cu[lo], want = sm_ip[lo] + pos / kPage;
+                    if (want != page_at) {
+                        page_at = want;
+                        page = free_pages[want];
+                        if ((unsigned)page >= (unsigned)num_pages) page = 0;
+                    }
+                    out[i] = page * kPage + pos % kPage;
+                }
+                if (last - first == 4) {
+                    *reinterpret_cast<int4*>(t.slot_mapping + g) = make_int4(out[0], out[1], out[2], out[3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (g + i >= first && g + i < last) t.slot_mapping[g + i] = out[i];
+                }
+            }
+        }
+    }
+}
+
+}  // namespace
+
+extern "C" int64_t cpa_tables_bytes(const cpa_config* cfg, const cpa_table_dims* dims) {
+    const int rc = q8_check(cfg, dims);
+    return rc != CPA_OK ? rc : q8_layout(*cfg, *dims).words * 4;
+}
+
+extern "C" int64_t cpa_tables_offset(const cpa_config* cfg, const cpa_table_dims* dims, int which) {
+    const int rc = q8_check(cfg, dims);
+    if (rc != CPA_OK) return rc;
+    const q8_offsets o = q8_layout(*cfg, *dims);
+    switch (which) {
+        case CPA_ARR_CU_SEQLENS: return o.cu * 4;
+        case CPA_ARR_PAGE_INDPTR: return o.indptr * 4;
+        case CPA_ARR_PAGE_INDICES: return o.pages * 4;
+        case CPA_ARR_SLOT_MAPPING: return o.slots * 4;
+        default: return CPA_EINVAL;
+    }
+}
+
+extern "C" int cpa_tables_build(const cpa_config* cfg, const cpa_table_dims* dims, const int32_t* d_block_lens,
+                                const int32_t* d_free_pages, int32_t num_free, void* d_tables, void* stream) {
+    const int rc = q8_check(cfg, dims);
+    if (rc != CPA_OK) return rc;
+    if (!d_block_lens || !d_free_pages || !d_tables || num_free < 0 || !cpa_aligned16(d_tables) ||
+        (reinterpret_cast<uintptr_t>(d_block_lens) & 3u) || (reinterpret_cast<uintptr_t>(d_free_pages) & 3u))
+        return CPA_EINVAL;
+    q8_tables t = q8_view(*cfg, *dims, d_tables);
+    if (dims->token_capacity == 0) t.slot_mapping = nullptr;
+    const int page_limit = std::min(num_free, dims->page_capacity);
+    const int token_limit = dims->token_capacity == 0 ? INT32_MAX : dims->token_capacity;
+    cudaStream_t st = (cudaStream_t)stream;
+    const int grid = std::max(1, std::min(kBuildCtas, std::max(dims->token_capacity, 4 * page_limit) / kTile + 1));
+    tables_build_kernel<<<grid, kThreads, 0, st>>>(t, d_block_lens, d_free_pages, dims->num_blocks, dims->max_new_tokens,
+                                                   dims->num_pages, page_limit, token_limit,
+                                                   dims->num_blocks * cfg->num_kv_heads);
+    return cudaGetLastError() == cudaSuccess ? CPA_OK : CPA_ECUDA;
+}
+
+extern "C" int cpa_tables_status(const void* d_tables, void* stream) {
+    if (!d_tables) return CPA_EINVAL;
+    int32_t head[kHeaderWords] = {};
+    cudaStream_t st = (cudaStream_t)stream;
+    if (cudaMemcpyAsync(head, d_tables, sizeof(head), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CPA_ECUDA;
+    }
+    int32_t word = head[0];
+    for (int i = kBuildWords; i < kBuildWords + kBuildCtas; ++i)
+        if (head[i]) word = head[i];          // faults of the build come first: what followed rests on them
+    return word == 0 ? CPA_OK : word == kStatusNoSpace ? CPA_ENOSPC : word == kStatusInvalid ? CPA_EINVAL : CPA_ETIMEOUT;
+}
