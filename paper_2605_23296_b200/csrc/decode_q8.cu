@@ -21,15 +21,18 @@
 // Weights carry V's page scale into f16, w_j = 2^(s_j + log2 vs - m_o), with a maximum m_o of their own, so that pages
 // whose scales lie far apart neither overflow nor vanish; the denominator keeps the plain maximum m_l.
 //
-// Work: the (block, kv head, page) triples of all blocks are laid end to end and cut into equal ranges, one per CTA of
-// the one wave, from the lengths on the device.  A CTA is one producer warp and four consumer warps around a ring of
-// stages; a stage is a round of up to 4 * TP pages of one (block, kv head), with their scales, and with the queries
-// (first round) and the new rows (last page) that belong to it: the consumers load nothing from global memory.  Consumer
-// w takes pages w, w + 4, ... of a round and keeps its own maxima, sums and O; at the end of a (block, kv head) inside
-// the range the four are merged through the stage that they have just consumed.  A range boundary inside a (block, kv
-// head) leaves partials in the workspace, and the last CTA to arrive (a counter in the tables) merges them in order.
+// Work: the (block, kv head, page) triples of all blocks are laid end to end and cut into ranges from the lengths on the
+// device: one equal range per CTA of the one wave.  (Handing the last sixth out in small ranges as CTAs
+// finish was slower, 116 us for 63: a range costs its producer a search and its merger a join.)  A CTA is four consumer
+// warps, a producer and a merger around a ring of stages; a stage is a round of up to 4 * TP pages of one (block, kv head),
+// with their scales, and with the queries (first round) and the new rows (last page) that belong to it: the consumers
+// load nothing from global memory.  Consumer w takes pages w, w + 4, ... of a round and keeps its own maxima, sums and
+// O; at the end of a (block, kv head) inside a range it leaves them in the stage that it has just consumed and goes on.
+// The merger joins the four from there.  A range boundary inside a (block, kv head) leaves partials in the workspace,
+// and the merger that arrives last (a counter in the tables) joins them in the order of the ranges.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "cache_q8.cuh"
 #include "cpa_tcgen05.cuh"
@@ -37,9 +40,13 @@
 namespace {
 
 constexpr int kCons = 4;                              // consumer warps
-constexpr int kQ8Threads = (kCons + 1) * 32;
+constexpr int kProducer = kCons, kMerger = kCons + 1;  // the other two warps
+constexpr int kQ8Threads = (kCons + 2) * 32;
 constexpr int kCtasPerSm = 2;
 constexpr int kStages = 3;
+constexpr int kAhead = 2;                             // rounds that the producer looks ahead
+constexpr int kUnitCost = 10;                         // what starting and ending a (block, kv head) costs, in pages
+constexpr uint32_t kLongSpin = 1u << 24;              // waits that last for a whole range of pages
 constexpr uint32_t kQ8Spin = 1u << 18;                // bounded waits (each try suspends briefly)
 constexpr float kBase = 6.f, kSlack = 9.f;            // weights: 2^kBase at the maximum, up to 2^(kBase + kSlack) above it
 
@@ -51,8 +58,8 @@ struct Q8Shape {
     static constexpr int kData = kRound * kPageBytes;
     // behind a stage's pages: queries, the new K and V rows, scales, the round's descriptor, and (max, sum, max) of the
     // four warps for the merge
-    static constexpr int kQ = 0, kNew = kQ + 8 * D * 2, kScale = kNew + 2 * D * 2, kDesc = kScale + kRound * 8,
-                         kMl = kDesc + 48, kLast = kMl + kCons * 8 * 16, kMeta = (kLast + 16 + 127) / 128 * 128;
+    static constexpr int kQ = 0, kNew = kQ + 8 * D * 2, kScale = kNew + 2 * D * 2, kDesc = (kScale + kRound * 8 + 15) / 16 * 16,
+                         kMl = kDesc + 48, kMeta = (kMl + kCons * 8 * 16 + 127) / 128 * 128;
     static constexpr int kSmem = kStages * (kData + kMeta) + 1024;
 };
 
@@ -60,12 +67,12 @@ struct round_desc {
     int b, g, page0, n;       // pages [page0, page0 + n) of block b, kv head g; n == 0: the end
     int flags;                // 1: first round of the segment, 2: last, 4: the last page takes the new row
     int len;                  // the block's tokens, the new one included
-    int parts, slot;          // CTAs that share the (block, kv head); this one's partial slot
-    int slot0, last_slot;     // partial slots: slot0 of the first CTA, then the even ones up to last_slot
-    int row;                  // page row of the pages' first code: where the new row goes
-    int pad;
+    int first, parts;         // the first of the CTAs that share the (block, kv head), and how many they are
 };
-static_assert(sizeof(round_desc) == 48, "a descriptor is three 16-byte words");
+
+// CTA r leaves a partial of a (block, kv head) that began before its range in slot 2 r, of one that begins in it and
+// goes on in 2 r + 1.
+__device__ __forceinline__ int slot_of(int r, int first) { return 2 * r + (r == first); }
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
@@ -92,9 +99,32 @@ __device__ __forceinline__ uint2 lds8(uint32_t a) {
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];\n" : "=r"(r.x), "=r"(r.y) : "r"(a));
     return r;
 }
+template <int IMM>
+__device__ __forceinline__ uint4 lds16_at(uint32_t a) {
+    uint4 r;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4 + %5];\n" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a), "n"(IMM));
+    return r;
+}
+template <int IMM>
+__device__ __forceinline__ uint2 lds8_at(uint32_t a) {
+    uint2 r;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2 + %3];\n" : "=r"(r.x), "=r"(r.y) : "r"(a), "n"(IMM));
+    return r;
+}
+__device__ __forceinline__ void sts16(uint32_t a, int x, int y, int z, int w) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" :: "r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// body(0), body(1), ... with the number as a constant
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void static_for(F&& body) {
+    if constexpr (I < N) {
+        body(std::integral_constant<int, I>{});
+        static_for<N, I + 1>(body);
+    }
+}
 __device__ __forceinline__ float ex2(float x) {
     float d;
-    asm("ex2.approx.f32 %0, %1;\n" : "=f"(d) : "f"(x));
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(d) : "f"(x));
     return d;
 }
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -102,8 +132,14 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
                  :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
-__device__ __forceinline__ uint32_t f16_lo(uint32_t w) { return e4m3x2_to_f16x2((uint16_t)w); }
-__device__ __forceinline__ uint32_t f16_hi(uint32_t w) { return e4m3x2_to_f16x2((uint16_t)(w >> 16)); }
+// four codes to two f16 pairs (the halves are named inside the assembly: taken apart in C++ each costs an instruction)
+struct f16x4 { uint32_t lo, hi; };
+__device__ __forceinline__ f16x4 to_f16x4(uint32_t w) {
+    f16x4 r;
+    asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}\n"
+        : "=r"(r.lo), "=r"(r.hi) : "r"(w));
+    return r;
+}
 
 // Byte offset of the 16-byte piece p of token row r inside a swizzled chunk (K or V) of a page.
 template <int D>
@@ -145,7 +181,8 @@ struct q8_args {
     float* ws;                 // [slots, G, D] accumulators, then [slots, G, 4] (max, sum, max of the weights, -)
     int B, Hq, Hkv, G;
     float scale_log2;
-    int min_quota;             // pages of a CTA's range at least
+    int min_quota;             // cells of a range at least
+    int slots;                 // partial slots of the workspace
 };
 
 // Stores a finished row pair: dims d, d + 1 of query head h.
@@ -157,35 +194,101 @@ __device__ __forceinline__ void store_pair(const q8_args& a, int b, int g, int h
         __floats2bfloat162_rn(o0 * inv * e * e, o1 * inv * e * e);
 }
 
+__device__ __forceinline__ float4* partial_ml(const q8_args& a, int D) {
+    return reinterpret_cast<float4*>(a.ws + (int64_t)a.slots * a.G * D);
+}
+// Where a consumer leaves dims 2u, 2u + 1 of head h inside its 8 x D floats: neither it nor the merger meets a bank twice.
+template <int D>
+__device__ __forceinline__ int dump_at(int h, int u) {
+    const int x = D == 128 ? ((u >> 4) & 1) << 2 : 0;
+    return (h * (D / 2) + (u ^ x ^ (h >> 1))) * 8;
+}
+
+// Joins the partials of a (block, kv head), for the heads of one task (128 floats: one head of 128, two of 64), by one
+// warp.  Lane i of a head's D / 4 lanes holds the factors of partial i of a batch and four dimensions of the result.
+constexpr int kJoin = 16;
+template <int D>
+__device__ __forceinline__ void join_partials(const q8_args& a, int blk, int head, int first, int parts, int task, int lane) {
+    constexpr int HL = D / 4;
+    const int sub = lane % HL, h = task * (32 / HL) + lane / HL;
+    const bool there = h < a.G;
+    const float4* ws_ml = partial_ml(a, D);
+    float Ml = -INFINITY, Mo = -INFINITY, L = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int at = 0; at < parts; at += kJoin) {
+        float4 m = make_float4(-INFINITY, 0.f, -INFINITY, 0.f), x[kJoin];
+#pragma unroll
+        for (int i = 0; i < kJoin; ++i)              // all loads of a batch are in flight together
+            x[i] = there && at + i < parts
+                       ? __ldcg(reinterpret_cast<const float4*>(a.ws + ((int64_t)slot_of(first + at + i, first) * a.G + h) * D) + sub)
+                       : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (there && sub < kJoin && at + sub < parts) m = __ldcg(ws_ml + (int64_t)slot_of(first + at + sub, first) * a.G + h);
+        float ml = m.x, mo = m.z;
+#pragma unroll
+        for (int w = HL / 2; w > 0; w >>= 1) {
+            ml = fmaxf(ml, __shfl_xor_sync(0xffffffffu, ml, w));
+            mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, w));
+        }
+        ml = fmaxf(ml, Ml);
+        mo = fmaxf(mo, Mo);
+        const float fl = Ml == -INFINITY ? 0.f : ex2(Ml - ml), fo = Mo == -INFINITY ? 0.f : ex2(Mo - mo);
+        Ml = ml;
+        Mo = mo;
+        // (a partial with a maximum of -inf has met nothing but NaN: its sums are NaN and pass on as they are)
+        L = L * fl + (m.x == -INFINITY ? m.y : ex2(m.x - Ml) * m.y);
+        const float f = m.z == -INFINITY ? 0.f : ex2(m.z - Mo);
+        o.x *= fo; o.y *= fo; o.z *= fo; o.w *= fo;
+#pragma unroll
+        for (int i = 0; i < kJoin; ++i) {
+            const float fi = __shfl_sync(0xffffffffu, f, i, HL);
+            o.x = fmaf(fi, x[i].x, o.x); o.y = fmaf(fi, x[i].y, o.y); o.z = fmaf(fi, x[i].z, o.z); o.w = fmaf(fi, x[i].w, o.w);
+        }
+    }
+#pragma unroll
+    for (int x = HL / 2; x > 0; x >>= 1) L += __shfl_xor_sync(0xffffffffu, L, x);
+    if (there) {
+        store_pair(a, blk, head, h, D, 4 * sub, o.x, o.y, L, Mo, Ml);
+        store_pair(a, blk, head, h, D, 4 * sub + 2, o.z, o.w, L, Mo, Ml);
+    }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kQ8Threads, kCtasPerSm)
 decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
     using Sh = Q8Shape<D>;
     constexpr int TP = Sh::TP;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t sm_full[kStages], sm_empty[kStages], sm_flush;
-    __shared__ int sm_scan[kQ8Threads / 32], sm_start[3];
+    __shared__ __align__(8) uint64_t sm_full[kStages], sm_empty[kStages], sm_dump[kStages], sm_end;
+    __shared__ int sm_scan[kQ8Threads / 32], sm_strip[kQ8Threads], sm_len[kQ8Threads], sm_ip[kQ8Threads], sm_dump_stage[kStages];
+    __shared__ int4 sm_final;                          // a merge that is left to all warps at the end
+    __shared__ volatile int sm_dead;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t data0 = (smem_u32(raw) + 1023u) & ~1023u, meta0 = data0 + kStages * Sh::kData;
-    const uint32_t full0 = smem_u32(sm_full), empty0 = smem_u32(sm_empty), flush_bar = smem_u32(&sm_flush);
+    const uint32_t full0 = smem_u32(sm_full), empty0 = smem_u32(sm_empty), dump0 = smem_u32(sm_dump), end_bar = smem_u32(&sm_end);
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, kCons); }
-        mbar_init(flush_bar, kCons * 32);
+        // full: the producer's announcement and its lanes' scales; empty: the consumers (the merger for them)
+        for (int s = 0; s < kStages; ++s) { mbar_init(full0 + 8 * s, 33); mbar_init(empty0 + 8 * s, kCons); mbar_init(dump0 + 8 * s, kCons); }
+        mbar_init(end_bar, 1);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
-        sm_start[0] = a.B;
+        asm volatile("prefetch.tensormap [%0];\n" :: "l"(&tm) : "memory");
+        sm_dead = 0;
     }
+    // the next launch of the stream may be made ready now (it waits as this one does)
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     // everything above touches nothing that an earlier launch writes; this one may have been started before that one ended
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
 
-    // ---- the cut: every thread takes a run of blocks, and the runs' page counts are scanned
+    // ---- the cut: every thread takes a strip of blocks, and the strips' page counts are scanned
     const int append = a.k_new != nullptr;
     const int run = (a.B + kQ8Threads - 1) / kQ8Threads, b_lo = min(a.B, tid * run), b_hi = min(a.B, b_lo + run);
-    int mine = 0;
+    int mine = 0, my_len = -1, my_ip = 0;
     for (int b = b_lo; b < b_hi; ++b) {
         int ip, status;
         const int len = block_len(b, a.t, a.lens, a.active, append, ip, status);
-        if (len > 0) mine += (len + kPage - 1) / kPage;
+        my_len = len;
+        my_ip = ip;
+        if (len > 0) mine += (len + kPage - 1) / kPage + kUnitCost;
         if (b % (int)gridDim.x != (int)blockIdx.x) continue;
         // this CTA keeps block b's books: status, new length, and the zero row of an empty block
         if (status) atomicCAS(a.t.header, 0, status);
@@ -208,51 +311,94 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
         if (w < warp) before += sm_scan[w];
         total += sm_scan[w];
     }
-    before += inc - mine;
+    sm_strip[tid] = before + inc - mine;               // pages of the blocks in front of the strip
+    if (tid < a.B && run == 1) { sm_len[tid] = my_len; sm_ip[tid] = my_ip; }
     const int64_t all = (int64_t)total * a.Hkv;
     const int64_t quota = max((all + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)a.min_quota);
-    const int64_t x0 = quota * blockIdx.x, x1 = min(x0 + quota, all);
-    if (x0 >= x1) return;                              // (uniform) more CTAs than work
-    if (mine > 0 && x0 >= (int64_t)before * a.Hkv && x0 < (int64_t)(before + mine) * a.Hkv) {
-        int64_t x = (int64_t)before * a.Hkv;
-        for (int b = b_lo; b < b_hi; ++b) {            // the block that the range starts in, and where in it
-            int ip, status;
-            const int len = block_len(b, a.t, a.lens, a.active, append, ip, status);
-            const int64_t units = len > 0 ? (int64_t)((len + kPage - 1) / kPage) * a.Hkv : 0;
-            if (x0 < x + units) {
-                sm_start[0] = b;
-                sm_start[1] = (int)((x0 - x) / (units / a.Hkv));
-                sm_start[2] = (int)((x0 - x) % (units / a.Hkv));
-                break;
-            }
-            x += units;
-        }
-    }
+    const int64_t x0 = quota * blockIdx.x;
+    if (x0 >= all) return;                             // (uniform) more CTAs than work
     __syncthreads();
 
+    const int tasks = (a.G * D + 127) / 128;           // of join_partials
     bool dead = false;
-    if (warp == kCons) {
+    // A wait that gives up ends the warp, and by the flag those that wait for it; every wait is bounded by itself too.
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        mbar_wait(bar, parity, dead, a.t.header, kQ8Spin);
+        if (__any_sync(0xffffffffu, dead)) { dead = true; sm_dead = 1; }
+        return !dead;
+    };
+    auto long_wait = [&](uint32_t bar, uint32_t parity) {
+        uint32_t spins = 0;
+        while (!dead && !mbar_try_wait(bar, parity))
+            if ((++spins & 1023u) == 0 && (sm_dead || spins > kLongSpin)) { dead = true; atomicCAS(a.t.header, 0, kStatusWaitGaveUp); }
+        if (__any_sync(0xffffffffu, dead)) { dead = true; sm_dead = 1; }
+        return !dead;
+    };
+
+    if (warp == kProducer) {
         // ================================================================ producer
         // A window of 32 blocks in the lanes' registers: tokens and first entry of the page list.
-        int win = sm_start[0], w_len, w_ip;
+        int win = 0, w_len, w_ip;
         auto window = [&]() {
             int status;
             w_len = -1;
             w_ip = 0;
-            if (win + lane < a.B) w_len = block_len(win + lane, a.t, a.lens, a.active, append, w_ip, status);
+            if (win + lane >= a.B) return;
+            if (run == 1) { w_len = sm_len[win + lane]; w_ip = sm_ip[win + lane]; }
+            else w_len = block_len(win + lane, a.t, a.lens, a.active, append, w_ip, status);
         };
-        window();
-        int b = sm_start[0], g = sm_start[1], p = sm_start[2];
-        int64_t left = x1 - x0, unit0 = x0 - p;         // pages of the range still to hand out; where this unit starts
-        int len = __shfl_sync(0xffffffffu, w_len, 0), ip = __shfl_sync(0xffffffffu, w_ip, 0);
-        int pages = (len + kPage - 1) / kPage;
+        int b = 0, g = 0, p = 0, len = 0, ip = 0, pages = 0;
+        const int64_t x = x0;
+        int64_t left = min(quota, all - x0), unit0 = 0;  // cells of the range still to hand out; where this unit starts
         bool opened = false;                            // a round of this unit has been handed out
-        // the next round of the range into `r`; its page list entries start at `ids`
-        auto next = [&](round_desc& r, int& ids) {
+        int parts = 0, first = 0;
+        // to the start of the range: the strip that holds it, the block in the strip, head and page in the block
+        auto locate = [&]() {
+            int lo = 0, hi = kQ8Threads - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if ((int64_t)sm_strip[mid] * a.Hkv <= x) lo = mid; else hi = mid - 1;
+            }
+            int64_t at = (int64_t)sm_strip[lo] * a.Hkv;
+            win = lo * run;
+            for (;;) {
+                window();
+                int sum = w_len > 0 ? (w_len + kPage - 1) / kPage + kUnitCost : 0;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int v = __shfl_up_sync(0xffffffffu, sum, o);
+                    if (lane >= o) sum += v;
+                }
+                const uint32_t past = __ballot_sync(0xffffffffu, at + (int64_t)sum * a.Hkv > x);
+                if (past) {
+                    const int l = __ffs(past) - 1;
+                    b = win + l;
+                    len = __shfl_sync(0xffffffffu, w_len, l);
+                    ip = __shfl_sync(0xffffffffu, w_ip, l);
+                    pages = (len + kPage - 1) / kPage;
+                    const int cells = pages + kUnitCost;
+                    const int64_t in = x - at - (int64_t)(__shfl_sync(0xffffffffu, sum, l) - cells) * a.Hkv;
+                    g = (int)(in / cells);
+                    p = (int)(in % cells);
+                    unit0 = x - p;
+                    if (p > pages) { left += p - pages; p = pages; }   // (the cells behind the pages stand for the unit's cost)
+                    opened = false;
+                    return;
+                }
+                at += (int64_t)__shfl_sync(0xffffffffu, sum, 31) * a.Hkv;
+                win += 32;
+                if (win >= a.B) { left = 0; return; }    // (cannot be reached: the range starts inside the blocks)
+            }
+        };
+        locate();
+        // the next round into `r`, and each lane's page of it
+        auto next = [&](round_desc& r, int& id) {
             r.n = 0;
             if (left <= 0) return;
             if (p == pages) {                           // on to the next kv head, or the next block that has pages
-                unit0 += pages;
+                unit0 += pages + kUnitCost;
+                left -= kUnitCost;
+                if (left <= 0) return;
                 p = 0;
                 opened = false;
                 if (++g == a.Hkv) {
@@ -261,82 +407,73 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                         if (++b >= win + 32) { win = b; window(); }
                         len = __shfl_sync(0xffffffffu, w_len, b - win);
                     } while (len <= 0 && b < a.B);
-                    if (b >= a.B) { left = 0; return; }  // (cannot be reached: the range ends inside the blocks)
+                    if (b >= a.B) { left = 0; return; }  // (cannot be reached: ranges end inside the blocks)
                     ip = __shfl_sync(0xffffffffu, w_ip, b - win);
                     pages = (len + kPage - 1) / kPage;
                 }
+            }
+            r.flags = 0;
+            if (!opened) {
+                first = (int)(unit0 / quota);
+                parts = (int)((unit0 + pages - 1) / quota) - first + 1;
+                r.flags = 1;
+                opened = true;
             }
             r.b = b;
             r.g = g;
             r.page0 = p;
             r.n = (int)min((int64_t)min(pages - p, Sh::kRound), left);
             r.len = len;
-            ids = ip + p;
+            r.first = first;
+            r.parts = parts;
+            id = lane < r.n ? __ldg(a.t.page_indices + ip + p + lane) : 0;
             p += r.n;
             left -= r.n;
-            r.flags = (opened ? 0 : 1) | (p == pages || left == 0 ? 2 : 0) | (append && p == pages ? 4 : 0);
-            opened = true;
-            const int64_t c0 = unit0 / quota, c1 = (unit0 + pages - 1) / quota;
-            r.parts = (int)(c1 - c0) + 1;
-            r.slot0 = (int)(2 * c0 + 1);
-            r.last_slot = (int)(2 * c1);
-            r.slot = (int)blockIdx.x == (int)c0 ? r.slot0 : 2 * (int)blockIdx.x;
-            r.pad = 0;
+            r.flags |= (p == pages || left == 0 ? 2 : 0) | (append && p == pages ? 4 : 0);
         };
-        // three rounds in flight: descriptor and page ids two ahead, scales one ahead
-        round_desc d0, d1, d2;
-        int at = 0, id0 = 0, id1 = 0, id2 = 0;
-        float2 sc0 = make_float2(0.f, 0.f), sc1 = sc0;
-        next(d0, at);
-        if (lane < d0.n) id0 = __ldg(a.t.page_indices + at + lane);
-        next(d1, at);
-        if (lane < d1.n) id1 = __ldg(a.t.page_indices + at + lane);
-        // (scales are read past the caches that __ldg may use: the append writes them in this launch)
-        if (lane < d0.n) sc0 = __ldcg(reinterpret_cast<const float2*>(a.scales) + (int64_t)id0 * a.Hkv + d0.g);
+        // Descriptors and page ids run kAhead rounds in front of the copies, so that no load is waited for.
+        round_desc d[kAhead + 1];
+        int id[kAhead + 1];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) next(d[i], id[i]);
         int it = 0;
         for (;; ++it) {
-            next(d2, at);
-            id2 = 0;
-            if (lane < d2.n) id2 = __ldg(a.t.page_indices + at + lane);
-            if (lane < d1.n) sc1 = __ldcg(reinterpret_cast<const float2*>(a.scales) + (int64_t)id1 * a.Hkv + d1.g);
+            next(d[kAhead], id[kAhead]);
             const int st = it % kStages;
-            if (it >= kStages) mbar_wait(empty0 + 8 * st, (uint32_t)(it / kStages - 1) & 1u, dead, a.t.header, kQ8Spin);
-            if (__any_sync(0xffffffffu, dead)) break;
+            if (it >= kStages && !wait(empty0 + 8 * st, (uint32_t)(it / kStages - 1) & 1u)) break;
             const uint32_t data = data0 + st * Sh::kData, meta = meta0 + st * Sh::kMeta, bar = full0 + 8 * st;
-            d0.row = (id0 * a.Hkv + d0.g);
-            d0.row = __shfl_sync(0xffffffffu, d0.row, d0.n > 0 ? d0.n - 1 : 0);    // (page, head) of the round's last page
-            if (lane < d0.n) {
-                asm volatile("st.shared.v2.f32 [%0], {%1,%2};\n" :: "r"(meta + Sh::kScale + 8 * lane), "f"(sc0.x), "f"(sc0.y) : "memory");
-            }
+            const int cell = id[0] * a.Hkv + d[0].g;    // (page, kv head)
+            const int last_cell = __shfl_sync(0xffffffffu, cell, d[0].n > 0 ? d[0].n - 1 : 0);
             if (lane == 0) {
-                const int4* w = reinterpret_cast<const int4*>(&d0);
-                for (int i = 0; i < 3; ++i)
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n"
-                                 :: "r"(meta + Sh::kDesc + 16 * i), "r"(w[i].x), "r"(w[i].y), "r"(w[i].z), "r"(w[i].w) : "memory");
+                sts16(meta + Sh::kDesc, d[0].b, d[0].g, d[0].page0, d[0].n);
+                sts16(meta + Sh::kDesc + 16, d[0].flags, d[0].len, d[0].first, d[0].parts);
+                sts16(meta + Sh::kDesc + 32, last_cell, 0, 0, 0);
+                if (d[0].n > 0)
+                    mbar_expect_tx(bar, d[0].n * Sh::kPageBytes + (d[0].flags & 1 ? a.G * D * 2 : 0) + (d[0].flags & 4 ? 2 * D * 2 : 0));
+                else
+                    mbar_arrive(bar);                   // the end: no copies
             }
             __syncwarp();
-            if (d0.n == 0) {                            // the end: no copies, the stage is complete at once
-                if (lane == 0) mbar_arrive(bar);
-                break;
+            if (lane < d[0].n) {
+                tma_load_2d(data + lane * Sh::kPageBytes, &tm, 0, cell * (Sh::kPageBytes / 128), bar);
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8;\n"
+                             :: "r"(meta + Sh::kScale + 8 * lane), "l"(a.scales + (int64_t)cell * 2) : "memory");
             }
+            // every lane's arrival, once its scale has landed
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" :: "r"(bar) : "memory");
+            if (d[0].n == 0) break;
             if (lane == 0) {
-                mbar_expect_tx(bar, d0.n * Sh::kPageBytes + (d0.flags & 1 ? a.G * D * 2 : 0) + (d0.flags & 4 ? 2 * D * 2 : 0));
-                if (d0.flags & 1) bulk_copy(meta + Sh::kQ, a.q + ((int64_t)d0.b * a.Hq + d0.g * a.G) * D, a.G * D * 2, bar);
-                if (d0.flags & 4) {
-                    const int64_t row = ((int64_t)d0.b * a.Hkv + d0.g) * D;
+                if (d[0].flags & 1) bulk_copy(meta + Sh::kQ, a.q + ((int64_t)d[0].b * a.Hq + d[0].g * a.G) * D, a.G * D * 2, bar);
+                if (d[0].flags & 4) {
+                    const int64_t row = ((int64_t)d[0].b * a.Hkv + d[0].g) * D;
                     bulk_copy(meta + Sh::kNew, a.k_new + row, D * 2, bar);
                     bulk_copy(meta + Sh::kNew + D * 2, a.v_new + row, D * 2, bar);
                 }
             }
-            __syncwarp();
-            if (lane < d0.n) tma_load_2d(data + lane * Sh::kPageBytes, &tm, 0, (id0 * a.Hkv + d0.g) * (Sh::kPageBytes / 128), bar);
-            d0 = d1;
-            d1 = d2;
-            id0 = id1;
-            id1 = id2;
-            sc0 = sc1;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) { d[i] = d[i + 1]; id[i] = id[i + 1]; }
         }
-        if (__any_sync(0xffffffffu, dead)) {            // a wait gave up: see the copies in flight through before leaving
+        if (dead) {                                     // a wait gave up: see the copies in flight through before leaving
             if (lane == 0)
                 for (int i = max(0, it - kStages); i < it; ++i)
                     mbar_drain(full0 + 8 * (i % kStages), (uint32_t)(i / kStages) & 1u, kDrainLimit);
@@ -345,15 +482,94 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
         return;
     }
 
+    if (warp == kMerger) {
+        // ================================================================ merger
+        for (int k = 0;; ++k) {
+            if (!long_wait(dump0 + 8 * (k % kStages), (uint32_t)(k / kStages) & 1u)) return;
+            const int st = sm_dump_stage[k % kStages];
+            if (st < 0) break;
+            const uint32_t data = data0 + st * Sh::kData, meta = meta0 + st * Sh::kMeta;
+            const uint4 e0 = lds16(meta + Sh::kDesc), e1 = lds16(meta + Sh::kDesc + 16);
+            const int blk = (int)e0.x, head = (int)e0.y, first = (int)e1.z, parts = (int)e1.w;
+            const int64_t row0 = (int64_t)slot_of((int)blockIdx.x, first) * a.G;
+            for (int h = 0; h < a.G; ++h) {
+                float Ml = -INFINITY, Mo = -INFINITY, L = 0.f, f[kCons];
+                float4 m[kCons];
+#pragma unroll
+                for (int w = 0; w < kCons; ++w) {
+                    const uint4 x = lds16(meta + Sh::kMl + (w * 8 + h) * 16);
+                    m[w] = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), 0.f);
+                    Ml = fmaxf(Ml, m[w].x);
+                    Mo = fmaxf(Mo, m[w].z);
+                }
+#pragma unroll
+                for (int w = 0; w < kCons; ++w) {
+                    // (a warp that had no page holds zeros under a maximum of -inf)
+                    f[w] = m[w].z == -INFINITY ? 0.f : ex2(m[w].z - Mo);
+                    L += m[w].x == -INFINITY ? m[w].y : ex2(m[w].x - Ml) * m[w].y;
+                }
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    const int u = lane + 32 * i;
+                    float o0 = 0.f, o1 = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kCons; ++w) {
+                        const uint2 x = lds8(data + w * Sh::kPageBytes + dump_at<D>(h, u));
+                        o0 = fmaf(f[w], __uint_as_float(x.x), o0);
+                        o1 = fmaf(f[w], __uint_as_float(x.y), o1);
+                    }
+                    if (parts == 1) store_pair(a, blk, head, h, D, 2 * u, o0, o1, L, Mo, Ml);
+                    else *reinterpret_cast<float2*>(a.ws + (row0 + h) * D + 2 * u) = make_float2(o0, o1);
+                }
+                if (parts > 1 && lane == 0) partial_ml(a, D)[row0 + h] = make_float4(Ml, L, Mo, 0.f);
+            }
+            __syncwarp();
+            if (lane < kCons) mbar_arrive(empty0 + 8 * st);      // for the four consumers
+            if (parts == 1) continue;
+            unsigned before_me = 0;
+            __threadfence();                                     // this lane's part of the partial, then the count
+            __syncwarp();
+            if (lane == 0)
+                before_me = atomicInc(reinterpret_cast<unsigned*>(a.t.tickets) + (int64_t)blk * a.Hkv + head,
+                                      (unsigned)parts - 1);      // back to zero with the last one
+            before_me = __shfl_sync(0xffffffffu, before_me, 0);
+            if (before_me != (unsigned)parts - 1) continue;
+            __threadfence();
+            // The last one in joins the partials: at the end of the CTA's work with all warps, else in the background.
+            const int nk = k + 1;
+            bool end = false;
+            if (mbar_try_wait(dump0 + 8 * (nk % kStages), (uint32_t)(nk / kStages) & 1u)) end = sm_dump_stage[nk % kStages] < 0;
+            end = __all_sync(0xffffffffu, end);
+            if (end) {
+                if (lane == 0) { sm_final = make_int4(blk, head, first, parts); mbar_arrive(end_bar); }
+                for (int task = kCons; task < tasks; task += kCons + 1) join_partials<D>(a, blk, head, first, parts, task, lane);
+                return;
+            }
+            for (int task = 0; task < tasks; ++task)
+                join_partials<D>(a, blk, head, first, parts, task, lane);
+        }
+        if (lane == 0) { sm_final = make_int4(0, 0, 0, 0); mbar_arrive(end_bar); }
+        return;
+    }
+
     // ==================================================================== consumers
     const int g8 = lane >> 2, t4 = lane & 3;
-    uint32_t flush_phase = 0;
-    auto flush_wait = [&]() {                           // all consumer threads, bounded
-        mbar_arrive(flush_bar);
-        mbar_wait(flush_bar, flush_phase, dead, a.t.header, kQ8Spin);
-        flush_phase ^= 1u;
-        dead = __any_sync(0xffffffffu, dead);
-    };
+    int segment = 0;
+    // this lane's places in a page (its own first page of a round): K rows key(g) and key(g + 8), V rows key(2t) ...
+    const uint32_t own_page = warp * Sh::kPageBytes;
+    uint32_t k_off[2], v_off[4];
+    if (D == 128) {                                     // rows 8 apart have the same swizzle, the other piece has not
+        k_off[0] = own_page + piece_at<D>(key_of_row<D>(g8), t4);
+        k_off[1] = own_page + piece_at<D>(key_of_row<D>(g8), t4 + 4);
+    } else {
+        k_off[0] = own_page + piece_at<D>(key_of_row<D>(g8), t4);
+        k_off[1] = own_page + piece_at<D>(key_of_row<D>(g8 + 8), t4);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int key = key_of_row<D>(2 * t4 + (r & 1) + 8 * (r >> 1));
+        v_off[r] = own_page + (D == 128 ? piece_at<D>(key, g8) : piece_at<D>(key, g8 >> 1) + (g8 & 1) * 8);
+    }
     uint32_t qf[D / 64][4][2];
     float acc[D / 16][4], c0 = 0.f, c1 = 0.f;           // c: what a score's sum is multiplied with, for heads 2t, 2t + 1
     float ml0 = -INFINITY, ml1 = -INFINITY, mo0 = -INFINITY, mo1 = -INFINITY, l0 = 0.f, l1 = 0.f;
@@ -361,11 +577,10 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
     for (int it = 0;; ++it) {
         const int st = it % kStages;
         const uint32_t data = data0 + st * Sh::kData, meta = meta0 + st * Sh::kMeta;
-        mbar_wait(full0 + 8 * st, (uint32_t)(it / kStages) & 1u, dead, a.t.header, kQ8Spin);
-        if (__any_sync(0xffffffffu, dead)) return;
+        if (!wait(full0 + 8 * st, (uint32_t)(it / kStages) & 1u)) return;
         const uint4 e0 = lds16(meta + Sh::kDesc), e1 = lds16(meta + Sh::kDesc + 16);
         const int page0 = (int)e0.z, n = (int)e0.w, flags = (int)e1.x, len = (int)e1.y;
-        if (n == 0) return;
+        if (n == 0) break;
         if (flags & 1) {
             // the queries as f16 B fragments: contracted elements 2t, 2t+1, 2t+8, 2t+9 of step (p, w) are dimensions
             // 64 p + 16 t + 4 w + 0 .. 3.  2^7 at the row's largest element.
@@ -410,7 +625,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             // ---- the block's newest page is this warp's: quantise the new row into it, here and in the pool
             const int slot = (len - 1) % kPage, j = n - 1;
             const uint32_t chunk0 = data + j * Sh::kPageBytes;
-            const int64_t cell = (int64_t)(int)lds16(meta + Sh::kDesc + 32).z;       // page * Hkv + g
+            const int64_t cell = (int64_t)(int)lds16(meta + Sh::kDesc + 32).x;       // page * Hkv + g
 #pragma unroll
             for (int kind = 0; kind < 2; ++kind) {
                 const uint32_t chunk = chunk0 + kind * (kPage * D);
@@ -469,47 +684,57 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             __syncwarp();
         }
 
+        // ---- slots behind the block's tokens may hold anything, a NaN among it that a weight of zero would not silence
+        const int cut_page = warp + kCons * (n_mine - 1), cut_at = len - (page0 + cut_page) * kPage;
+        if (n_mine > 0 && cut_at < kPage) {
+            for (int i = lane; i < (kPage - cut_at) * (D / 16); i += 32) {
+                const int r = cut_at + i / (D / 16);
+                sts16(data + cut_page * Sh::kPageBytes + kPage * D + piece_at<D>(r, i % (D / 16)), 0, 0, 0, 0);
+            }
+            fence_async();
+            __syncwarp();
+        }
         // ---- scores of this warp's pages: s[i] = (key(g), head 2t), (key(g), 2t+1), (key(g+8), 2t), (key(g+8), 2t+1)
         float s[TP][4], lv[TP];
         float hi0 = -INFINITY, hi1 = -INFINITY, ho0 = -INFINITY, ho1 = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < TP; ++i) {
+        const uint32_t ka = data + k_off[0], kb = data + k_off[1];
+        static_for<TP>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, at = kCons * i * Sh::kPageBytes;
             if (i >= n_mine) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[i][e] = -INFINITY;
                 lv[i] = 0.f;
-                continue;
+                return;
             }
             const int j = warp + kCons * i;
-            const uint32_t kc = data + j * Sh::kPageBytes;
             const uint2 sc = lds8(meta + Sh::kScale + 8 * j);
-            float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};
+            // rows key(g) and key(g + 8); at 128, pieces t and t + 4 of each
+            const uint4 r0 = lds16_at<at>(ka), r1 = D == 128 ? lds16_at<at + 1024>(ka) : lds16_at<at>(kb);
+            const uint4 r2 = D == 128 ? lds16_at<at>(kb) : r0, r3 = D == 128 ? lds16_at<at + 1024>(kb) : r1;
+            const uint32_t w0[8] = {r0.x, r0.y, r0.z, r0.w, r2.x, r2.y, r2.z, r2.w};
+            const uint32_t w1[8] = {r1.x, r1.y, r1.z, r1.w, r3.x, r3.y, r3.z, r3.w};
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int p = 0; p < D / 64; ++p) {
-                const uint4 r0 = lds16(kc + piece_at<D>(key_of_row<D>(g8), t4 + 4 * p));
-                const uint4 r1 = lds16(kc + piece_at<D>(key_of_row<D>(g8 + 8), t4 + 4 * p));
-                mma_f16(sa, f16_lo(r0.x), f16_lo(r1.x), f16_hi(r0.x), f16_hi(r1.x), qf[p][0][0], qf[p][0][1]);
-                mma_f16(sb, f16_lo(r0.y), f16_lo(r1.y), f16_hi(r0.y), f16_hi(r1.y), qf[p][1][0], qf[p][1][1]);
-                mma_f16(sa, f16_lo(r0.z), f16_lo(r1.z), f16_hi(r0.z), f16_hi(r1.z), qf[p][2][0], qf[p][2][1]);
-                mma_f16(sb, f16_lo(r0.w), f16_lo(r1.w), f16_hi(r0.w), f16_hi(r1.w), qf[p][3][0], qf[p][3][1]);
+            for (int w = 0; w < D / 16; ++w) {
+                const f16x4 x0 = to_f16x4(w0[w]), x1 = to_f16x4(w1[w]);
+                mma_f16(sum, x0.lo, x1.lo, x0.hi, x1.hi, qf[w >> 2][w & 3][0], qf[w >> 2][w & 3][1]);
             }
             const float ks = __uint_as_float(sc.x), k0 = ks * c0, k1 = ks * c1;
-            s[i][0] = (sa[0] + sb[0]) * k0;
-            s[i][1] = (sa[1] + sb[1]) * k1;
-            s[i][2] = (sa[2] + sb[2]) * k0;
-            s[i][3] = (sa[3] + sb[3]) * k1;
-            asm("lg2.approx.f32 %0, %1;\n" : "=f"(lv[i]) : "f"(__uint_as_float(sc.y)));
-            const int valid = len - (page0 + j) * kPage;     // slots behind it may hold anything
-            if (valid < kPage) {
-                if (key_of_row<D>(g8) >= valid) s[i][0] = s[i][1] = -INFINITY;
-                if (key_of_row<D>(g8 + 8) >= valid) s[i][2] = s[i][3] = -INFINITY;
+            s[i][0] = sum[0] * k0;
+            s[i][1] = sum[1] * k1;
+            s[i][2] = sum[2] * k0;
+            s[i][3] = sum[3] * k1;
+            asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(lv[i]) : "f"(__uint_as_float(sc.y)));
+            if (j == cut_page && cut_at < kPage) {
+                if (key_of_row<D>(g8) >= cut_at) s[i][0] = s[i][1] = -INFINITY;
+                if (key_of_row<D>(g8 + 8) >= cut_at) s[i][2] = s[i][3] = -INFINITY;
             }
             const float a0 = fmaxf(s[i][0], s[i][2]), a1 = fmaxf(s[i][1], s[i][3]);
             hi0 = fmaxf(hi0, a0);
             hi1 = fmaxf(hi1, a1);
             ho0 = fmaxf(ho0, a0 + lv[i]);
             ho1 = fmaxf(ho1, a1 + lv[i]);
-        }
+        });
         if (n_mine > 0) {
             // ---- raise the maxima when a score has passed them by more than the headroom (always at the first page)
             const bool passed = hi0 > ml0 + kSlack || hi1 > ml1 + kSlack || ho0 > mo0 + kSlack || ho1 > mo1 + kSlack;
@@ -534,32 +759,27 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             }
             // ---- weights, and O^T += V^T P^T
             const float b0 = kBase - mo0, b1 = kBase - mo1;
+            uint32_t va[4];
 #pragma unroll
-            for (int i = 0; i < TP; ++i) {
-                if (i >= n_mine) continue;
-                const int j = warp + kCons * i;
+            for (int r = 0; r < 4; ++r) va[r] = data + v_off[r];
+            static_for<TP>([&](auto ic) {
+                constexpr int i = decltype(ic)::value, at = kCons * i * Sh::kPageBytes + kPage * D;
+                if (i >= n_mine) return;
                 l0 += ex2(s[i][0] - ml0) + ex2(s[i][2] - ml0);
                 l1 += ex2(s[i][1] - ml1) + ex2(s[i][3] - ml1);
                 const float u0 = b0 + lv[i], u1 = b1 + lv[i];
                 const uint32_t p0 = transpose8(pack_f16(ex2(s[i][0] + u0), ex2(s[i][1] + u1)));
                 const uint32_t p1 = transpose8(pack_f16(ex2(s[i][2] + u0), ex2(s[i][3] + u1)));
-                const uint32_t vc = data + j * Sh::kPageBytes + kPage * D;
-                const int valid = len - (page0 + j) * kPage;
                 constexpr int W = D / 32;                    // words of codes per lane and key
-                uint32_t v[4][W];
+                uint32_t v[4][W];                            // keys key(2t), key(2t + 1), key(2t + 8), key(2t + 9)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int key = key_of_row<D>(2 * t4 + (r & 1) + 8 * (r >> 1));
-                    if (D == 128) {
-                        const uint4 x = lds16(vc + piece_at<D>(key, g8));
-                        v[r][0] = x.x; v[r][1] = x.y; v[r][W - 2] = x.z; v[r][W - 1] = x.w;
+                    if constexpr (D == 128) {
+                        const uint4 x = r < 2 ? lds16_at<at>(va[r]) : lds16_at<at + 1024>(va[r - 2]);
+                        v[r][0] = x.x; v[r][1] = x.y; v[r][2] = x.z; v[r][3] = x.w;
                     } else {
-                        const uint2 x = lds8(vc + piece_at<D>(key, g8 >> 1) + (g8 & 1) * 8);
+                        const uint2 x = lds8_at<at>(va[r]);
                         v[r][0] = x.x; v[r][1] = x.y;
-                    }
-                    if (valid < kPage && key >= valid) {     // a weight of zero would not silence a NaN
-#pragma unroll
-                        for (int w = 0; w < W; ++w) v[r][w] = 0u;
                     }
                 }
 #pragma unroll
@@ -567,10 +787,11 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                     // codes of two keys side by side: (dims 0, 1 of the word) and (dims 2, 3)
                     const uint32_t a01 = __byte_perm(v[0][w], v[1][w], 0x5140), a23 = __byte_perm(v[0][w], v[1][w], 0x7362);
                     const uint32_t b01 = __byte_perm(v[2][w], v[3][w], 0x5140), b23 = __byte_perm(v[2][w], v[3][w], 0x7362);
-                    mma_f16(acc[2 * w], f16_lo(a01), f16_hi(a01), f16_lo(b01), f16_hi(b01), p0, p1);
-                    mma_f16(acc[2 * w + 1], f16_lo(a23), f16_hi(a23), f16_lo(b23), f16_hi(b23), p0, p1);
+                    const f16x4 xa = to_f16x4(a01), xb = to_f16x4(b01), ya = to_f16x4(a23), yb = to_f16x4(b23);
+                    mma_f16(acc[2 * w], xa.lo, xa.hi, xb.lo, xb.hi, p0, p1);
+                    mma_f16(acc[2 * w + 1], ya.lo, ya.hi, yb.lo, yb.hi, p0, p1);
                 }
-            }
+            });
         }
         __syncwarp();
         if (!(flags & 2)) {
@@ -578,111 +799,42 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             continue;
         }
 
-        // ---- the segment is done: merge the four warps through the stage (each writes over its own first page)
+        // ---- the segment is done: leave O and the sums to the merger, over this warp's first page of the round
         l0 += __shfl_xor_sync(0xffffffffu, l0, 4);
         l1 += __shfl_xor_sync(0xffffffffu, l1, 4);
         l0 += __shfl_xor_sync(0xffffffffu, l0, 8);
         l1 += __shfl_xor_sync(0xffffffffu, l1, 8);
         l0 += __shfl_xor_sync(0xffffffffu, l0, 16);
         l1 += __shfl_xor_sync(0xffffffffu, l1, 16);
-        // row h of [8][D] floats, as pairs: pair u sits at u ^ swz(u, h), so that neither side meets a bank twice
-        auto pair_at = [](int h, int u) {
-            const int x = D == 128 ? ((u >> 4) & 1) << 2 : 0;
-            return (h * (D / 2) + (u ^ x ^ (h >> 1))) * 8;
-        };
         const uint32_t mine_o = data + warp * Sh::kPageBytes;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
             const int u = g8 * (D / 16) + j;                 // dims 2u, 2u + 1 = rows g, g + 8 of tile j
-            asm volatile("st.shared.v2.f32 [%0], {%1,%2};\n" :: "r"(mine_o + pair_at(2 * t4, u)), "f"(acc[j][0]), "f"(acc[j][2]) : "memory");
-            asm volatile("st.shared.v2.f32 [%0], {%1,%2};\n" :: "r"(mine_o + pair_at(2 * t4 + 1, u)), "f"(acc[j][1]), "f"(acc[j][3]) : "memory");
+            asm volatile("st.shared.v2.f32 [%0], {%1,%2};\n" :: "r"(mine_o + dump_at<D>(2 * t4, u)), "f"(acc[j][0]), "f"(acc[j][2]) : "memory");
+            asm volatile("st.shared.v2.f32 [%0], {%1,%2};\n" :: "r"(mine_o + dump_at<D>(2 * t4 + 1, u)), "f"(acc[j][1]), "f"(acc[j][3]) : "memory");
         }
         if (g8 == 0) {
             const uint32_t to = meta + Sh::kMl + (warp * 8 + 2 * t4) * 16;
             asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%3};\n" :: "r"(to), "f"(ml0), "f"(l0), "f"(mo0) : "memory");
             asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%3};\n" :: "r"(to + 16), "f"(ml1), "f"(l1), "f"(mo1) : "memory");
         }
-        fence_async();
-        flush_wait();
-        if (dead) return;
-        const int blk = (int)e0.x, head = (int)e0.y;
-        const uint4 e2 = lds16(meta + Sh::kDesc + 32);
-        const int parts = (int)e1.z, slot = (int)e1.w, slot0 = (int)e2.x, last_slot = (int)e2.y;
-        float* ws_o = a.ws;
-        float4* ws_ml = reinterpret_cast<float4*>(a.ws + (int64_t)2 * gridDim.x * a.G * D);
-        for (int i = tid; i < a.G * (D / 2); i += kCons * 32) {
-            const int h = i / (D / 2), u = i % (D / 2);
-            float4 m[kCons];
-            float Ml = -INFINITY, Mo = -INFINITY, L = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll
-            for (int w = 0; w < kCons; ++w) {
-                const uint4 x = lds16(meta + Sh::kMl + (w * 8 + h) * 16);
-                m[w] = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), 0.f);
-                Ml = fmaxf(Ml, m[w].x);
-                Mo = fmaxf(Mo, m[w].z);
-            }
-#pragma unroll
-            for (int w = 0; w < kCons; ++w) {
-                const uint2 x = lds8(data + w * Sh::kPageBytes + pair_at(h, u));
-                const float f = m[w].z == -INFINITY ? 0.f : ex2(m[w].z - Mo);
-                // (a warp that had no page holds zeros under a maximum of -inf)
-                L += m[w].x == -INFINITY ? m[w].y : ex2(m[w].x - Ml) * m[w].y;
-                o0 = fmaf(f, __uint_as_float(x.x), o0);
-                o1 = fmaf(f, __uint_as_float(x.y), o1);
-            }
-            if (parts == 1) {
-                store_pair(a, blk, head, h, D, 2 * u, o0, o1, L, Mo, Ml);
-            } else {
-                const int64_t row = (int64_t)slot * a.G + h;
-                *reinterpret_cast<float2*>(ws_o + row * D + 2 * u) = make_float2(o0, o1);
-                if (u == 0) ws_ml[row] = make_float4(Ml, L, Mo, 0.f);
-            }
-        }
-        if (parts > 1) {
-            // ---- the last of the CTAs that share this (block, kv head) merges their partials, in order
-            __threadfence();
-            flush_wait();
-            if (dead) return;
-            if (tid == 0) {
-                __threadfence();
-                const unsigned before_me = atomicInc(reinterpret_cast<unsigned*>(a.t.tickets) + (int64_t)blk * a.Hkv + head,
-                                                     (unsigned)parts - 1);           // back to zero with the last one
-                asm volatile("st.shared.u32 [%0], %1;\n" :: "r"(meta + Sh::kLast), "r"(before_me == (unsigned)parts - 1 ? 1u : 0u) : "memory");
-            }
-            flush_wait();
-            if (dead) return;
-            uint32_t last;
-            asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(last) : "r"(meta + Sh::kLast));
-            if (last) {
-                __threadfence();
-                auto slot_of = [&](int i) { return i == 0 ? slot0 : slot0 + 2 * i - 1; };
-                (void)last_slot;
-                for (int i = tid; i < a.G * (D / 2); i += kCons * 32) {
-                    const int h = i / (D / 2), u = i % (D / 2);
-                    float Ml = -INFINITY, Mo = -INFINITY, L = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll 4
-                    for (int k = 0; k < parts; ++k) {
-                        const float4 m = __ldcg(ws_ml + (int64_t)slot_of(k) * a.G + h);
-                        Ml = fmaxf(Ml, m.x);
-                        Mo = fmaxf(Mo, m.z);
-                    }
-#pragma unroll 4
-                    for (int k = 0; k < parts; ++k) {
-                        const int64_t row = (int64_t)slot_of(k) * a.G + h;
-                        const float4 m = __ldcg(ws_ml + row);
-                        const float2 x = __ldcg(reinterpret_cast<const float2*>(ws_o + row * D + 2 * u));
-                        const float f = ex2(m.z - Mo);
-                        L = fmaf(ex2(m.x - Ml), m.y, L);
-                        o0 = fmaf(f, x.x, o0);
-                        o1 = fmaf(f, x.y, o1);
-                    }
-                    store_pair(a, blk, head, h, D, 2 * u, o0, o1, L, Mo, Ml);
-                }
-            }
-        }
+        // Entry `segment` of the merger's queue.  Its place is free: the entry before it in that place belonged to a
+        // segment whose stage has been handed back, or this one could not have got one.
+        if (warp == 0 && lane == 0) sm_dump_stage[segment % kStages] = st;
+        fence_async();                                       // the copy that refills the stage comes after these stores
         __syncwarp();
-        if (lane == 0) mbar_arrive(empty0 + 8 * st);
+        if (lane == 0) mbar_arrive(dump0 + 8 * (segment % kStages));
+        ++segment;
     }
+    // ---- the end: tell the merger, and help it with what it finds to be joined last
+    if (warp == 0 && lane == 0) sm_dump_stage[segment % kStages] = -1;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(dump0 + 8 * (segment % kStages));
+    if (!long_wait(end_bar, 0)) return;
+    const int4 fin = sm_final;
+    if (fin.w > 0)
+        for (int task = warp; task < tasks; task += kCons + 1)
+            join_partials<D>(a, fin.x, fin.y, fin.z, fin.w, task, lane);
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -702,6 +854,11 @@ int device_sms(int dev) {
 }
 
 constexpr int kSmsByDefault = 148;                     // what the workspace is sized for when num_sms is 0
+
+// Two partial slots per CTA.
+int partial_slots(const cpa_config* cfg) {
+    return 2 * kCtasPerSm * (cfg->num_sms ? cfg->num_sms : kSmsByDefault);
+}
 
 template <int D>
 int launch_q8(const cpa_config* cfg, const cpa_table_dims* dims, q8_args& a, cudaStream_t st) {
@@ -729,6 +886,7 @@ int launch_q8(const cpa_config* cfg, const cpa_table_dims* dims, q8_args& a, cud
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return CPA_ECUDA;
     a.min_quota = Sh::kRound;
+    a.slots = partial_slots(cfg);
     // one wave; no more CTAs than the table's pages could keep busy, or the blocks' books need
     const int64_t most = ((int64_t)dims->page_capacity * cfg->num_kv_heads + a.min_quota - 1) / a.min_quota;
     cudaLaunchConfig_t lc = {};
@@ -768,9 +926,7 @@ extern "C" int64_t cpa_decode_q8_workspace_bytes(const cpa_config* cfg) {
     const cpa_table_dims one{1, 0, 1, 1, 0};
     const int rc = q8_check(cfg, &one);
     if (rc != CPA_OK) return rc;
-    // two partial slots per CTA of the wave
-    const int64_t slots = 2 * kCtasPerSm * (cfg->num_sms ? cfg->num_sms : kSmsByDefault);
-    return slots * (cfg->num_q_heads / cfg->num_kv_heads) * (cfg->head_dim + 4) * 4;
+    return (int64_t)partial_slots(cfg) * (cfg->num_q_heads / cfg->num_kv_heads) * (cfg->head_dim + 4) * 4;
 }
 
 extern "C" int cpa_decode_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const void* q,
