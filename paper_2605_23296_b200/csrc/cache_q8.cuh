@@ -75,6 +75,26 @@ inline int q8_check(const cpa_config* c, const cpa_table_dims* d) {
     return CPA_OK;
 }
 
+// A programmatic launch: the grid may be made ready while the stream's earlier work ends; the kernel waits for that
+// work (griddepcontrol.wait) before it reads anything.
+template <class... P, class... A>
+int q8_launch(void (*kernel)(P...), int grid, int threads, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)grid);
+    lc.blockDim = dim3((unsigned)threads);
+    lc.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    if (cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CPA_ECUDA;
+    }
+    return CPA_OK;
+}
+
 // ---------------------------------------------------------------- number format
 // Scale of a page whose largest finite magnitude has the fp32 bits `amax`: 448 = 1.75 * 2^8, so the exponent is that of
 // amax less 8, and one more when amax's significand is above 1.75.

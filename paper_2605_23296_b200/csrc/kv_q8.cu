@@ -3,9 +3,10 @@
 // Append: per page, kv head and K or V, s = 2^e with amax(page) <= 448 s, code = e4m3(x / s); a page that holds tokens
 // already keeps its scale or, when the new rows need a larger one, has its codes re-rounded (code * s_old / s_new).
 // Read: bf16(code * s).  Both move 3 bytes per element (bf16 and code) and compute little, so HBM bounds them.  The
-// unit of work is a touched (page, kv head): one warp takes its K and V, because a scale needs the page's whole amax
-// before the first code can be written; with the rows in registers everything is read once.  Consecutive warps take the
-// heads of one page, so that a token's row is read whole.
+// unit of work is a touched (page, kv head) of K or of V: one warp takes all of it, because a scale needs the page's whole
+// amax before the first code can be written; with the rows in registers everything is read once.  (K and V in one warp
+// needs twice the registers and was slower.)  Consecutive warps take the heads of one page, so that a token's row is
+// read whole.
 //
 // Units of work without a host that knows the lengths: block b is given the unit numbers from base_b = cu[b] / 16 + 2 b
 // on.  n new tokens behind c cached ones touch at most n / 16 + 2 pages and base grows by at least that much, so the
@@ -28,19 +29,22 @@ struct page_unit {
 // cu == nullptr: one row per block
 __device__ __forceinline__ int cu_at(const int32_t* cu, int b) { return cu ? __ldg(cu + b) : b; }
 
+// By a whole warp: 32 candidates are looked at per load.
 __device__ __forceinline__ page_unit find_unit(int u, const q8_tables& t, const int32_t* __restrict__ cu,
-                                               const int32_t* __restrict__ first, int B, int rows) {
-    int lo = 0, hi = B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (cu_at(cu, mid) / kPage + 2 * mid <= u) lo = mid; else hi = mid - 1;
+                                               const int32_t* __restrict__ first, int B, int rows, int lane) {
+    int lo = 0, size = B;
+    while (size > 1) {
+        const int step = (size + 31) / 32, i = lane * step, b = lo + i;
+        const uint32_t below = __ballot_sync(0xffffffffu, i < size && cu_at(cu, b) / kPage + 2 * b <= u);
+        const int skip = max(__popc(below) - 1, 0) * step;
+        lo += skip;
+        size = min(step, size - skip);
     }
     page_unit r{-1, 0, 0, 0, 0};
-    const int c0 = cu_at(cu, lo), c1 = cu_at(cu, lo + 1), n = c1 - c0;
-    const int at = first ? __ldg(first + lo) : 0;
-    const int j = u - (c0 / kPage + 2 * lo);
-    if (n <= 0 || at < 0 || c0 < 0 || c1 > rows || j < 0) return r;
+    const int c0 = cu_at(cu, lo), c1 = cu_at(cu, lo + 1), at = first ? __ldg(first + lo) : 0;
     const int ip = __ldg(t.page_indptr + lo), np = __ldg(t.page_indptr + lo + 1) - ip;
+    const int n = c1 - c0, j = u - (c0 / kPage + 2 * lo);
+    if (n <= 0 || at < 0 || c0 < 0 || c1 > rows || j < 0) return r;
     if ((int64_t)at + n > (int64_t)np * kPage) return r;            // does not fit: the whole block is left out
     const int pg = at / kPage + j;
     if (pg * kPage >= at + n) return r;
@@ -65,8 +69,10 @@ kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* _
                     const int32_t* __restrict__ cu, const int32_t* __restrict__ lens, int32_t* __restrict__ lens_out,
                     uint8_t* __restrict__ pool, float* __restrict__ scales, int B, int rows, int Hkv, int64_t n_items) {
     constexpr int PIECES = D / 8;                 // 16-byte pieces of a bf16 row
-    constexpr int N = kPage * PIECES / 32;        // pieces per lane of a (page, head)
+    constexpr int N = kPage * PIECES / 32;        // pieces per lane of a page's K or V
     const int lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
     const int64_t tid = (int64_t)blockIdx.x * (kWarps * 32) + threadIdx.x, n_threads = (int64_t)gridDim.x * (kWarps * 32);
     for (int64_t b = tid; b < B; b += n_threads) {
         const int st = range_status((int)b, t, cu, lens, rows);
@@ -74,52 +80,57 @@ kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* _
         if (lens_out) lens_out[b] = (lens ? lens[b] : 0) + (st ? 0 : cu_at(cu, (int)b + 1) - cu_at(cu, (int)b));
     }
     for (int64_t item = tid >> 5; item < n_items; item += n_threads >> 5) {
-        const int g = (int)(item % Hkv);
-        const page_unit u = find_unit((int)(item / Hkv), t, cu, lens, B, rows);
+        const int kind = (int)(item & 1), g = (int)((item >> 1) % Hkv);
+        const page_unit u = find_unit((int)((item >> 1) / Hkv), t, cu, lens, B, rows, lane);
         if (u.block < 0) continue;
-        uint4 x[2][N];
+        const uint4* from = (kind ? v_new : k_new) + ((int64_t)u.row * Hkv + g) * PIECES;
+        uint4 x[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int slot = (lane + 32 * i) / PIECES, piece = lane % PIECES;
-            const int64_t src = ((int64_t)(u.row + slot - u.p0) * Hkv + g) * PIECES + piece;
-            const bool mine = slot >= u.p0 && slot < u.p1;
-            x[0][i] = mine ? __ldcs(k_new + src) : make_uint4(0, 0, 0, 0);
-            x[1][i] = mine ? __ldcs(v_new + src) : make_uint4(0, 0, 0, 0);
+            x[i] = slot >= u.p0 && slot < u.p1 ? __ldcs(from + (int64_t)(slot - u.p0) * Hkv * PIECES + piece) : make_uint4(0, 0, 0, 0);
         }
-        uint8_t* chunk = pool + ((int64_t)u.page * Hkv + g) * (2 * kPage * D);
-        float* sc = scales + ((int64_t)u.page * Hkv + g) * 2;
+        const int64_t cell = (int64_t)u.page * Hkv + g;
+        float* sc = scales + cell * 2 + kind;
+        uint8_t* to = pool + cell * (2 * kPage * D) + kind * (kPage * D);
+        const float old = u.p0 > 0 ? *sc : 0.f;   // the page holds tokens already
+        // largest magnitude, as bf16 bits of two halves; infinities and NaN, which do not count, are sorted out only
+        // where the page has any
+        uint32_t two = 0;
 #pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-            uint32_t amax = 0;
+        for (int i = 0; i < N; ++i)
+            two = __vmaxu2(__vmaxu2(two, __vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu)),
+                           __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu));
+        uint32_t amax = __reduce_max_sync(0xffffffffu, max(two & 0xFFFFu, two >> 16)) << 16;
+        if (amax >= 0x7F800000u) {
+            amax = 0;
 #pragma unroll
-            for (int i = 0; i < N; ++i) amax = max(amax, q8_amax8(x[kind][i]));
+            for (int i = 0; i < N; ++i) amax = max(amax, q8_amax8(x[i]));
             amax = __reduce_max_sync(0xffffffffu, amax);
-            float s = q8_scale(amax);
-            uint8_t* to = chunk + kind * (kPage * D);
-            if (u.p0 > 0) {                       // the page holds tokens already
-                const float old = sc[kind];
-                if (s > old) {
-                    const float f = old * q8_inverse(s);
-                    for (int i = lane; i < u.p0 * (D / 4); i += 32) {
-                        uint32_t* c = reinterpret_cast<uint32_t*>(to) + i;
-                        *c = q8_rescale4(*c, f);
-                    }
-                } else {
-                    s = old;
-                }
-            }
-            // (a scale that another writer of the pool has left need not be a power of two)
-            const bool pow2 = (__float_as_uint(s) & 0x807FFFFFu) == 0 && s <= 0x1p120f;
-            const float inv = pow2 ? q8_inverse(s) : 1.f / s;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int slot = (lane + 32 * i) / PIECES, piece = lane % PIECES;
-                if (slot >= u.p0 && slot < u.p1)
-                    *reinterpret_cast<uint2*>(to + slot * D + piece * 8) = q8_codes8(x[kind][i], inv);
-            }
-            __syncwarp();                         // every lane has read the old scale
-            if (lane == 0) sc[kind] = s;
         }
+        float s = q8_scale(amax);
+        if (u.p0 > 0) {
+            if (s > old) {
+                const float f = old * q8_inverse(s);
+                for (int i = lane; i < u.p0 * (D / 4); i += 32) {
+                    uint32_t* c = reinterpret_cast<uint32_t*>(to) + i;
+                    *c = q8_rescale4(*c, f);
+                }
+            } else {
+                s = old;
+            }
+        }
+        // (a scale that another writer of the pool has left need not be a power of two)
+        const bool pow2 = (__float_as_uint(s) & 0x807FFFFFu) == 0 && s <= 0x1p120f;
+        const float inv = pow2 ? q8_inverse(s) : 1.f / s;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int slot = (lane + 32 * i) / PIECES, piece = lane % PIECES;
+            if (slot >= u.p0 && slot < u.p1)
+                *reinterpret_cast<uint2*>(to + slot * D + piece * 8) = q8_codes8(x[i], inv);
+        }
+        __syncwarp();                             // every lane has read the old scale
+        if (lane == 0) *sc = s;
     }
 }
 
@@ -129,51 +140,48 @@ kv_read_q8_kernel(q8_tables t, const int32_t* __restrict__ cu, const int32_t* __
                   const uint8_t* __restrict__ pool, const float* __restrict__ scales, uint4* __restrict__ k_out,
                   uint4* __restrict__ v_out, int B, int rows, int Hkv, int64_t n_items) {
     constexpr int PIECES = D / 16;                // 16-byte pieces of a row of codes
-    constexpr int N = kPage * PIECES / 32;        // pieces per lane of a (page, head)
+    constexpr int N = kPage * PIECES / 32;        // pieces per lane of a page's K or V
     const int lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
     const int64_t tid = (int64_t)blockIdx.x * (kWarps * 32) + threadIdx.x, n_threads = (int64_t)gridDim.x * (kWarps * 32);
     for (int64_t b = tid; b < B; b += n_threads) {
         const int st = range_status((int)b, t, cu, first, rows);
         if (st) atomicCAS(t.header, 0, st);
     }
     for (int64_t item = tid >> 5; item < n_items; item += n_threads >> 5) {
-        const int g = (int)(item % Hkv);
-        const page_unit u = find_unit((int)(item / Hkv), t, cu, first, B, rows);
+        const int kind = (int)(item & 1), g = (int)((item >> 1) % Hkv);
+        const page_unit u = find_unit((int)((item >> 1) / Hkv), t, cu, first, B, rows, lane);
         if (u.block < 0) continue;
-        const uint4* chunk = reinterpret_cast<const uint4*>(pool + ((int64_t)u.page * Hkv + g) * (2 * kPage * D));
-        const float2 sc = *reinterpret_cast<const float2*>(scales + ((int64_t)u.page * Hkv + g) * 2);
-        uint4 x[2][N];
+        const int64_t cell = (int64_t)u.page * Hkv + g;
+        const uint4* chunk = reinterpret_cast<const uint4*>(pool + cell * (2 * kPage * D) + kind * (kPage * D));
+        const float s = __ldg(scales + cell * 2 + kind);
+        uint4 x[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = lane + 32 * i, slot = at / PIECES;
-            const bool mine = slot >= u.p0 && slot < u.p1;
-            x[0][i] = mine ? __ldcs(chunk + at) : make_uint4(0, 0, 0, 0);
-            x[1][i] = mine ? __ldcs(chunk + kPage * PIECES + at) : make_uint4(0, 0, 0, 0);
+            x[i] = slot >= u.p0 && slot < u.p1 ? __ldcs(chunk + at) : make_uint4(0, 0, 0, 0);
         }
+        uint4* out = (kind ? v_out : k_out) + ((int64_t)u.row * Hkv + g) * (2 * PIECES);
+        auto two = [&](uint32_t codes) {
+            const float2 f = e4m3x2_to_f32((uint16_t)codes);
+            const __nv_bfloat162 r = __floats2bfloat162_rn(mul_keep(f.x, s), mul_keep(f.y, s));
+            return *reinterpret_cast<const uint32_t*>(&r);
+        };
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int slot = (lane + 32 * i) / PIECES, piece = lane % PIECES;
             if (slot < u.p0 || slot >= u.p1) continue;
-            const int64_t dst = (((int64_t)(u.row + slot - u.p0) * Hkv + g) * PIECES + piece) * 2;
-#pragma unroll
-            for (int kind = 0; kind < 2; ++kind) {
-                const float s = kind ? sc.y : sc.x;
-                auto two = [&](uint32_t codes) {
-                    const float2 f = e4m3x2_to_f32((uint16_t)codes);
-                    const __nv_bfloat162 r = __floats2bfloat162_rn(mul_keep(f.x, s), mul_keep(f.y, s));
-                    return *reinterpret_cast<const uint32_t*>(&r);
-                };
-                const uint4 c = x[kind][i];
-                uint4* out = (kind ? v_out : k_out) + dst;
-                __stcs(out, make_uint4(two(c.x), two(c.x >> 16), two(c.y), two(c.y >> 16)));
-                __stcs(out + 1, make_uint4(two(c.z), two(c.z >> 16), two(c.w), two(c.w >> 16)));
-            }
+            uint4* dst = out + (int64_t)(slot - u.p0) * Hkv * (2 * PIECES) + 2 * piece;
+            const uint4 c = x[i];
+            __stcs(dst, make_uint4(two(c.x), two(c.x >> 16), two(c.y), two(c.y >> 16)));
+            __stcs(dst + 1, make_uint4(two(c.z), two(c.z >> 16), two(c.w), two(c.w >> 16)));
         }
     }
 }
 
-// (page, head) items of `rows` rows over B blocks, idle unit numbers included, and the launch's CTAs
-int64_t page_items(int64_t rows, int B, int Hkv) { return (rows / kPage + 2 * (int64_t)B) * Hkv; }
+// (page, head, K or V) items of `rows` rows over B blocks, idle unit numbers included, and the launch's CTAs
+int64_t page_items(int64_t rows, int B, int Hkv) { return (rows / kPage + 2 * (int64_t)B) * Hkv * 2; }
 int page_grid(int64_t items) { return (int)std::min<int64_t>((items + kWarps - 1) / kWarps, 1 << 20); }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -193,10 +201,8 @@ extern "C" int cpa_kv_append_q8(const cpa_config* cfg, const cpa_table_dims* dim
     const int B = dims->num_blocks, Hkv = cfg->num_kv_heads;
     const int64_t items = page_items(num_rows, B, Hkv);
     auto kernel = cfg->head_dim == 128 ? kv_append_q8_kernel<128> : kv_append_q8_kernel<64>;
-    kernel<<<page_grid(items), kWarps * 32, 0, (cudaStream_t)stream>>>(
-        t, (const uint4*)k_new, (const uint4*)v_new, d_cu_new, d_lens, d_lens_out, (uint8_t*)kv_pool, kv_scales, B,
-        num_rows, Hkv, items);
-    return cudaGetLastError() == cudaSuccess ? CPA_OK : CPA_ECUDA;
+    return q8_launch(kernel, page_grid(items), kWarps * 32, (cudaStream_t)stream, t, (const uint4*)k_new,
+                     (const uint4*)v_new, d_cu_new, d_lens, d_lens_out, (uint8_t*)kv_pool, kv_scales, B, num_rows, Hkv, items);
 }
 
 extern "C" int cpa_kv_read_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const int32_t* d_first,
@@ -212,7 +218,6 @@ extern "C" int cpa_kv_read_q8(const cpa_config* cfg, const cpa_table_dims* dims,
     const int B = dims->num_blocks, Hkv = cfg->num_kv_heads;
     const int64_t items = page_items(num_rows, B, Hkv);
     auto kernel = cfg->head_dim == 128 ? kv_read_q8_kernel<128> : kv_read_q8_kernel<64>;
-    kernel<<<page_grid(items), kWarps * 32, 0, (cudaStream_t)stream>>>(
-        t, d_cu, d_first, (const uint8_t*)kv_pool, kv_scales, (uint4*)k_out, (uint4*)v_out, B, num_rows, Hkv, items);
-    return cudaGetLastError() == cudaSuccess ? CPA_OK : CPA_ECUDA;
+    return q8_launch(kernel, page_grid(items), kWarps * 32, (cudaStream_t)stream, t, d_cu, d_first,
+                     (const uint8_t*)kv_pool, kv_scales, (uint4*)k_out, (uint4*)v_out, B, num_rows, Hkv, items);
 }

@@ -15,10 +15,10 @@
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kPerThread = 4;                     // blocks of a chunk per thread
+constexpr int kThreads = 256;
+constexpr int kPerThread = 8;                     // blocks of a chunk per thread
 constexpr int kChunk = kThreads * kPerThread;
-constexpr int kTile = 4096;                       // tokens (or pages) per tile of the fills
+constexpr int kTile = kThreads * 4;               // tokens per tile of the fill, four to a thread
 
 struct pair64 { int64_t tokens, pages; };
 
@@ -44,14 +44,26 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
     __shared__ pair64 sm_warp[kThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
-    // totals, in 64 bits; a negative length or too many pages or tokens leaves empty tables and a status
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    // Totals, in 64 bits; a negative length or too many pages or tokens leaves empty tables and a status.  The lengths
+    // of the first chunk stay in registers.
+    int L[kPerThread];
     pair64 sum{0, 0};
     bool bad = false;
-    for (int b = tid; b < B; b += kThreads) {
-        const int64_t L = lens[b];
-        bad |= L < 0;
-        sum.tokens += L;
-        sum.pages += (L + T + kPage - 1) / kPage;
+    auto load = [&](int at) {
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+            const int b = at + tid * kPerThread + i;
+            L[i] = b < B ? lens[b] : -1;
+            bad |= b < B && L[i] < 0;
+        }
+    };
+    auto pages_of = [&](int len) { return len < 0 ? 0 : (int)(((int64_t)len + T + kPage - 1) / kPage); };
+    for (int at = (B - 1) / kChunk * kChunk; at >= 0; at -= kChunk) {
+        load(at);
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) { sum.tokens += max(L[i], 0); sum.pages += pages_of(L[i]); }
     }
     bad = __syncthreads_or((int)bad);
     const pair64 total = cta_sum(sum, sm_warp);
@@ -81,15 +93,14 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
     pair64 run{0, 0};
     for (int at = 0; at < B; at += kChunk) {
         // exclusive scan of this chunk's lengths and pages on top of `run`
+        if (at > 0) load(at);
         int tok[kPerThread], pg[kPerThread], mine_t = 0, mine_p = 0;
-        const int b0 = at + tid * kPerThread;
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
-            const int L = b0 + i < B ? lens[b0 + i] : 0;
             tok[i] = mine_t;
             pg[i] = mine_p;
-            mine_t += L;
-            mine_p += b0 + i < B ? (int)(((int64_t)L + T + kPage - 1) / kPage) : 0;
+            mine_t += max(L[i], 0);
+            mine_p += pages_of(L[i]);
         }
         int inc_t = mine_t, inc_p = mine_p;
 #pragma unroll
@@ -126,10 +137,11 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
         __syncthreads();
         if (t.slot_mapping == nullptr) continue;
         // slots of the chunk's tokens, in tiles that go round the CTAs
-        for (int tile = t0 / kTile; (int64_t)tile * kTile < t1; ++tile) {
-            if (tile % (int)gridDim.x != (int)blockIdx.x) continue;
-            for (int j = tid * 4; j < kTile; j += kThreads * 4) {
-                const int64_t g = (int64_t)tile * kTile + j;      // four tokens, 16-byte aligned in the map
+        const int grid = (int)gridDim.x, me = (int)blockIdx.x, from = t0 / kTile;
+        for (int64_t tile = me + (from > me ? (from - me + grid - 1) / grid * grid : 0); tile * kTile < t1; tile += grid) {
+            {
+                const int j = tid * 4;
+                const int64_t g = tile * kTile + j;      // four tokens, 16-byte aligned in the map
                 const int first = (int)max((int64_t)t0, g), last = (int)min((int64_t)t1, g + 4);
                 if (first >= last) continue;
                 int lo = 0, hi = n - 1;                            // last block of the chunk that starts at or before it
@@ -196,11 +208,9 @@ extern "C" int cpa_tables_build(const cpa_config* cfg, const cpa_table_dims* dim
     const int page_limit = std::min(num_free, dims->page_capacity);
     const int token_limit = dims->token_capacity == 0 ? INT32_MAX : dims->token_capacity;
     cudaStream_t st = (cudaStream_t)stream;
-    const int grid = std::max(1, std::min(kBuildCtas, std::max(dims->token_capacity, 4 * page_limit) / kTile + 1));
-    tables_build_kernel<<<grid, kThreads, 0, st>>>(t, d_block_lens, d_free_pages, dims->num_blocks, dims->max_new_tokens,
-                                                   dims->num_pages, page_limit, token_limit,
-                                                   dims->num_blocks * cfg->num_kv_heads);
-    return cudaGetLastError() == cudaSuccess ? CPA_OK : CPA_ECUDA;
+    const int grid = std::max(1, std::min(kBuildCtas, (int)(std::max<int64_t>(dims->token_capacity, (int64_t)page_limit) / kTile) + 1));
+    return q8_launch(tables_build_kernel, grid, kThreads, st, t, d_block_lens, d_free_pages, dims->num_blocks,
+                     dims->max_new_tokens, dims->num_pages, page_limit, token_limit, dims->num_blocks * cfg->num_kv_heads);
 }
 
 extern "C" int cpa_tables_status(const void* d_tables, void* stream) {
