@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kWarps * 32)
 kv_read_q8_kernel(q8_tables t, const int32_t* __restrict__ cu, const int32_t* __restrict__ first,
                   const uint8_t* __restrict__ pool, const float* __restrict__ scales, uint4* __restrict__ k_out,
                   uint4* __restrict__ v_out, int B, int rows, int Hkv, int64_t n_items) {
-    constexpr int PIECES = D / 16;                // 16-byte pieces of a row of codes
+    constexpr int PIECES = D / 8;                 // pieces of 8 codes of a row: a warp's stores are whole lines
     constexpr int N = kPage * PIECES / 32;        // pieces per lane of a page's K or V
     const int lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
@@ -154,15 +154,15 @@ kv_read_q8_kernel(q8_tables t, const int32_t* __restrict__ cu, const int32_t* __
         const page_unit u = find_unit((int)((item >> 1) / Hkv), t, cu, first, B, rows, lane);
         if (u.block < 0) continue;
         const int64_t cell = (int64_t)u.page * Hkv + g;
-        const uint4* chunk = reinterpret_cast<const uint4*>(pool + cell * (2 * kPage * D) + kind * (kPage * D));
+        const uint2* chunk = reinterpret_cast<const uint2*>(pool + cell * (2 * kPage * D) + kind * (kPage * D));
         const float s = __ldg(scales + cell * 2 + kind);
-        uint4 x[N];
+        uint2 x[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int at = lane + 32 * i, slot = at / PIECES;
-            x[i] = slot >= u.p0 && slot < u.p1 ? __ldcs(chunk + at) : make_uint4(0, 0, 0, 0);
+            x[i] = slot >= u.p0 && slot < u.p1 ? __ldcs(chunk + at) : make_uint2(0, 0);
         }
-        uint4* out = (kind ? v_out : k_out) + ((int64_t)u.row * Hkv + g) * (2 * PIECES);
+        uint4* out = (kind ? v_out : k_out) + ((int64_t)u.row * Hkv + g) * PIECES;
         auto two = [&](uint32_t codes) {
             const float2 f = e4m3x2_to_f32((uint16_t)codes);
             const __nv_bfloat162 r = __floats2bfloat162_rn(mul_keep(f.x, s), mul_keep(f.y, s));
@@ -171,11 +171,9 @@ kv_read_q8_kernel(q8_tables t, const int32_t* __restrict__ cu, const int32_t* __
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int slot = (lane + 32 * i) / PIECES, piece = lane % PIECES;
-            if (slot < u.p0 || slot >= u.p1) continue;
-            uint4* dst = out + (int64_t)(slot - u.p0) * Hkv * (2 * PIECES) + 2 * piece;
-            const uint4 c = x[i];
-            __stcs(dst, make_uint4(two(c.x), two(c.x >> 16), two(c.y), two(c.y >> 16)));
-            __stcs(dst + 1, make_uint4(two(c.z), two(c.z >> 16), two(c.w), two(c.w >> 16)));
+            if (slot >= u.p0 && slot < u.p1)
+                __stcs(out + (int64_t)(slot - u.p0) * Hkv * PIECES + piece,
+                       make_uint4(two(x[i].x), two(x[i].x >> 16), two(x[i].y), two(x[i].y >> 16)));
         }
     }
 }

@@ -19,6 +19,7 @@ constexpr int kThreads = 256;
 constexpr int kPerThread = 8;                     // blocks of a chunk per thread
 constexpr int kChunk = kThreads * kPerThread;
 constexpr int kTile = kThreads * 4;               // tokens per tile of the fill, four to a thread
+constexpr int kGroups = 2;
 
 struct pair64 { int64_t tokens, pages; };
 
@@ -48,6 +49,9 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     // Totals, in 64 bits; a negative length or too many pages or tokens leaves empty tables and a status.  The lengths
     // of the first chunk stay in registers.
+    // (this thread's first page id is fetched beside the first lengths, whether the blocks will take it or not)
+    const int list0 = blockIdx.x * kThreads + tid;
+    const int id0 = list0 < page_limit ? __ldg(free_pages + list0) : 0;
     int L[kPerThread];
     pair64 sum{0, 0};
     bool bad = false;
@@ -72,23 +76,13 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
     for (int i = blockIdx.x * kThreads + tid; i < n_tickets; i += gridDim.x * kThreads) t.tickets[i] = 0;
     if (status) {
         for (int b = blockIdx.x * kThreads + tid; b <= B; b += gridDim.x * kThreads) t.cu_seqlens[b] = t.page_indptr[b] = 0;
-        if (blockIdx.x == 0 && tid < kHeaderWords) t.header[tid] = tid == kBuildWords ? status : 0;
+        for (int i = tid; blockIdx.x == 0 && i < kHeaderWords; i += kThreads) t.header[i] = i == kBuildWords ? status : 0;
         return;
     }
     // every CTA writes its own word of the header, so nothing has to be cleared in front of the launch
-    if (blockIdx.x == 0 && tid < kHeaderWords && (tid < kBuildWords || tid >= kBuildWords + (int)gridDim.x))
-        t.header[tid] = tid == 1 ? (int)total.tokens : tid == 2 ? (int)total.pages : 0;
-
-    // the page list; an id outside the pool is replaced by page 0, so that no later call leaves the pool
-    bool bad_id = false;
-    for (int i = blockIdx.x * kThreads + tid; i < (int)total.pages; i += gridDim.x * kThreads) {
-        const int id = free_pages[i];
-        const bool out = (unsigned)id >= (unsigned)num_pages;
-        bad_id |= out;
-        t.page_indices[i] = out ? 0 : id;
-    }
-    bad_id = __syncthreads_or((int)bad_id);
-    if (tid == 0) t.header[kBuildWords + blockIdx.x] = bad_id ? kStatusInvalid : 0;
+    for (int i = tid; blockIdx.x == 0 && i < kHeaderWords; i += kThreads)
+        if (i < kBuildWords || i >= kBuildWords + (int)gridDim.x)
+            t.header[i] = i == 1 ? (int)total.tokens : i == 2 ? (int)total.pages : 0;
 
     pair64 run{0, 0};
     for (int at = 0; at < B; at += kChunk) {
@@ -136,44 +130,54 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
         if (blockIdx.x == 0 && tid == 0 && at + n == B) { t.cu_seqlens[B] = t1; t.page_indptr[B] = (int)run.pages; }
         __syncthreads();
         if (t.slot_mapping == nullptr) continue;
-        // slots of the chunk's tokens, in tiles that go round the CTAs
+        // slots of the chunk's tokens, in tiles that go round the CTAs; a thread takes groups of four tokens (16 bytes of
+        // the map) of kGroups tiles at once, to have their page ids in flight together
         const int grid = (int)gridDim.x, me = (int)blockIdx.x, from = t0 / kTile;
-        for (int64_t tile = me + (from > me ? (from - me + grid - 1) / grid * grid : 0); tile * kTile < t1; tile += grid) {
-            {
-                const int j = tid * 4;
-                const int64_t g = tile * kTile + j;      // four tokens, 16-byte aligned in the map
-                const int first = (int)max((int64_t)t0, g), last = (int)min((int64_t)t1, g + 4);
-                if (first >= last) continue;
+        for (int64_t tile = me + (from > me ? (from - me + grid - 1) / grid * grid : 0); tile * kTile < t1; tile += kGroups * grid) {
+            int out[kGroups][4];
+#pragma unroll
+            for (int q = 0; q < kGroups; ++q) {
+                const int64_t g = (tile + q * grid) * kTile + tid * 4;
+                const int first = (int)max((int64_t)t0, g);
                 int lo = 0, hi = n - 1;                            // last block of the chunk that starts at or before it
                 while (lo < hi) {
                     const int mid = (lo + hi + 1) >> 1;
                     if (sm_cu[mid] <= first) lo = mid; else hi = mid - 1;
                 }
-                int out[4], page_at = -1, page = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int64_t token = g + i;
-                    out[i] = 0;
-                    if (token < first || token >= last) continue;
+                    out[q][i] = 0;
+                    if (token < t0 || token >= t1) continue;
                     while (sm_cu[lo + 1] <= token) ++lo;           // blocks of length zero are stepped over
-                    const int pos = (int)token - sm_cu[lo], want = sm_ip[lo] + pos / kPage;
-                    if (want != page_at) {
-                        page_at = want;
-                        page = free_pages[want];
-                        if ((unsigned)page >= (unsigned)num_pages) page = 0;
-                    }
-                    out[i] = page * kPage + pos % kPage;
+                    const int pos = (int)token - sm_cu[lo];
+                    const int page = __ldg(free_pages + sm_ip[lo] + pos / kPage);
+                    out[q][i] = ((unsigned)page < (unsigned)num_pages ? page : 0) * kPage + pos % kPage;
                 }
-                if (last - first == 4) {
-                    *reinterpret_cast<int4*>(t.slot_mapping + g) = make_int4(out[0], out[1], out[2], out[3]);
+            }
+#pragma unroll
+            for (int q = 0; q < kGroups; ++q) {
+                const int64_t g = (tile + q * grid) * kTile + tid * 4;
+                if (g >= t0 && g + 4 <= t1) {
+                    *reinterpret_cast<int4*>(t.slot_mapping + g) = make_int4(out[q][0], out[q][1], out[q][2], out[q][3]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (g + i >= first && g + i < last) t.slot_mapping[g + i] = out[i];
+                        if (g + i >= t0 && g + i < t1) t.slot_mapping[g + i] = out[q][i];
                 }
             }
         }
     }
+    // the page list; an id outside the pool is replaced by page 0, so that no later call leaves the pool
+    bool bad_id = false;
+    for (int i = list0; i < (int)total.pages; i += gridDim.x * kThreads) {
+        const int id = i == list0 ? id0 : __ldg(free_pages + i);
+        const bool out = (unsigned)id >= (unsigned)num_pages;
+        bad_id |= out;
+        t.page_indices[i] = out ? 0 : id;
+    }
+    bad_id = __syncthreads_or((int)bad_id);
+    if (tid == 0) t.header[kBuildWords + blockIdx.x] = bad_id ? kStatusInvalid : 0;
 }
 
 }  // namespace
