@@ -145,11 +145,9 @@ _lib.cpa_strerror.restype = ctypes.c_char_p
 
 def _ptr(x) -> Optional[int]:
     """Device/host address of a tensor-like, or the integer itself."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
-    return int(x.data_ptr())
+    return x.data_ptr()
 
 
 def _i32(a) -> np.ndarray:
@@ -386,7 +384,7 @@ def cpa_tables_offset(cfg: cpa_config, dims: cpa_table_dims, which: int) -> int:
 
 def cpa_tables_build(cfg: cpa_config, dims: cpa_table_dims, d_block_lens, d_free_pages, num_free: int, d_tables,
                      stream: int = 0) -> int:
-    return _lib.cpa_tables_build(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_block_lens), _ptr(d_free_pages),
+    return _lib.cpa_tables_build(cfg, dims, _ptr(d_block_lens), _ptr(d_free_pages),
                                  int(num_free), _ptr(d_tables), stream or None)
 
 
@@ -396,7 +394,7 @@ def cpa_tables_status(d_tables, stream: int = 0) -> int:
 
 def cpa_kv_append_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, k_new, v_new, d_cu_new, num_rows: int, d_lens,
                      d_lens_out, kv_pool, kv_scales, stream: int = 0) -> int:
-    return _lib.cpa_kv_append_q8(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_tables), _ptr(k_new), _ptr(v_new),
+    return _lib.cpa_kv_append_q8(cfg, dims, _ptr(d_tables), _ptr(k_new), _ptr(v_new),
                                  _ptr(d_cu_new), int(num_rows), _ptr(d_lens), _ptr(d_lens_out), _ptr(kv_pool),
                                  _ptr(kv_scales), stream or None)
 
@@ -407,18 +405,18 @@ def cpa_decode_q8_workspace_bytes(cfg: cpa_config) -> int:
 
 def cpa_decode_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, q, d_lens, d_active, kv_pool, kv_scales, o, d_workspace,
                   stream: int = 0) -> int:
-    return _lib.cpa_decode_q8(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_tables), _ptr(q), _ptr(d_lens),
+    return _lib.cpa_decode_q8(cfg, dims, _ptr(d_tables), _ptr(q), _ptr(d_lens),
                               _ptr(d_active), _ptr(kv_pool), _ptr(kv_scales), _ptr(o), _ptr(d_workspace), stream or None)
 
 
 def cpa_decode_append_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, q, k_new, v_new, d_lens, d_lens_out, d_active,
                          kv_pool, kv_scales, o, d_workspace, stream: int = 0) -> int:
-    return _lib.cpa_decode_append_q8(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_tables), _ptr(q), _ptr(k_new),
+    return _lib.cpa_decode_append_q8(cfg, dims, _ptr(d_tables), _ptr(q), _ptr(k_new),
                                      _ptr(v_new), _ptr(d_lens), _ptr(d_lens_out), _ptr(d_active), _ptr(kv_pool),
                                      _ptr(kv_scales), _ptr(o), _ptr(d_workspace), stream or None)
 
 
 def cpa_kv_read_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, d_first, d_cu, num_rows: int, kv_pool, kv_scales,
                    k_out, v_out, stream: int = 0) -> int:
-    return _lib.cpa_kv_read_q8(ctypes.byref(cfg), ctypes.byref(dims), _ptr(d_tables), _ptr(d_first), _ptr(d_cu),
+    return _lib.cpa_kv_read_q8(cfg, dims, _ptr(d_tables), _ptr(d_first), _ptr(d_cu),
                                int(num_rows), _ptr(kv_pool), _ptr(kv_scales), _ptr(k_out), _ptr(v_out), stream or None)

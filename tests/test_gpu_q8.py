@@ -457,7 +457,8 @@ def test_a_run_captured_and_replayed(B):
         for i in range(2):                      # both steps of a replay take the same rows
             for blk in range(3):
                 c.want.append(blk, vals[1][1][blk:blk + 1], vals[2][1][blk:blk + 1])
-            c.check_rows(o[i], vals[0][1], what=f"replay {r}.{i}") if i == 1 else None
+            if i == 1:
+                c.check_rows(o[i], vals[0][1], what=f"replay {r}")
         c.lens = a
         c.check_pool(f"replay {r}")
     assert c.status() == B.CPA_OK
