@@ -26,7 +26,7 @@ constexpr int kPage = 16;                     // tokens per page
 // Device tables, int32 words: a header (word 0: what append and decode launches record, 1 tokens, 2 pages, from word
 // kBuildWords on what each CTA of the build has found), then cu_seqlens, page_indptr, the page list, the slot map and
 // the merge tickets of the decode (zero between launches), each 16-byte aligned.
-constexpr int kBuildWords = 4, kBuildCtas = 592, kHeaderWords = 596;   // 596: a multiple of 4
+constexpr int kBuildWords = 4, kBuildCtas = 296, kHeaderWords = 300;   // 300: a multiple of 4
 struct q8_tables {
     int32_t* header;
     int32_t* cu_seqlens;     // [B+1]

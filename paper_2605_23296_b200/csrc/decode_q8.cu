@@ -160,13 +160,11 @@ __device__ __forceinline__ int key_of_row(int i) {
 // A block's tokens as this launch sees them, or -1 when it sits out.
 __device__ __forceinline__ int block_len(int b, const q8_tables& t, const int32_t* __restrict__ lens,
                                          const int32_t* __restrict__ active, int append, int& ip, int& status) {
-    status = 0;
-    ip = __ldg(t.page_indptr + b);
-    if (active && active[b] == 0) return -1;
-    const int64_t room = (int64_t)(__ldg(t.page_indptr + b + 1) - ip) * kPage, len = lens[b];
-    if (len < 0) status = kStatusInvalid;
-    else if (len + append > room) status = kStatusNoSpace;
-    return status ? -1 : (int)len + append;
+    // (all loads first, so that those of several blocks can be in flight together)
+    const int len = lens[b], first = __ldg(t.page_indptr + b), end = __ldg(t.page_indptr + b + 1), on = active ? active[b] : 1;
+    ip = first;
+    status = on == 0 ? 0 : len < 0 ? kStatusInvalid : (int64_t)len + append > (int64_t)(end - first) * kPage ? kStatusNoSpace : 0;
+    return on == 0 || status ? -1 : len + append;
 }
 
 struct q8_args {
@@ -283,19 +281,21 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
     const int append = a.k_new != nullptr;
     const int run = (a.B + kQ8Threads - 1) / kQ8Threads, b_lo = min(a.B, tid * run), b_hi = min(a.B, b_lo + run);
     int mine = 0, my_len = -1, my_ip = 0;
+#pragma unroll 4
     for (int b = b_lo; b < b_hi; ++b) {
+        int status;
+        my_len = block_len(b, a.t, a.lens, a.active, append, my_ip, status);
+        if (my_len > 0) mine += (my_len + kPage - 1) / kPage + kUnitCost;
+    }
+    // this CTA keeps the books of every gridDim-th block: status, new length, and the zero row of an empty block
+    for (int64_t b = blockIdx.x + (int64_t)gridDim.x * tid; b < a.B; b += (int64_t)gridDim.x * kQ8Threads) {
         int ip, status;
-        const int len = block_len(b, a.t, a.lens, a.active, append, ip, status);
-        my_len = len;
-        my_ip = ip;
-        if (len > 0) mine += (len + kPage - 1) / kPage + kUnitCost;
-        if (b % (int)gridDim.x != (int)blockIdx.x) continue;
-        // this CTA keeps block b's books: status, new length, and the zero row of an empty block
+        const int len = block_len((int)b, a.t, a.lens, a.active, append, ip, status);
         if (status) atomicCAS(a.t.header, 0, status);
         if (a.lens_out) a.lens_out[b] = len < 0 ? a.lens[b] : len;
         if (len == 0)
             for (int i = 0; i < a.Hq * (D / 8); ++i)
-                reinterpret_cast<uint4*>(a.o + (int64_t)b * a.Hq * D)[i] = make_uint4(0, 0, 0, 0);
+                reinterpret_cast<uint4*>(a.o + b * a.Hq * D)[i] = make_uint4(0, 0, 0, 0);
     }
     int inc = mine;
 #pragma unroll
@@ -526,15 +526,16 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             __syncwarp();
             if (lane < kCons) mbar_arrive(empty0 + 8 * st);      // for the four consumers
             if (parts == 1) continue;
+            // One atomic publishes this partial (the lanes' stores come before it by the warp barrier) and, for the one who
+            // finds all others counted, makes theirs visible.  The counter is back at zero after the last.
             unsigned before_me = 0;
-            __threadfence();                                     // this lane's part of the partial, then the count
             __syncwarp();
             if (lane == 0)
-                before_me = atomicInc(reinterpret_cast<unsigned*>(a.t.tickets) + (int64_t)blk * a.Hkv + head,
-                                      (unsigned)parts - 1);      // back to zero with the last one
+                asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;\n" : "=r"(before_me)
+                             : "l"(a.t.tickets + (int64_t)blk * a.Hkv + head), "r"(parts - 1) : "memory");
             before_me = __shfl_sync(0xffffffffu, before_me, 0);
             if (before_me != (unsigned)parts - 1) continue;
-            __threadfence();
+            __syncwarp();
             // The last one in joins the partials: at the end of the CTA's work with all warps, else in the background.
             const int nk = k + 1;
             bool end = false;
@@ -885,7 +886,7 @@ int launch_q8(const cpa_config* cfg, const cpa_table_dims* dims, q8_args& a, cud
     if (fn(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, a.pool, size, stride, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return CPA_ECUDA;
-    a.min_quota = Sh::kRound;
+    a.min_quota = 8;
     a.slots = partial_slots(cfg);
     // one wave; no more CTAs than the table's pages could keep busy, or the blocks' books need
     const int64_t most = ((int64_t)dims->page_capacity * cfg->num_kv_heads + a.min_quota - 1) / a.min_quota;

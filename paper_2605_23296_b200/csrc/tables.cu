@@ -15,8 +15,8 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kPerThread = 8;                     // blocks of a chunk per thread
+constexpr int kThreads = 512;
+constexpr int kPerThread = 4;                     // blocks of a chunk per thread
 constexpr int kChunk = kThreads * kPerThread;
 constexpr int kTile = kThreads * 4;               // tokens per tile of the fill, four to a thread
 constexpr int kGroups = 2;
@@ -134,7 +134,7 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
         // the map) of kGroups tiles at once, to have their page ids in flight together
         const int grid = (int)gridDim.x, me = (int)blockIdx.x, from = t0 / kTile;
         for (int64_t tile = me + (from > me ? (from - me + grid - 1) / grid * grid : 0); tile * kTile < t1; tile += kGroups * grid) {
-            int out[kGroups][4];
+            int out[kGroups][4], page[kGroups][4];
 #pragma unroll
             for (int q = 0; q < kGroups; ++q) {
                 const int64_t g = (tile + q * grid) * kTile + tid * 4;
@@ -147,17 +147,19 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int64_t token = g + i;
-                    out[q][i] = 0;
+                    out[q][i] = page[q][i] = 0;
                     if (token < t0 || token >= t1) continue;
                     while (sm_cu[lo + 1] <= token) ++lo;           // blocks of length zero are stepped over
                     const int pos = (int)token - sm_cu[lo];
-                    const int page = __ldg(free_pages + sm_ip[lo] + pos / kPage);
-                    out[q][i] = ((unsigned)page < (unsigned)num_pages ? page : 0) * kPage + pos % kPage;
+                    out[q][i] = pos % kPage;
+                    page[q][i] = __ldg(free_pages + sm_ip[lo] + pos / kPage);
                 }
             }
 #pragma unroll
             for (int q = 0; q < kGroups; ++q) {
                 const int64_t g = (tile + q * grid) * kTile + tid * 4;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[q][i] += ((unsigned)page[q][i] < (unsigned)num_pages ? page[q][i] : 0) * kPage;
                 if (g >= t0 && g + 4 <= t1) {
                     *reinterpret_cast<int4*>(t.slot_mapping + g) = make_int4(out[q][0], out[q][1], out[q][2], out[q][3]);
                 } else {
