@@ -181,6 +181,7 @@ struct q8_args {
     float scale_log2;
     int min_quota;             // cells of a range at least
     int slots;                 // partial slots of the workspace
+    int list_len;              // entries of the page list, in use or not
 };
 
 // Stores a finished row pair: dims d, d + 1 of query head h.
@@ -259,6 +260,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
     __shared__ __align__(8) uint64_t sm_full[kStages], sm_empty[kStages], sm_dump[kStages], sm_end;
     __shared__ int sm_scan[kQ8Threads / 32], sm_strip[kQ8Threads], sm_len[kQ8Threads], sm_ip[kQ8Threads], sm_dump_stage[kStages];
     __shared__ int4 sm_final;                          // a merge that is left to all warps at the end
+    __shared__ int sm_down;
     __shared__ volatile int sm_dead;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t data0 = (smem_u32(raw) + 1023u) & ~1023u, meta0 = data0 + kStages * Sh::kData;
@@ -272,6 +274,16 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
         asm volatile("prefetch.tensormap [%0];\n" :: "l"(&tm) : "memory");
         sm_dead = 0;
     }
+    // What the start is going to wait for, towards L2 while the stream's earlier work ends (a line that is still to be
+    // written is updated there): lengths, page offsets and, each CTA its share, the page list.
+    {
+        const int64_t at = ((int64_t)blockIdx.x * kQ8Threads + tid) * 32;
+        if (at < a.list_len) asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.t.page_indices + at));
+        if (at < a.B) {
+            asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.lens + at));
+            asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.t.page_indptr + at));
+        }
+    }
     // the next launch of the stream may be made ready now (it waits as this one does)
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     // everything above touches nothing that an earlier launch writes; this one may have been started before that one ended
@@ -280,11 +292,12 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
     // ---- the cut: every thread takes a strip of blocks, and the strips' page counts are scanned
     const int append = a.k_new != nullptr;
     const int run = (a.B + kQ8Threads - 1) / kQ8Threads, b_lo = min(a.B, tid * run), b_hi = min(a.B, b_lo + run);
-    int mine = 0, my_len = -1, my_ip = 0;
+    int mine = 0, my_len = -1, my_ip = 0, first_len = 0;
 #pragma unroll 4
     for (int b = b_lo; b < b_hi; ++b) {
         int status;
         my_len = block_len(b, a.t, a.lens, a.active, append, my_ip, status);
+        if (my_len > 0 && mine == 0) first_len = my_len;
         if (my_len > 0) mine += (my_len + kPage - 1) / kPage + kUnitCost;
     }
     // this CTA keeps the books of every gridDim-th block: status, new length, and the zero row of an empty block
@@ -312,6 +325,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
         total += sm_scan[w];
     }
     sm_strip[tid] = before + inc - mine;               // pages of the blocks in front of the strip
+    if (mine > 0 && before + inc == mine) sm_down = first_len & 1;   // (one thread: the first strip that holds any)
     if (tid < a.B && run == 1) { sm_len[tid] = my_len; sm_ip[tid] = my_ip; }
     const int64_t all = (int64_t)total * a.Hkv;
     const int64_t quota = max((all + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)a.min_quota);
@@ -347,12 +361,22 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             if (run == 1) { w_len = sm_len[win + lane]; w_ip = sm_ip[win + lane]; }
             else w_len = block_len(win + lane, a.t, a.lens, a.active, append, w_ip, status);
         };
-        int b = 0, g = 0, p = 0, len = 0, ip = 0, pages = 0;
-        const int64_t x = x0;
-        int64_t left = min(quota, all - x0), unit0 = 0;  // cells of the range still to hand out; where this unit starts
+        int b = 0, g = 0, len = 0, ip = 0, pages = 0;
+        // Consecutive steps walk the pages in opposite directions (the first block's length says which), so that what a
+        // step has read last, and L2 still holds, is what the next one reads first.
+        const bool down = sm_down != 0;
+        const int64_t x1 = min(x0 + quota, all), x = down ? x1 - 1 : x0;
+        int64_t unit0 = 0;                              // where the unit starts
+        int pb = 0, pe = 0;                             // its pages inside the range that are still to hand out
         bool opened = false;                            // a round of this unit has been handed out
         int parts = 0, first = 0;
-        // to the start of the range: the strip that holds it, the block in the strip, head and page in the block
+        auto clip = [&]() {
+            pages = (len + kPage - 1) / kPage;
+            pb = (int)max((int64_t)0, x0 - unit0);
+            pe = (int)min((int64_t)pages, x1 - unit0);
+            opened = false;
+        };
+        // to the cell that the walk starts at: the strip that holds it, the block in the strip, head and page in the block
         auto locate = [&]() {
             int lo = 0, hi = kQ8Threads - 1;
             while (lo < hi) {
@@ -375,42 +399,38 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                     b = win + l;
                     len = __shfl_sync(0xffffffffu, w_len, l);
                     ip = __shfl_sync(0xffffffffu, w_ip, l);
-                    pages = (len + kPage - 1) / kPage;
-                    const int cells = pages + kUnitCost;
+                    const int cells = (len + kPage - 1) / kPage + kUnitCost;
                     const int64_t in = x - at - (int64_t)(__shfl_sync(0xffffffffu, sum, l) - cells) * a.Hkv;
                     g = (int)(in / cells);
-                    p = (int)(in % cells);
-                    unit0 = x - p;
-                    if (p > pages) { left += p - pages; p = pages; }   // (the cells behind the pages stand for the unit's cost)
-                    opened = false;
+                    unit0 = x - in % cells;
+                    clip();
                     return;
                 }
                 at += (int64_t)__shfl_sync(0xffffffffu, sum, 31) * a.Hkv;
                 win += 32;
-                if (win >= a.B) { left = 0; return; }    // (cannot be reached: the range starts inside the blocks)
+                if (win >= a.B) return;                  // (cannot be reached: the walk starts inside the blocks)
             }
         };
         locate();
         // the next round into `r`, and each lane's page of it
         auto next = [&](round_desc& r, int& id) {
             r.n = 0;
-            if (left <= 0) return;
-            if (p == pages) {                           // on to the next kv head, or the next block that has pages
-                unit0 += pages + kUnitCost;
-                left -= kUnitCost;
-                if (left <= 0) return;
-                p = 0;
-                opened = false;
-                if (++g == a.Hkv) {
-                    g = 0;
+            while (pb >= pe) {                          // on to the next (block, kv head) that has pages in the range
+                if (down ? unit0 <= x0 : unit0 + pages + kUnitCost >= x1) return;
+                const int from = pages;
+                g += down ? -1 : 1;
+                if (g < 0 || g == a.Hkv) {
+                    g = down ? a.Hkv - 1 : 0;
                     do {
-                        if (++b >= win + 32) { win = b; window(); }
+                        b += down ? -1 : 1;
+                        if (b < 0 || b >= a.B) { pb = pe = 0; unit0 = down ? x0 : x1; return; }   // (cannot be reached)
+                        if (b < win || b >= win + 32) { win = down ? max(b - 31, 0) : b; window(); }
                         len = __shfl_sync(0xffffffffu, w_len, b - win);
-                    } while (len <= 0 && b < a.B);
-                    if (b >= a.B) { left = 0; return; }  // (cannot be reached: ranges end inside the blocks)
+                    } while (len <= 0);
                     ip = __shfl_sync(0xffffffffu, w_ip, b - win);
-                    pages = (len + kPage - 1) / kPage;
                 }
+                unit0 += down ? -((len + kPage - 1) / kPage + kUnitCost) : from + kUnitCost;
+                clip();
             }
             r.flags = 0;
             if (!opened) {
@@ -421,15 +441,14 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             }
             r.b = b;
             r.g = g;
-            r.page0 = p;
-            r.n = (int)min((int64_t)min(pages - p, Sh::kRound), left);
+            r.n = min(pe - pb, Sh::kRound);
+            r.page0 = down ? pe - r.n : pb;
             r.len = len;
             r.first = first;
             r.parts = parts;
-            id = lane < r.n ? __ldg(a.t.page_indices + ip + p + lane) : 0;
-            p += r.n;
-            left -= r.n;
-            r.flags |= (p == pages || left == 0 ? 2 : 0) | (append && p == pages ? 4 : 0);
+            id = lane < r.n ? __ldg(a.t.page_indices + ip + r.page0 + lane) : 0;
+            (down ? pe : pb) += down ? -r.n : r.n;
+            r.flags |= (pb >= pe ? 2 : 0) | (append && r.page0 + r.n == pages ? 4 : 0);
         };
         // Descriptors and page ids run kAhead rounds in front of the copies, so that no load is waited for.
         round_desc d[kAhead + 1];
@@ -492,6 +511,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             const uint4 e0 = lds16(meta + Sh::kDesc), e1 = lds16(meta + Sh::kDesc + 16);
             const int blk = (int)e0.x, head = (int)e0.y, first = (int)e1.z, parts = (int)e1.w;
             const int64_t row0 = (int64_t)slot_of((int)blockIdx.x, first) * a.G;
+#pragma unroll 2
             for (int h = 0; h < a.G; ++h) {
                 float Ml = -INFINITY, Mo = -INFINITY, L = 0.f, f[kCons];
                 float4 m[kCons];
@@ -888,6 +908,7 @@ int launch_q8(const cpa_config* cfg, const cpa_table_dims* dims, q8_args& a, cud
         return CPA_ECUDA;
     a.min_quota = 8;
     a.slots = partial_slots(cfg);
+    a.list_len = dims->page_capacity;
     // one wave; no more CTAs than the table's pages could keep busy, or the blocks' books need
     const int64_t most = ((int64_t)dims->page_capacity * cfg->num_kv_heads + a.min_quota - 1) / a.min_quota;
     cudaLaunchConfig_t lc = {};
