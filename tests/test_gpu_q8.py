@@ -22,7 +22,7 @@ def _i32(a):
 
 def _bf16(x):
     """float64 values rounded to bf16: the device tensor, and the same values in float64."""
-    t = torch.tensor(np.asarray(x), dtype=torch.float64).to(torch.bfloat16)
+    t = torch.tensor(np.ascontiguousarray(x), dtype=torch.float64).to(torch.bfloat16)
     return t.cuda(), t.double().numpy()
 
 
@@ -540,3 +540,62 @@ def test_a_long_history_in_one_block(B):
     shaken = (c.scale * qq.abs() @ kk.abs().transpose(1, 2)).amax(2).reshape(-1, 1)
     tol = oq.decode_tolerance(*(t.cpu().numpy() for t in (want, spread, shaken)), d)
     assert (np.abs(o[0].double().cpu().numpy() - want.cpu().numpy()) <= tol).all()
+
+
+@pytest.mark.parametrize("num_sms", [1, 3, 0, 300])
+@pytest.mark.parametrize("blocks,hi", [(500, 40), (193, 3), (385, 130)])
+def test_many_blocks(B, blocks, hi, num_sms):
+    # more blocks than threads, a third of them empty, some sitting out; both directions of the walk
+    rng = np.random.default_rng(blocks + num_sms)
+    lens = [int(n) if rng.random() < 0.67 else 0 for n in rng.integers(1, hi + 1, blocks)]
+    c = Cache(B, lens, 2, 2, 64, 3, num_sms=num_sms, seed=hi)
+    c.append(_values(rng, sum(lens), 2, 64), _values(rng, sum(lens), 2, 64), lens)
+    on = rng.random(blocks) < 0.8
+    on[0] = True
+    active = _i32(on)
+    for t in range(2):
+        o, qf = c.decode(rng.standard_normal((blocks, 6, 64)), active)
+        c.check_rows(o, qf, np.flatnonzero(on), f"decode {t}")
+        assert (o[~torch.from_numpy(on).cuda()] == 9).all()
+        o, qf = c.step(rng.standard_normal((blocks, 6, 64)), _values(rng, blocks, 2, 64), _values(rng, blocks, 2, 64), active)
+        c.check_rows(o, qf, np.flatnonzero(on), f"step {t}")
+    c.check_pool()
+    assert c.status() == B.CPA_OK
+
+
+def test_cuts_at_every_place(B):
+    # one to twelve SMs and blocks of one to eighty pages: range ends fall inside blocks, on their edges, and into the
+    # cells that stand for a block's own cost
+    rng = np.random.default_rng(21)
+    for num_sms in range(1, 13):
+        lens = [int(x) for x in rng.integers(1, 1280, rng.integers(1, 6))]
+        c = Cache(B, lens, 2, 1, 128, 2, num_sms=num_sms, seed=num_sms)
+        c.append(_values(rng, sum(lens), 1, 128), _values(rng, sum(lens), 1, 128), lens)
+        for t in range(2):
+            o, qf = c.step(rng.standard_normal((len(lens), 2, 128)), _values(rng, len(lens), 1, 128), _values(rng, len(lens), 1, 128))
+            c.check_rows(o, qf, what=f"{num_sms} SMs")
+        c.check_pool()
+
+
+def test_calls_of_all_kinds_back_to_back(B):
+    # every call starts while the one before it ends: append, read, decode and step of one cache without a wait between
+    lens = [200, 31, 64]
+    c = Cache(B, lens, 40, 2, 64)
+    rng = np.random.default_rng(22)
+    c.append(*(_values(rng, sum(lens), 2, 64) for _ in range(2)), lens)
+    outs = []
+    for t in range(6):
+        q, k, v = rng.standard_normal((3, 8, 64)), _values(rng, 3, 2, 64), _values(rng, 3, 2, 64)
+        c.append(k, v)
+        o, qf = c.decode(q)
+        outs.append((o, [c.want.decode(b, qf[b], c.scale) for b in range(3)]))
+        k2, v2 = torch.empty(3, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+        assert B.cpa_kv_read_q8(c.cfg, c.dims, c.tables, c.lens - 1, _i32([0, 1, 2, 3]), 3, c.pool, c.scales, k2, v2) == 0
+        rows = np.concatenate([c.want.rows(b, int(c.want.lens[b]) - 1, int(c.want.lens[b])) for b in range(3)], 2).transpose(0, 2, 1, 3)
+        o, qf = c.step(q[::-1], v, k)
+        outs.append((o, [c.want.decode(b, qf[b], c.scale) for b in range(3)]))
+        assert np.array_equal(k2.double().cpu().numpy(), rows[0]) and np.array_equal(v2.double().cpu().numpy(), rows[1])
+    c.check_pool()
+    for o, want in outs:
+        for b in range(3):
+            assert (np.abs(o[b].double().cpu().numpy() - want[b][0]) <= oq.decode_tolerance(*want[b], 64)).all()
