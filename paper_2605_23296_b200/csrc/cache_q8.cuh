@@ -143,6 +143,16 @@ __device__ __forceinline__ uint2 q8_codes8(uint4 v, float inv) {
     };
     return make_uint2(two(v.x) | (two(v.y) << 16), two(v.z) | (two(v.w) << 16));
 }
+// The same for a power of two: the product of a bf16 value with it is a bf16 value (where it is not, being subnormal, the
+// code is zero all the same), so two values take one product.
+__device__ __forceinline__ uint2 q8_codes8_pow2(uint4 v, uint32_t inv2) {
+    auto two = [&](uint32_t w) {
+        uint32_t p;
+        asm("mul.rn.bf16x2 %0, %1, %2;\n" : "=r"(p) : "r"(w), "r"(inv2));
+        return to_e4m3x2(__uint_as_float(p << 16), __uint_as_float(p & 0xFFFF0000u));
+    };
+    return make_uint2(two(v.x) | (two(v.y) << 16), two(v.z) | (two(v.w) << 16));
+}
 __device__ __forceinline__ uint32_t q8_amax8(uint4 v) {
     uint32_t m = 0;
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
