@@ -18,8 +18,8 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kPerThread = 4;                     // blocks of a chunk per thread
 constexpr int kChunk = kThreads * kPerThread;
-constexpr int kTile = kThreads * 4;               // tokens per tile of the fill, four to a thread
-constexpr int kGroups = 2;
+constexpr int kRun = 8;                           // tokens per thread and tile of the fill
+constexpr int kTile = kThreads * kRun;
 
 struct pair64 { int64_t tokens, pages; };
 
@@ -130,42 +130,36 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
         if (blockIdx.x == 0 && tid == 0 && at + n == B) { t.cu_seqlens[B] = t1; t.page_indptr[B] = (int)run.pages; }
         __syncthreads();
         if (t.slot_mapping == nullptr) continue;
-        // slots of the chunk's tokens, in tiles that go round the CTAs; a thread takes groups of four tokens (16 bytes of
-        // the map) of kGroups tiles at once, to have their page ids in flight together
+        // Slots of the chunk's tokens, in tiles that go round the CTAs; a thread takes eight tokens (two 16-byte words of
+        // the map), which mostly lie in one block and in one or two of its pages.
         const int grid = (int)gridDim.x, me = (int)blockIdx.x, from = t0 / kTile;
-        for (int64_t tile = me + (from > me ? (from - me + grid - 1) / grid * grid : 0); tile * kTile < t1; tile += kGroups * grid) {
-            int out[kGroups][4], page[kGroups][4];
-#pragma unroll
-            for (int q = 0; q < kGroups; ++q) {
-                const int64_t g = (tile + q * grid) * kTile + tid * 4;
-                const int first = (int)max((int64_t)t0, g);
-                int lo = 0, hi = n - 1;                            // last block of the chunk that starts at or before it
-                while (lo < hi) {
-                    const int mid = (lo + hi + 1) >> 1;
-                    if (sm_cu[mid] <= first) lo = mid; else hi = mid - 1;
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t token = g + i;
-                    out[q][i] = page[q][i] = 0;
-                    if (token < t0 || token >= t1) continue;
-                    while (sm_cu[lo + 1] <= token) ++lo;           // blocks of length zero are stepped over
-                    const int pos = (int)token - sm_cu[lo];
-                    out[q][i] = pos % kPage;
-                    page[q][i] = __ldg(free_pages + sm_ip[lo] + pos / kPage);
-                }
+        for (int64_t tile = me + (from > me ? (from - me + grid - 1) / grid * grid : 0); tile * kTile < t1; tile += grid) {
+            const int64_t g = tile * kTile + tid * kRun;
+            const int first = (int)max((int64_t)t0, g), last = (int)min((int64_t)t1, g + kRun);
+            if (first >= last) continue;
+            int lo = 0, hi = n - 1;                                // last block of the chunk that starts at or before it
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (sm_cu[mid] <= first) lo = mid; else hi = mid - 1;
             }
+            auto page_at = [&](int i) {
+                const int page = __ldg(free_pages + i);
+                return (unsigned)page < (unsigned)num_pages ? page : 0;
+            };
+            if (last - first == kRun && sm_cu[lo + 1] >= last) {
+                const int pos = first - sm_cu[lo], at = sm_ip[lo] + pos / kPage, off = pos % kPage;
+                const int a = page_at(at), b = off + kRun > kPage ? page_at(at + 1) : a;
+                int out[kRun];
 #pragma unroll
-            for (int q = 0; q < kGroups; ++q) {
-                const int64_t g = (tile + q * grid) * kTile + tid * 4;
+                for (int i = 0; i < kRun; ++i) out[i] = (off + i < kPage ? a : b) * kPage + (off + i) % kPage;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) out[q][i] += ((unsigned)page[q][i] < (unsigned)num_pages ? page[q][i] : 0) * kPage;
-                if (g >= t0 && g + 4 <= t1) {
-                    *reinterpret_cast<int4*>(t.slot_mapping + g) = make_int4(out[q][0], out[q][1], out[q][2], out[q][3]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (g + i >= t0 && g + i < t1) t.slot_mapping[g + i] = out[q][i];
+                for (int i = 0; i < kRun; i += 4)
+                    *reinterpret_cast<int4*>(t.slot_mapping + g + i) = make_int4(out[i], out[i + 1], out[i + 2], out[i + 3]);
+            } else {
+                for (int token = first; token < last; ++token) {
+                    while (sm_cu[lo + 1] <= token) ++lo;           // blocks of length zero are stepped over
+                    const int pos = token - sm_cu[lo];
+                    t.slot_mapping[token] = page_at(sm_ip[lo] + pos / kPage) * kPage + pos % kPage;
                 }
             }
         }
