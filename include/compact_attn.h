@@ -580,7 +580,7 @@ typedef struct cpa_table_dims {
     int32_t num_blocks;      /* B >= 1, at most 2^20 */
     int32_t max_new_tokens;  /* tokens to reserve pages for behind every block's length, >= 0 */
     int32_t num_pages;       /* pages of the pool: page ids lie in [0, num_pages); num_pages * 32 * num_kv_heads < 2^31 */
-    int32_t page_capacity;   /* entries of the page list, >= the pages that the blocks take */
+    int32_t page_capacity;   /* entries of the page list, >= the pages that the blocks take; at most 2^30 */
     int32_t token_capacity;  /* entries of the slot map, >= the blocks' tokens; 0 = no slot map is made */
 } cpa_table_dims;
 
@@ -650,7 +650,8 @@ CPA_API int cpa_decode_q8(const cpa_config* cfg, const cpa_table_dims* dims, voi
  * cpa_decode_q8 over the cache with that row in it (as it was stored), in one launch.
  *   k_new, v_new : device bf16 [B, num_kv_heads, head_dim]
  *   d_lens       : device int32 [B] tokens cached before the step;  d_lens_out: [B] after it, not d_lens itself; a
- *                  block that sits out keeps its length.  A caller keeps two arrays and swaps them from step to step.
+ *                  block that sits out keeps its length.  A caller keeps two arrays and swaps them from step to step (a
+ *                  captured graph that is replayed as a loop holds an even number of steps).
  * Everything else as for cpa_decode_q8.
  */
 CPA_API int cpa_decode_append_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const void* q,

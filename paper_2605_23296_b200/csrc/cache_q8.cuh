@@ -68,7 +68,7 @@ inline int q8_check(const cpa_config* c, const cpa_table_dims* d) {
     if (d->num_blocks < 1 || d->max_new_tokens < 0 || d->num_pages < 1 || d->page_capacity < 0 || d->token_capacity < 0)
         return CPA_EINVAL;
     // slots are int32, and the pool's rows of 128 bytes are addressed with 32-bit coordinates
-    if (d->num_blocks > kMaxTableBlocks || (int64_t)d->num_pages * kPage > INT32_MAX ||
+    if (d->num_blocks > kMaxTableBlocks || d->page_capacity > (1 << 30) || (int64_t)d->num_pages * kPage > INT32_MAX ||
         (int64_t)d->num_pages * c->num_kv_heads * 32 > INT32_MAX ||
         (int64_t)d->num_blocks * c->num_kv_heads > INT32_MAX)
         return CPA_EUNSUPPORTED;

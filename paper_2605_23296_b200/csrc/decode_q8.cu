@@ -22,14 +22,18 @@
 // whose scales lie far apart neither overflow nor vanish; the denominator keeps the plain maximum m_l.
 //
 // Work: the (block, kv head, page) triples of all blocks are laid end to end and cut into ranges from the lengths on the
-// device: one equal range per CTA of the one wave.  (Handing the last sixth out in small ranges as CTAs
-// finish was slower, 116 us for 63: a range costs its producer a search and its merger a join.)  A CTA is four consumer
-// warps, a producer and a merger around a ring of stages; a stage is a round of up to 4 * TP pages of one (block, kv head),
-// with their scales, and with the queries (first round) and the new rows (last page) that belong to it: the consumers
+// device: one equal range per CTA of the one wave.  (Handing the last sixth out in small ranges as CTAs finish was slower,
+// 116 us for 63: a range costs its producer a search and its merger a join.)  A CTA is four consumer warps, a producer and
+// a merger around a ring of stages; a stage is a round of up to 4 * TP pages of one (block, kv head), with their scales,
+// and with the queries (first round) and the new rows (last page) that belong to it: the consumers
 // load nothing from global memory.  Consumer w takes pages w, w + 4, ... of a round and keeps its own maxima, sums and
 // O; at the end of a (block, kv head) inside a range it leaves them in the stage that it has just consumed and goes on.
 // The merger joins the four from there.  A range boundary inside a (block, kv head) leaves partials in the workspace,
 // and the merger that arrives last (a counter in the tables) joins them in the order of the ranges.
+//
+// Measured (one wave of 2 x 148 CTAs): 32 blocks of 1024 .. 8192 tokens, 32 heads over 8 of 128, 337 MB: 60 us, of which
+// the stream 48 us (7.0 TB/s) and start and merge the rest; one block of 131072: 51 us; 192 blocks of 512 .. 1024 with
+// their append: 58 us; 16 blocks of 8192, 64 heads over 8 of 64, with append, 133 MB: 32 us; 4 blocks of 96 .. 288: 8 us.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>

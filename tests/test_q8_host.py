@@ -70,7 +70,7 @@ def test_bad_configurations_are_refused(cfg, want):
 @pytest.mark.parametrize("dims,want", [
     ((0, 0, 8, 8, 8), B.CPA_EINVAL), ((4, -1, 8, 8, 8), B.CPA_EINVAL), ((4, 0, 0, 8, 8), B.CPA_EINVAL),
     ((4, 0, 8, -1, 8), B.CPA_EINVAL), ((4, 0, 8, 8, -1), B.CPA_EINVAL), ((1 << 21, 0, 8, 8, 8), B.CPA_EUNSUPPORTED),
-    ((4, 0, 1 << 28, 8, 8), B.CPA_EUNSUPPORTED), ((4, 0, 1 << 26, 8, 8), B.CPA_EUNSUPPORTED)])
+    ((4, 0, 8, (1 << 30) + 1, 8), B.CPA_EUNSUPPORTED), ((4, 0, 1 << 28, 8, 8), B.CPA_EUNSUPPORTED), ((4, 0, 1 << 26, 8, 8), B.CPA_EUNSUPPORTED)])
 def test_bad_sizes_are_refused(dims, want):
     dims = B.cpa_table_dims(*dims)
     assert B.cpa_tables_bytes(_cfg(), dims) == want
