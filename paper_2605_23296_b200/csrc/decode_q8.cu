@@ -137,6 +137,13 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n"
                  :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+// Whether a phase has completed, without the pause of a try.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok;
+}
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
 // four codes to two f16 pairs (the halves are named inside the assembly: taken apart in C++ each costs an instruction)
 struct f16x4 { uint32_t lo, hi; };
@@ -565,7 +572,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             // The last one in joins the partials: at the end of the CTA's work with all warps, else in the background.
             const int nk = k + 1;
             bool end = false;
-            if (mbar_try_wait(dump0 + 8 * (nk % kStages), (uint32_t)(nk / kStages) & 1u)) end = sm_dump_stage[nk % kStages] < 0;
+            if (mbar_test(dump0 + 8 * (nk % kStages), (uint32_t)(nk / kStages) & 1u)) end = sm_dump_stage[nk % kStages] < 0;
             end = __all_sync(0xffffffffu, end);
             if (end) {
                 if (lane == 0) { sm_final = make_int4(blk, head, first, parts); mbar_arrive(end_bar); }
