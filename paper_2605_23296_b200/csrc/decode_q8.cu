@@ -922,8 +922,9 @@ int launch_q8(const cpa_config* cfg, const cpa_table_dims* dims, q8_args& a, cud
     a.min_quota = 8;
     a.slots = partial_slots(cfg);
     a.list_len = dims->page_capacity;
-    // one wave; no more CTAs than the table's pages could keep busy, or the blocks' books need
-    const int64_t most = ((int64_t)dims->page_capacity * cfg->num_kv_heads + a.min_quota - 1) / a.min_quota;
+    // one wave; no more CTAs than the table's pages and blocks could keep busy
+    const int64_t most = (((int64_t)dims->page_capacity + (int64_t)Sh::kUnitCost * dims->num_blocks) * cfg->num_kv_heads +
+                          a.min_quota - 1) / a.min_quota;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(kCtasPerSm * sms, most)));
     lc.blockDim = dim3(kQ8Threads);
