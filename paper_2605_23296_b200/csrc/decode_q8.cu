@@ -43,7 +43,7 @@
 
 namespace {
 
-constexpr int kCons = 4;                              // consumer warps
+constexpr int kCons = 4;                              // consumer warps (the merger counts on four: four times eight heads are its lanes)
 constexpr int kProducer = kCons, kMerger = kCons + 1;  // the other two warps
 constexpr int kQ8Threads = (kCons + 2) * 32;
 constexpr int kCtasPerSm = 2;
@@ -524,37 +524,43 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             const uint4 e0 = lds16(meta + Sh::kDesc), e1 = lds16(meta + Sh::kDesc + 16);
             const int blk = (int)e0.x, head = (int)e0.y, first = (int)e1.z, parts = (int)e1.w;
             const int64_t row0 = (int64_t)slot_of((int)blockIdx.x, first) * a.G;
-#pragma unroll 2
+            // lane (w, h): consumer w's factor of head h, and with the other lanes of h the head's maxima and sum
+            const uint4 x = lds16(meta + Sh::kMl + lane * 16);
+            const float ml = __uint_as_float(x.x), l = __uint_as_float(x.y), mo = __uint_as_float(x.z);
+            float Ml = fmaxf(ml, __shfl_xor_sync(0xffffffffu, ml, 8)), Mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, 8));
+            Ml = fmaxf(Ml, __shfl_xor_sync(0xffffffffu, Ml, 16));
+            Mo = fmaxf(Mo, __shfl_xor_sync(0xffffffffu, Mo, 16));
+            // (a consumer that had no page holds zeros under a maximum of -inf)
+            float f = mo == -INFINITY ? 0.f : ex2(mo - Mo), L = ml == -INFINITY ? l : ex2(ml - Ml) * l;
+            L += __shfl_xor_sync(0xffffffffu, L, 8);
+            L += __shfl_xor_sync(0xffffffffu, L, 16);
+            // The finished row's factor 2^(Mo - kBase - Ml) / L goes in two halves: on its own it may leave fp32's range
+            // where the result does not.
+            const float e = parts == 1 ? ex2(0.5f * (Mo - kBase - Ml)) : 1.f;
+            if (parts == 1) f *= 1.f / L;
+            else if (lane < a.G) partial_ml(a, D)[row0 + lane] = make_float4(Ml, L, Mo, 0.f);
+#pragma unroll 4
             for (int h = 0; h < a.G; ++h) {
-                float Ml = -INFINITY, Mo = -INFINITY, L = 0.f, f[kCons];
-                float4 m[kCons];
+                float fw[kCons];
 #pragma unroll
-                for (int w = 0; w < kCons; ++w) {
-                    const uint4 x = lds16(meta + Sh::kMl + (w * 8 + h) * 16);
-                    m[w] = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), 0.f);
-                    Ml = fmaxf(Ml, m[w].x);
-                    Mo = fmaxf(Mo, m[w].z);
-                }
-#pragma unroll
-                for (int w = 0; w < kCons; ++w) {
-                    // (a warp that had no page holds zeros under a maximum of -inf)
-                    f[w] = m[w].z == -INFINITY ? 0.f : ex2(m[w].z - Mo);
-                    L += m[w].x == -INFINITY ? m[w].y : ex2(m[w].x - Ml) * m[w].y;
-                }
+                for (int w = 0; w < kCons; ++w) fw[w] = __shfl_sync(0xffffffffu, f, 8 * w + h);
+                const float eh = __shfl_sync(0xffffffffu, e, h);
 #pragma unroll
                 for (int i = 0; i < D / 64; ++i) {
                     const int u = lane + 32 * i;
                     float o0 = 0.f, o1 = 0.f;
 #pragma unroll
                     for (int w = 0; w < kCons; ++w) {
-                        const uint2 x = lds8(data + w * Sh::kPageBytes + dump_at<D>(h, u));
-                        o0 = fmaf(f[w], __uint_as_float(x.x), o0);
-                        o1 = fmaf(f[w], __uint_as_float(x.y), o1);
+                        const uint2 y = lds8(data + w * Sh::kPageBytes + dump_at<D>(h, u));
+                        o0 = fmaf(fw[w], __uint_as_float(y.x), o0);
+                        o1 = fmaf(fw[w], __uint_as_float(y.y), o1);
                     }
-                    if (parts == 1) store_pair(a, blk, head, h, D, 2 * u, o0, o1, L, Mo, Ml);
-                    else *reinterpret_cast<float2*>(a.ws + (row0 + h) * D + 2 * u) = make_float2(o0, o1);
+                    if (parts == 1)
+                        *reinterpret_cast<__nv_bfloat162*>(a.o + ((int64_t)blk * a.Hq + head * a.G + h) * D + 2 * u) =
+                            __floats2bfloat162_rn(o0 * eh * eh, o1 * eh * eh);
+                    else
+                        *reinterpret_cast<float2*>(a.ws + (row0 + h) * D + 2 * u) = make_float2(o0, o1);
                 }
-                if (parts > 1 && lane == 0) partial_ml(a, D)[row0 + h] = make_float4(Ml, L, Mo, 0.f);
             }
             __syncwarp();
             if (lane < kCons) mbar_arrive(empty0 + 8 * st);      // for the four consumers
@@ -619,29 +625,33 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             // the queries as f16 B fragments: contracted elements 2t, 2t+1, 2t+8, 2t+9 of step (p, w) are dimensions
             // 64 p + 16 t + 4 w + 0 .. 3.  2^7 at the row's largest element.
             uint4 v[D / 64][2];
-            uint32_t amax = 0;
+            uint32_t two = 0;                                // largest magnitudes, as bf16 bits in two halves
 #pragma unroll
             for (int p = 0; p < D / 64; ++p)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     v[p][i] = g8 < a.G ? lds16(meta + Sh::kQ + (g8 * D + 64 * p + 16 * t4 + 8 * i) * 2) : make_uint4(0, 0, 0, 0);
-                    const uint32_t w[4] = {v[p][i].x, v[p][i].y, v[p][i].z, v[p][i].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) amax = max(amax, max((w[j] << 16) & 0x7FFFFFFFu, w[j] & 0x7FFF0000u));
+                    two = __vmaxu2(__vmaxu2(two, __vmaxu2(v[p][i].x & 0x7FFF7FFFu, v[p][i].y & 0x7FFF7FFFu)),
+                                   __vmaxu2(v[p][i].z & 0x7FFF7FFFu, v[p][i].w & 0x7FFF7FFFu));
                 }
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-            int e = (int)(amax >> 23);                   // biased exponent; infinities and NaN go through as they are
+            two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, 1));
+            two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, 2));
+            const int amax = (int)max(two & 0xFFFFu, two >> 16);
+            int e = amax >> 7;                               // biased exponent; infinities and NaN go through as they are
             e = amax == 0 || e == 255 ? 134 : max(e, 8);
-            const float up = __uint_as_float((uint32_t)(261 - e) << 23), down = __uint_as_float((uint32_t)(e - 7) << 23);
+            const float down = __uint_as_float((uint32_t)(e - 7) << 23);
+            const uint32_t up2 = (uint32_t)(261 - e) << 7 | (uint32_t)(261 - e) << 23;     // a bf16 pair
 #pragma unroll
             for (int p = 0; p < D / 64; ++p)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t w[4] = {v[p][i].x, v[p][i].y, v[p][i].z, v[p][i].w};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        qf[p][2 * i + (j >> 1)][j & 1] = pack_f16(__uint_as_float(w[j] << 16) * up, __uint_as_float(w[j] & 0xFFFF0000u) * up);
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t x;                          // (exact, and what becomes subnormal is below f16's range)
+                        asm("mul.rn.bf16x2 %0, %1, %2;\n" : "=r"(x) : "r"(w[j]), "r"(up2));
+                        qf[p][2 * i + (j >> 1)][j & 1] = pack_f16(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+                    }
                 }
             const float c = down * a.scale_log2;
             c0 = __shfl_sync(0xffffffffu, c, 8 * t4);
@@ -654,6 +664,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                 for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
         }
         const int n_mine = (n - warp + kCons - 1) / kCons;   // this warp's pages of the round (may be 0)
+        bool wrote = false;                                  // into the stage: the copy that refills it has to come after
 
         if ((flags & 4) && n_mine > 0 && warp + kCons * (n_mine - 1) == n - 1) {
             // ---- the block's newest page is this warp's: quantise the new row into it, here and in the pool
@@ -714,7 +725,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                     a.scales[cell * 2 + kind] = s;
                 }
             }
-            fence_async();                                   // the copy that refills the stage comes after these stores
+            wrote = true;
             __syncwarp();
         }
 
@@ -725,7 +736,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                 const int r = cut_at + i / (D / 16);
                 sts16(data + cut_page * Sh::kPageBytes + kPage * D + piece_at<D>(r, i % (D / 16)), 0, 0, 0, 0);
             }
-            fence_async();
+            wrote = true;
             __syncwarp();
         }
         // ---- scores of this warp's pages: s[i] = (key(g), head 2t), (key(g), 2t+1), (key(g+8), 2t), (key(g+8), 2t+1)
@@ -788,6 +799,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                 l0 *= raise(ml0, hi0);
                 l1 *= raise(ml1, hi1);
                 const float f0 = raise(mo0, ho0), f1 = raise(mo1, ho1);
+                if (!(flags & 1))                            // (a segment's first round finds zeros)
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j) { acc[j][0] *= f0; acc[j][1] *= f1; acc[j][2] *= f0; acc[j][3] *= f1; }
             }
@@ -827,12 +839,14 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                 }
             });
         }
-        __syncwarp();
         if (!(flags & 2)) {
+            if (wrote) fence_async();
+            __syncwarp();
             if (lane == 0) mbar_arrive(empty0 + 8 * st);
             continue;
         }
 
+        __syncwarp();                                        // every lane has read its pages
         // ---- the segment is done: leave O and the sums to the merger, over this warp's first page of the round
         l0 += __shfl_xor_sync(0xffffffffu, l0, 4);
         l1 += __shfl_xor_sync(0xffffffffu, l1, 4);
