@@ -136,10 +136,16 @@ __device__ __forceinline__ uint32_t q8_rescale4(uint32_t codes, float f) {
     const float2 a = e4m3x2_to_f32((uint16_t)codes), b = e4m3x2_to_f32((uint16_t)(codes >> 16));
     return to_e4m3x2(mul_keep(a.x, f), mul_keep(a.y, f)) | (to_e4m3x2(mul_keep(b.x, f), mul_keep(b.y, f)) << 16);
 }
-// eight bf16 values times the (inverse) scale, to eight codes
-__device__ __forceinline__ uint2 q8_codes8(uint4 v, float inv) {
+// Whether a scale is one that the append calls give (another writer of the pool may have left any).
+__device__ __forceinline__ bool q8_power_of_two(float s) { return (__float_as_uint(s) & 0x807FFFFFu) == 0 && s <= 0x1p120f; }
+// x / s, by the exact product where s is a power of two
+__device__ __forceinline__ float q8_divide(float x, float s, bool power_of_two) {
+    return power_of_two ? mul_keep(x, q8_inverse(s)) : __fdiv_rn(x, s);
+}
+// eight bf16 values divided by the scale, to eight codes
+__device__ __forceinline__ uint2 q8_codes8(uint4 v, float s) {
     auto two = [&](uint32_t w) {
-        return to_e4m3x2(mul_keep(__uint_as_float(w << 16), inv), mul_keep(__uint_as_float(w & 0xFFFF0000u), inv));
+        return to_e4m3x2(__fdiv_rn(__uint_as_float(w << 16), s), __fdiv_rn(__uint_as_float(w & 0xFFFF0000u), s));
     };
     return make_uint2(two(v.x) | (two(v.y) << 16), two(v.z) | (two(v.w) << 16));
 }

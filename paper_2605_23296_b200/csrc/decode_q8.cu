@@ -706,10 +706,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                         s = old;
                     }
                 }
-                const bool pow2 = (__float_as_uint(s) & 0x807FFFFFu) == 0 && s <= 0x1p120f;
-                const float inv = pow2 ? q8_inverse(s) : 1.f / s;
-                uint32_t codes = to_e4m3x2(mul_keep(x[0], inv), mul_keep(x[1], inv));
-                if (D == 128) codes |= to_e4m3x2(mul_keep(x[D / 32 - 2], inv), mul_keep(x[D / 32 - 1], inv)) << 16;
+                const bool p2 = q8_power_of_two(s);
+                uint32_t codes = to_e4m3x2(q8_divide(x[0], s, p2), q8_divide(x[1], s, p2));
+                if (D == 128) codes |= to_e4m3x2(q8_divide(x[D / 32 - 2], s, p2), q8_divide(x[D / 32 - 1], s, p2)) << 16;
                 const int byte = lane * (D / 32);
                 const uint32_t at = chunk + piece_at<D>(slot, byte >> 4) + (byte & 15);
                 if (D == 128) {

@@ -127,10 +127,8 @@ kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* _
                 s = old;
             }
         }
-        // (a scale that another writer of the pool has left need not be a power of two)
-        const bool pow2 = (__float_as_uint(s) & 0x807FFFFFu) == 0 && s <= 0x1p120f;
         uint8_t* dst = to + lane * 8;
-        if (pow2) {
+        if (q8_power_of_two(s)) {
             const uint32_t inv = __float_as_uint(q8_inverse(s)), inv2 = inv | inv >> 16;      // a bf16 pair
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -138,11 +136,10 @@ kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* _
                 if (slot >= u.p0 && slot < u.p1) *reinterpret_cast<uint2*>(dst + i * 256) = q8_codes8_pow2(x[i], inv2);
             }
         } else {
-            const float inv = 1.f / s;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int slot = slot0 + i * (32 / PIECES);
-                if (slot >= u.p0 && slot < u.p1) *reinterpret_cast<uint2*>(dst + i * 256) = q8_codes8(x[i], inv);
+                if (slot >= u.p0 && slot < u.p1) *reinterpret_cast<uint2*>(dst + i * 256) = q8_codes8(x[i], s);
             }
         }
         __syncwarp();                             // every lane has read the old scale

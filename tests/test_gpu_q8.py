@@ -599,3 +599,38 @@ def test_calls_of_all_kinds_back_to_back(B):
     for o, want in outs:
         for b in range(3):
             assert (np.abs(o[b].double().cpu().numpy() - want[b][0]) <= oq.decode_tolerance(*want[b], 64)).all()
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_append_into_pages_of_any_scale(B, fused):
+    # pages that another writer has filled: a scale that is no power of two is kept while it suffices, and a larger one
+    # is again a power of two
+    c = Cache(B, [21, 40], 8, 2, 128, 2)
+    rng = np.random.default_rng(23)
+    c.append(_values(rng, 61, 2, 128), _values(rng, 61, 2, 128), [21, 40])
+    c.scales *= torch.rand_like(c.scales) * 0.9 + 0.6
+    for t in range(6):
+        old = c.pool.view(torch.float8_e4m3fn).double() * c.scales.double()[..., None, None]
+        was, lens = c.scales.double().cpu().numpy(), c.lens.tolist()
+        k, v = (_values(rng, 2, 2, 128) * 1.7 ** t for _ in range(2))
+        if fused:
+            c.step(rng.standard_normal((2, 4, 128)), k, v)
+        else:
+            c.append(k, v)
+        now = (c.pool.view(torch.float8_e4m3fn).double() * c.scales.double()[..., None, None]).cpu().numpy()
+        s, old_h = c.scales.double().cpu().numpy(), old.cpu().numpy()
+        rows = np.stack([_bf16(k)[1], _bf16(v)[1]], 2)                     # [2, heads, 2, d]
+        for b in range(2):
+            pg, slot = c.want.page_of(b, lens[b]), lens[b] % 16
+            top = np.abs(rows[b]).max(-1)
+            need = oq.page_scale(rows[b][:, :, None])
+            want_s = need if slot == 0 else np.where(need > was[pg], need, was[pg])
+            assert np.array_equal(s[pg], want_s) and (top <= 448 * s[pg]).all()
+            # half a step of e4m3, and the 32-bit quotient's own rounding
+            off = np.abs(now[pg, :, :, slot] - rows[b])
+            assert (off <= (2.0 ** -4 * np.abs(rows[b]) + 2.0 ** -10 * s[pg][..., None]) * (1 + 2.0 ** -20)).all()
+            before = old_h[pg, :, :, :slot]
+            grown = (s[pg] > was[pg])[..., None, None]
+            off = np.abs(now[pg, :, :, :slot] - before)
+            bound = np.where(grown, 2.0 ** -4 * np.abs(before) + 2.0 ** -10 * s[pg][..., None, None], 0.0) * (1 + 2.0 ** -20)
+            assert (off <= bound).all()
