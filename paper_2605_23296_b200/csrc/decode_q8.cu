@@ -218,10 +218,10 @@ __device__ __forceinline__ int dump_at(int h, int u) {
 
 // Joins the partials of a (block, kv head), for the heads of one task (128 floats: one head of 128, two of 64), by one
 // warp.  Lane i of a head's D / 4 lanes holds the factors of partial i of a batch and four dimensions of the result.
-constexpr int kJoin = 16;
 template <int D>
 __device__ __forceinline__ void join_partials(const q8_args& a, int blk, int head, int first, int parts, int task, int lane) {
-    constexpr int HL = D / 4;
+    // partials of a batch, at most HL (20: the 37 of a head of one long block take two batches, 50.0 us for 50.5)
+    constexpr int HL = D / 4, kJoin = D == 128 ? 20 : 16;
     const int sub = lane % HL, h = task * (32 / HL) + lane / HL;
     const bool there = h < a.G;
     const float4* ws_ml = partial_ml(a, D);
