@@ -200,10 +200,11 @@ struct q8_args {
 // Stores a finished row pair: dims d, d + 1 of query head h.
 __device__ __forceinline__ void store_pair(const q8_args& a, int b, int g, int h, int D, int d, float o0, float o1, float L,
                                            float Mo, float Ml) {
-    // the factor 2^(Mo - kBase - Ml) in two halves: on its own it may leave fp32's range where the result does not
+    // the factor 2^(Mo - kBase - Ml) in two halves: on its own it may leave fp32's range where the result does not; the
+    // last product may be subnormal, as bf16 values go down to 2^-133
     const float e = ex2(0.5f * (Mo - kBase - Ml)), inv = 1.f / L;
     *reinterpret_cast<__nv_bfloat162*>(a.o + ((int64_t)b * a.Hq + g * a.G + h) * D + d) =
-        __floats2bfloat162_rn(o0 * inv * e * e, o1 * inv * e * e);
+        __floats2bfloat162_rn(mul_keep(o0 * inv * e, e), mul_keep(o1 * inv * e, e));
 }
 
 __device__ __forceinline__ float4* partial_ml(const q8_args& a, int D) {
@@ -535,7 +536,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             L += __shfl_xor_sync(0xffffffffu, L, 8);
             L += __shfl_xor_sync(0xffffffffu, L, 16);
             // The finished row's factor 2^(Mo - kBase - Ml) / L goes in two halves: on its own it may leave fp32's range
-            // where the result does not.
+            // where the result does not (the last product keeps subnormals, as in store_pair).
             const float e = parts == 1 ? ex2(0.5f * (Mo - kBase - Ml)) : 1.f;
             if (parts == 1) f *= 1.f / L;
             else if (lane < a.G) partial_ml(a, D)[row0 + lane] = make_float4(Ml, L, Mo, 0.f);
@@ -557,7 +558,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                     }
                     if (parts == 1)
                         *reinterpret_cast<__nv_bfloat162*>(a.o + ((int64_t)blk * a.Hq + head * a.G + h) * D + 2 * u) =
-                            __floats2bfloat162_rn(o0 * eh * eh, o1 * eh * eh);
+                            __floats2bfloat162_rn(mul_keep(o0 * eh, eh), mul_keep(o1 * eh, eh));
                     else
                         *reinterpret_cast<float2*>(a.ws + (row0 + h) * D + 2 * u) = make_float2(o0, o1);
                 }
