@@ -566,9 +566,10 @@ CPA_API int cpa_decode_static(const cpa_plan* plan, const void* q, const void* k
  * The append calls give a (page, kv head, K or V) the smallest power of two s >= 2^-126 for which no finite magnitude
  * that the page has held exceeds 448 s; code = x / s rounded to nearest even.  An infinity is stored as +-448, a NaN as
  * NaN.  When a later row needs a larger scale, the codes that the page holds are rounded again (code * s_old / s_new),
- * which only changes codes that become subnormal.  A block's first row in a page starts the page's scale afresh.  The
- * calls that read take any scale, the append calls any positive scale they find.  Slots behind a block's length may hold
- * anything, their page's scale counts only once a row is there.
+ * which only changes codes that become subnormal.  A block's first row in a page starts the page's scale afresh.  Another
+ * writer's pages may have any finite scale that is not negative, zero and subnormal ones among them (cpa_kv_read_q8 takes
+ * negative ones too).  Slots behind a block's length may hold anything, their page's scale counts only once a row is
+ * there.
  *
  * cpa_config: num_q_heads, num_kv_heads, head_dim (64, 128), page_size (16), scale and num_sms as for a plan (the SMs a
  * decode launch may fill, 0 = all); group size G <= 8, at most 1024 kv heads; the other fields are not used.

@@ -36,6 +36,7 @@
 // their append: 58 us; 16 blocks of 8192, 64 heads over 8 of 64, with append, 133 MB: 32 us; 4 blocks of 96 .. 288: 8 us.
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <type_traits>
 
 #include "cache_q8.cuh"
@@ -769,7 +770,8 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             s[i][1] = sum[1] * k1;
             s[i][2] = sum[2] * k0;
             s[i][3] = sum[3] * k1;
-            asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(lv[i]) : "f"(__uint_as_float(sc.y)));
+            // (zero gives -inf: the page takes part in the sums with weights of zero; scales below the normal range count)
+            asm("lg2.approx.f32 %0, %1;\n" : "=f"(lv[i]) : "f"(__uint_as_float(sc.y)));
             if (j == cut_page && cut_at < kPage) {
                 if (key_of_row<D>(g8) >= cut_at) s[i][0] = s[i][1] = -INFINITY;
                 if (key_of_row<D>(g8 + 8) >= cut_at) s[i][2] = s[i][3] = -INFINITY;
@@ -804,7 +806,8 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                 for (int j = 0; j < D / 16; ++j) { acc[j][0] *= f0; acc[j][1] *= f1; acc[j][2] *= f0; acc[j][3] *= f1; }
             }
             // ---- weights, and O^T += V^T P^T
-            const float b0 = kBase - mo0, b1 = kBase - mo1;
+            // (a maximum of -inf: nothing but pages whose V scale is zero so far, whose weights have to come out as zero)
+            const float b0 = kBase - fmaxf(mo0, -FLT_MAX), b1 = kBase - fmaxf(mo1, -FLT_MAX);
             uint32_t va[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) va[r] = data + v_off[r];

@@ -39,3 +39,45 @@ def test_rows_below_the_normal_range_keep_their_values(B, d, num_sms):
     o, qf = c.step(q, _values(rng, 3, 2, d), _values(rng, 3, 2, d) * 2.0 ** -129)
     c.check_rows(o, qf, what="step")
     c.check_pool()
+
+
+def _set_scales(c, kind, pages, value):
+    """Gives pages (positions in each block's list) of K (0) or V (1) a scale, on the device and in the oracle."""
+    for b, n in enumerate(c.lens0):
+        for j in range(-(-n // 16)):
+            if pages(j, -(-n // 16)):
+                pg = c.want.page_of(b, 16 * j)
+                c.scales[pg, :, kind] = value
+                c.want.scales[pg, :, kind] = value
+
+
+WHERE = {"all": lambda j, n: True, "one warp": lambda j, n: j % 4 == 1, "another warp": lambda j, n: j % 4 == 2,
+         "first round": lambda j, n: j < 16, "last round": lambda j, n: j >= n - 16, "even": lambda j, n: j % 2 == 0,
+         "all but one": lambda j, n: j != 2}
+
+
+@pytest.mark.parametrize("where", list(WHERE))
+@pytest.mark.parametrize("value", [0.0, 2.0 ** -149, 2.0 ** -130, 1.25 * 2.0 ** -127])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_of_zero_and_below_the_normal_range(B, d, value, where):
+    # what another writer gives a page of zeros; both directions of the walk (even and odd first lengths)
+    for first, num_sms in ((700, 0), (701, 0), (700, 1), (701, 1)):
+        c = Cache(B, [first, 33, 16, 640], 2, 2, d, 4, seed=d, num_sms=num_sms)
+        rng = np.random.default_rng(first + d)
+        n = sum(c.lens0)
+        c.append(_values(rng, n, 2, d), _values(rng, n, 2, d), c.lens0)
+        _set_scales(c, 1, WHERE[where], value)
+        _steps(c, rng, f"{first} {num_sms}")
+
+
+@pytest.mark.parametrize("value", [0.0, 2.0 ** -130])
+def test_read_back_of_such_pages(B, value):
+    c = Cache(B, [100], 0, 2, 64)
+    rng = np.random.default_rng(3)
+    c.append(_values(rng, 100, 2, 64), _values(rng, 100, 2, 64), [100])
+    for kind in (0, 1):
+        _set_scales(c, kind, WHERE["even"], value)
+    out = torch.empty(2, 100, 2, 64, dtype=torch.bfloat16, device="cuda")
+    assert B.cpa_kv_read_q8(c.cfg, c.dims, c.tables, None, _i32([0, 100]), 100, c.pool, c.scales, out[0], out[1]) == 0
+    want = torch.from_numpy(c.want.rows(0, 0, 100).transpose(0, 2, 1, 3)).bfloat16()     # (small ones are rounded once)
+    assert torch.equal(out.cpu(), want)
