@@ -134,6 +134,12 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(d) : "f"(x));
     return d;
 }
+// product rounded towards zero, which keeps subnormals and never gives an infinity of finite factors
+__device__ __forceinline__ float mul_down(float a, float b) {
+    float d;
+    asm("mul.rz.f32 %0, %1, %2;\n" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n"
                  :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
@@ -655,7 +661,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                         qf[p][2 * i + (j >> 1)][j & 1] = pack_f16(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
                     }
                 }
-            const float c = down * a.scale_log2;
+            const float c = mul_keep(down, a.scale_log2);
             c0 = __shfl_sync(0xffffffffu, c, 8 * t4);
             c1 = __shfl_sync(0xffffffffu, c, 8 * t4 + 4);
             ml0 = ml1 = mo0 = mo1 = -INFINITY;
@@ -765,7 +771,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                 const f16x4 x0 = to_f16x4(w0[w]), x1 = to_f16x4(w1[w]);
                 mma_f16(sum, x0.lo, x1.lo, x0.hi, x1.hi, qf[w >> 2][w & 3][0], qf[w >> 2][w & 3][1]);
             }
-            const float ks = __uint_as_float(sc.x), k0 = ks * c0, k1 = ks * c1;
+            // (either factor may be subnormal; rounded towards zero a product that passes fp32's range stays finite, so that
+            // keys of zeros score zero there too)
+            const float ks = __uint_as_float(sc.x), k0 = mul_down(ks, c0), k1 = mul_down(ks, c1);
             s[i][0] = sum[0] * k0;
             s[i][1] = sum[1] * k1;
             s[i][2] = sum[2] * k0;

@@ -81,3 +81,39 @@ def test_read_back_of_such_pages(B, value):
     assert B.cpa_kv_read_q8(c.cfg, c.dims, c.tables, None, _i32([0, 100]), 100, c.pool, c.scales, out[0], out[1]) == 0
     want = torch.from_numpy(c.want.rows(0, 0, 100).transpose(0, 2, 1, 3)).bfloat16()     # (small ones are rounded once)
     assert torch.equal(out.cpu(), want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q_exp,k_exp,scale_exp", [(-118, 118, None), (118, -118, None), (118, None, -130), (100, None, -112),
+                                                   (-100, 100, None)])
+def test_scores_whose_factors_leave_the_normal_range(B, d, q_exp, k_exp, scale_exp):
+    # scores of ordinary size out of a tiny query and huge keys, or the other way round
+    c = Cache(B, [300, 17], 0, 2, d, 4, seed=d)
+    rng = np.random.default_rng(41)
+    k = _values(rng, 317, 2, d, 0.2).clip(-7, 7) * 2.0 ** (k_exp or 0)
+    c.append(k, _values(rng, 317, 2, d), [300, 17])
+    if scale_exp is not None:
+        _set_scales(c, 0, WHERE["all"], 2.0 ** scale_exp)
+    o, qf = c.decode(rng.standard_normal((2, 8, d)) * 2.0 ** q_exp)
+    c.check_rows(o, qf)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_of_minus_infinity_beside_a_zero(B, d):
+    # keys so large that their scores pass fp32's range downwards take no weight, and do not spoil the keys of zeros in
+    # their own pages: the answer is the mean of the zero keys' values
+    n = 330
+    c = Cache(B, [n, n + 1], 0, 1, d, 1, seed=d)
+    rng = np.random.default_rng(42)
+    q = rng.choice([-1.0, 1.0], (2, 1, d)) * 2.0 ** 60
+    zero = (rng.random(2 * n + 1) < 0.1) | (np.arange(2 * n + 1) % 8 == 3)       # some in every page
+    k = np.concatenate([np.repeat(-q[0][None], n, 0), np.repeat(-q[1][None], n + 1, 0)]) * 2.0 ** 40
+    k[zero] = 0.0
+    v = rng.standard_normal((2 * n + 1, 1, d))
+    c.append(k, v, [n, n + 1])
+    o, _ = c.decode(q)
+    for b, (lo, hi) in enumerate(((0, n), (n, 2 * n + 1))):
+        rows = c.want.rows(b, 0, hi - lo)[1, 0][zero[lo:hi]]
+        want, spread = rows.mean(0), np.abs(rows).mean(0)
+        off = np.abs(o[b, 0].double().cpu().numpy() - want)
+        assert (off <= oq.decode_tolerance(want, spread, 0.0, d)).all(), off.max()
