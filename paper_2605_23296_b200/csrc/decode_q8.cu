@@ -53,6 +53,9 @@ constexpr int kAhead = 2;                             // rounds that the produce
 constexpr uint32_t kLongSpin = 1u << 24;              // waits that last for a whole range of pages
 constexpr uint32_t kQ8Spin = 1u << 18;                // bounded waits (each try suspends briefly)
 constexpr float kBase = 6.f, kSlack = 9.f;            // weights: 2^kBase at the maximum, up to 2^(kBase + kSlack) above it
+// What the running maxima start from.  Finite, so that scores of -inf (beyond fp32, or of a V scale of zero) less a maximum
+// that has met nothing else are -inf and their weights zero; a row of nothing else is 0 / 0, NaN, as a softmax's is.
+constexpr float kLowest = -FLT_MAX;
 
 template <int D>
 struct Q8Shape {
@@ -254,8 +257,8 @@ __device__ __forceinline__ void join_partials(const q8_args& a, int blk, int hea
         const float fl = Ml == -INFINITY ? 0.f : ex2(Ml - ml), fo = Mo == -INFINITY ? 0.f : ex2(Mo - mo);
         Ml = ml;
         Mo = mo;
-        // (a partial with a maximum of -inf has met nothing but NaN: its sums are NaN and pass on as they are)
-        L = L * fl + (m.x == -INFINITY ? m.y : ex2(m.x - Ml) * m.y);
+        // (lanes without a partial hold a maximum of -inf and a sum of zero)
+        L = L * fl + (m.x == -INFINITY ? 0.f : ex2(m.x - Ml) * m.y);
         const float f = m.z == -INFINITY ? 0.f : ex2(m.z - Mo);
         o.x *= fo; o.y *= fo; o.z *= fo; o.w *= fo;
 #pragma unroll
@@ -538,8 +541,8 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             float Ml = fmaxf(ml, __shfl_xor_sync(0xffffffffu, ml, 8)), Mo = fmaxf(mo, __shfl_xor_sync(0xffffffffu, mo, 8));
             Ml = fmaxf(Ml, __shfl_xor_sync(0xffffffffu, Ml, 16));
             Mo = fmaxf(Mo, __shfl_xor_sync(0xffffffffu, Mo, 16));
-            // (a consumer that had no page holds zeros under a maximum of -inf)
-            float f = mo == -INFINITY ? 0.f : ex2(mo - Mo), L = ml == -INFINITY ? l : ex2(ml - Ml) * l;
+            // (a consumer that had no page holds zeros under the lowest maximum)
+            float f = ex2(mo - Mo), L = ex2(ml - Ml) * l;
             L += __shfl_xor_sync(0xffffffffu, L, 8);
             L += __shfl_xor_sync(0xffffffffu, L, 16);
             // The finished row's factor 2^(Mo - kBase - Ml) / L goes in two halves: on its own it may leave fp32's range
@@ -620,7 +623,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
     }
     uint32_t qf[D / 64][4][2];
     float acc[D / 16][4], c0 = 0.f, c1 = 0.f;           // c: what a score's sum is multiplied with, for heads 2t, 2t + 1
-    float ml0 = -INFINITY, ml1 = -INFINITY, mo0 = -INFINITY, mo1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    float ml0 = kLowest, ml1 = kLowest, mo0 = kLowest, mo1 = kLowest, l0 = 0.f, l1 = 0.f;
 
     for (int it = 0;; ++it) {
         const int st = it % kStages;
@@ -664,7 +667,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             const float c = mul_keep(down, a.scale_log2);
             c0 = __shfl_sync(0xffffffffu, c, 8 * t4);
             c1 = __shfl_sync(0xffffffffu, c, 8 * t4 + 4);
-            ml0 = ml1 = mo0 = mo1 = -INFINITY;
+            ml0 = ml1 = mo0 = mo1 = kLowest;
             l0 = l1 = 0.f;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j)
@@ -802,7 +805,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                     ho1 = fmaxf(ho1, __shfl_xor_sync(0xffffffffu, ho1, o));
                 }
                 auto raise = [](float& m, float hi) {        // the factor of what was summed under the old maximum
-                    const float up = fmaxf(m, hi), f = m == -INFINITY ? 0.f : ex2(m - up);
+                    const float up = fmaxf(m, hi), f = ex2(m - up);
                     m = up;
                     return f;
                 };
@@ -814,8 +817,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                 for (int j = 0; j < D / 16; ++j) { acc[j][0] *= f0; acc[j][1] *= f1; acc[j][2] *= f0; acc[j][3] *= f1; }
             }
             // ---- weights, and O^T += V^T P^T
-            // (a maximum of -inf: nothing but pages whose V scale is zero so far, whose weights have to come out as zero)
-            const float b0 = kBase - fmaxf(mo0, -FLT_MAX), b1 = kBase - fmaxf(mo1, -FLT_MAX);
+            const float b0 = kBase - mo0, b1 = kBase - mo1;
             uint32_t va[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) va[r] = data + v_off[r];

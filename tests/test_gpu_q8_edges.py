@@ -117,3 +117,32 @@ def test_scores_of_minus_infinity_beside_a_zero(B, d):
         want, spread = rows.mean(0), np.abs(rows).mean(0)
         off = np.abs(o[b, 0].double().cpu().numpy() - want)
         assert (off <= oq.decode_tolerance(want, spread, 0.0, d)).all(), off.max()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [0, 1, 5, 18, 41])
+def test_whole_pages_of_minus_infinity(B, d, page):
+    # every score but those of one page passes fp32's range downwards: warps, rounds and whole ranges meet nothing else
+    n = 700
+    for more in (0, 1):
+        c = Cache(B, [n + more, 64], 0, 1, d, 1, seed=d)
+        rng = np.random.default_rng(43)
+        q = rng.choice([-1.0, 1.0], (2, 1, d)) * 2.0 ** 37
+        k = np.repeat(-q[0][None], n + more + 64, 0) * 2.0 ** 63
+        k[16 * page:16 * page + 16] = 0.0
+        k[n + more:] = 0.0
+        v = rng.standard_normal((n + more + 64, 1, d))
+        c.append(k, v, [n + more, 64])
+        o, _ = c.decode(q)
+        for b, rows in enumerate((c.want.rows(0, 16 * page, min(16 * page + 16, n + more))[1, 0], c.want.rows(1, 0, 64)[1, 0])):
+            want, spread = rows.mean(0), np.abs(rows).mean(0)
+            off = np.abs(o[b, 0].double().cpu().numpy() - want)
+            assert (off <= oq.decode_tolerance(want, spread, 0.0, d)).all(), (more, b, off.max())
+
+
+def test_a_row_of_nothing_but_minus_infinity_is_nan(B):
+    c = Cache(B, [100], 0, 1, 64, 1)
+    q = np.full((1, 1, 64), 2.0 ** 37)
+    c.append(np.full((100, 1, 64), -2.0 ** 100), np.ones((100, 1, 64)), [100])
+    o, _ = c.decode(q)
+    assert torch.isnan(o).all()
