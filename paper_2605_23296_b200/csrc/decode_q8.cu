@@ -703,7 +703,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
                     float old;
                     asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(old) : "r"(sc_at));
                     if (s > old) {
-                        const float f = old * q8_inverse(s);
+                        const float f = mul_keep(old, q8_inverse(s));   // (another writer's scale may be subnormal)
                         for (int i = lane; i < slot * (D / 4); i += 32) {
                             const int r = i / (D / 4), c = i % (D / 4);
                             const uint32_t at = chunk + piece_at<D>(r, c >> 2) + (c & 3) * 4;

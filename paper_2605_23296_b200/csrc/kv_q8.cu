@@ -118,7 +118,7 @@ kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* _
         float s = q8_scale(amax);
         if (u.p0 > 0) {
             if (s > old) {
-                const float f = old * q8_inverse(s);
+                const float f = mul_keep(old, q8_inverse(s));   // (another writer's scale may be subnormal)
                 for (int i = lane; i < u.p0 * (D / 4); i += 32) {
                     uint32_t* c = reinterpret_cast<uint32_t*>(to) + i;
                     *c = q8_rescale4(*c, f);

@@ -146,3 +146,23 @@ def test_a_row_of_nothing_but_minus_infinity_is_nan(B):
     c.append(np.full((100, 1, 64), -2.0 ** 100), np.ones((100, 1, 64)), [100])
     o, _ = c.decode(q)
     assert torch.isnan(o).all()
+
+
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("old", [2.0 ** -130, 2.0 ** -149, 1.5 * 2.0 ** -128, 0.0])
+def test_append_to_pages_whose_scale_is_below_the_normal_range(B, d, old, fused):
+    # another writer's page: its codes are rounded again to the new scale, not lost
+    c = Cache(B, [21, 40], 8, 2, d, 2)
+    rng = np.random.default_rng(51)
+    c.append(_values(rng, 61, 2, d), _values(rng, 61, 2, d), [21, 40])
+    for kind in (0, 1):
+        _set_scales(c, kind, WHERE["all"], old)
+    for t in range(3):
+        k, v = (_values(rng, 2, 2, d) * 2.0 ** (6 * t - 122) for _ in range(2))
+        if fused:
+            o, qf = c.step(rng.standard_normal((2, 4, d)), k, v)
+            c.check_rows(o, qf, what=f"step {t}")
+        else:
+            c.append(k, v)
+        c.check_pool(f"token {t}")
