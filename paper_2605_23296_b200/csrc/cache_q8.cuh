@@ -110,10 +110,15 @@ __device__ __forceinline__ uint32_t q8_finite_abs(uint32_t bits) {
     const uint32_t a = bits & 0x7FFFFFFFu;
     return a < 0x7F800000u ? a : 0u;
 }
-// product that keeps subnormal inputs (the file's other arithmetic may flush them)
+// product and quotient that keep subnormals (the file's other arithmetic may flush them)
 __device__ __forceinline__ float mul_keep(float a, float b) {
     float d;
     asm("mul.rn.f32 %0, %1, %2;\n" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float div_keep(float a, float b) {
+    float d;
+    asm("div.rn.f32 %0, %1, %2;\n" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
 // two values to e4m3, nearest even; beyond 448 (infinities alone get there) to 448; NaN stays NaN
@@ -140,12 +145,12 @@ __device__ __forceinline__ uint32_t q8_rescale4(uint32_t codes, float f) {
 __device__ __forceinline__ bool q8_power_of_two(float s) { return (__float_as_uint(s) & 0x807FFFFFu) == 0 && s <= 0x1p120f; }
 // x / s, by the exact product where s is a power of two
 __device__ __forceinline__ float q8_divide(float x, float s, bool power_of_two) {
-    return power_of_two ? mul_keep(x, q8_inverse(s)) : __fdiv_rn(x, s);
+    return power_of_two ? mul_keep(x, q8_inverse(s)) : div_keep(x, s);
 }
 // eight bf16 values divided by the scale, to eight codes
 __device__ __forceinline__ uint2 q8_codes8(uint4 v, float s) {
     auto two = [&](uint32_t w) {
-        return to_e4m3x2(__fdiv_rn(__uint_as_float(w << 16), s), __fdiv_rn(__uint_as_float(w & 0xFFFF0000u), s));
+        return to_e4m3x2(div_keep(__uint_as_float(w << 16), s), div_keep(__uint_as_float(w & 0xFFFF0000u), s));
     };
     return make_uint2(two(v.x) | (two(v.y) << 16), two(v.z) | (two(v.w) << 16));
 }

@@ -166,3 +166,22 @@ def test_append_to_pages_whose_scale_is_below_the_normal_range(B, d, old, fused)
         else:
             c.append(k, v)
         c.check_pool(f"token {t}")
+
+
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_of_tiny_rows_under_a_scale_that_is_no_power_of_two(B, d, fused):
+    # rows below fp32's normal range, divided by a kept scale of 1.5 * 2^-126.  (A bf16 value over 1.5 is a midpoint of two
+    # codes exactly or by 2^-9 of itself at least, so the 32-bit quotient rounds to the code that the 64-bit one gives.)
+    c = Cache(B, [21, 40], 8, 2, d, 2)
+    rng = np.random.default_rng(52)
+    c.append(_values(rng, 61, 2, d) * 2.0 ** -120, _values(rng, 61, 2, d) * 2.0 ** -120, [21, 40])
+    for kind in (0, 1):
+        _set_scales(c, kind, WHERE["all"], 1.5 * 2.0 ** -126)
+    for t in range(3):
+        k, v = (_values(rng, 2, 2, d) * 2.0 ** (t - 129) for _ in range(2))
+        if fused:
+            c.step(rng.standard_normal((2, 4, d)), k, v)
+        else:
+            c.append(k, v)
+        c.check_pool(f"token {t}")
