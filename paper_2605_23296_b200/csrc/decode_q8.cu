@@ -41,6 +41,7 @@
 
 #include "cache_q8.cuh"
 #include "cpa_tcgen05.cuh"
+#include "ring.h"
 
 namespace {
 
@@ -516,12 +517,14 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) { d[i] = d[i + 1]; id[i] = id[i + 1]; }
         }
-        if (dead) {                                     // a wait gave up: see the copies in flight through before leaving
-            if (lane == 0)
-                for (int i = max(0, it - kStages); i < it; ++i)
-                    mbar_drain(full0 + 8 * (i % kStages), (uint32_t)(i / kStages) & 1u, kDrainLimit);
-            __syncwarp();
+        // See the copies in flight through before leaving: the consumers do so by using them, but not when one of their
+        // waits has given up, which this warp need not have met.
+        if (lane == 0) {
+            const ring_rounds left = ring_in_flight(it, kStages, !dead);
+            for (int i = left.first; i < left.end; ++i)
+                mbar_drain(full0 + 8 * (i % kStages), (uint32_t)(i / kStages) & 1u, kDrainLimit);
         }
+        __syncwarp();
         return;
     }
 
