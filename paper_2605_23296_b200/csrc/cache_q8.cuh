@@ -75,6 +75,21 @@ inline int q8_check(const cpa_config* c, const cpa_table_dims* d) {
     return CPA_OK;
 }
 
+// Loads of what an earlier launch of the stream may have written.  A programmatic launch begins before that launch has
+// ended, so its kernel may use neither non-coherent loads (their data would have to be constant from the kernel's begin)
+// nor ordinary ones of a __restrict__ const argument (which the compiler may turn into those, or move in front of the
+// wait).  Volatile assembly stays behind the wait, which is volatile assembly too.
+__device__ __forceinline__ int32_t ld_i32(const int32_t* p) {
+    int32_t v;
+    asm volatile("ld.global.s32 %0, [%1];\n" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float ld_f32(const float* p) {
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];\n" : "=f"(v) : "l"(p));
+    return v;
+}
+
 // A programmatic launch: the grid may be made ready while the stream's earlier work ends; the kernel waits for that
 // work (griddepcontrol.wait) before it reads anything.
 template <class... P, class... A>

@@ -182,10 +182,11 @@ __device__ __forceinline__ int key_of_row(int i) {
 }
 
 // A block's tokens as this launch sees them, or -1 when it sits out.
-__device__ __forceinline__ int block_len(int b, const q8_tables& t, const int32_t* __restrict__ lens,
-                                         const int32_t* __restrict__ active, int append, int& ip, int& status) {
+__device__ __forceinline__ int block_len(int b, const q8_tables& t, const int32_t* lens, const int32_t* active, int append,
+                                         int& ip, int& status) {
     // (all loads first, so that those of several blocks can be in flight together)
-    const int len = lens[b], first = __ldg(t.page_indptr + b), end = __ldg(t.page_indptr + b + 1), on = active ? active[b] : 1;
+    const int len = ld_i32(lens + b), first = ld_i32(t.page_indptr + b), end = ld_i32(t.page_indptr + b + 1),
+              on = active ? ld_i32(active + b) : 1;
     ip = first;
     status = on == 0 ? 0 : len < 0 ? kStatusInvalid : (int64_t)len + append > (int64_t)(end - first) * kPage ? kStatusNoSpace : 0;
     return on == 0 || status ? -1 : len + append;
@@ -330,7 +331,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
         int ip, status;
         const int len = block_len((int)b, a.t, a.lens, a.active, append, ip, status);
         if (status) atomicCAS(a.t.header, 0, status);
-        if (a.lens_out) a.lens_out[b] = len < 0 ? a.lens[b] : len;
+        if (a.lens_out) a.lens_out[b] = len < 0 ? ld_i32(a.lens + b) : len;
         if (len == 0)
             for (int i = 0; i < a.Hq * (D / 8); ++i)
                 reinterpret_cast<uint4*>(a.o + b * a.Hq * D)[i] = make_uint4(0, 0, 0, 0);
@@ -471,7 +472,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap tm, const q8_args a) {
             r.len = len;
             r.first = first;
             r.parts = parts;
-            id = lane < r.n ? __ldg(a.t.page_indices + ip + r.page0 + lane) : 0;
+            id = lane < r.n ? ld_i32(a.t.page_indices + ip + r.page0 + lane) : 0;
             (down ? pe : pb) += down ? -r.n : r.n;
             r.flags |= (pb >= pe ? 2 : 0) | (append && r.page0 + r.n == pages ? 4 : 0);
         };

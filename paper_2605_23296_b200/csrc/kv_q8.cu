@@ -30,11 +30,11 @@ struct page_unit {
 };
 
 // cu == nullptr: one row per block
-__device__ __forceinline__ int cu_at(const int32_t* cu, int b) { return cu ? __ldg(cu + b) : b; }
+__device__ __forceinline__ int cu_at(const int32_t* cu, int b) { return cu ? ld_i32(cu + b) : b; }
 
 // By a whole warp: 32 candidates are looked at per load.
-__device__ __forceinline__ page_unit find_unit(int u, const q8_tables& t, const int32_t* __restrict__ cu,
-                                               const int32_t* __restrict__ first, int B, int rows, int lane) {
+__device__ __forceinline__ page_unit find_unit(int u, const q8_tables& t, const int32_t* cu, const int32_t* first, int B, int rows,
+                                               int lane) {
     int lo = 0, size = B;
     while (size > 1) {
         const int step = (size + 31) / 32, i = lane * step, b = lo + i;
@@ -44,15 +44,15 @@ __device__ __forceinline__ page_unit find_unit(int u, const q8_tables& t, const 
         size = min(step, size - skip);
     }
     page_unit r{-1, 0, 0, 0, 0};
-    const int c0 = cu_at(cu, lo), c1 = cu_at(cu, lo + 1), at = first ? __ldg(first + lo) : 0;
-    const int ip = __ldg(t.page_indptr + lo), np = __ldg(t.page_indptr + lo + 1) - ip;
+    const int c0 = cu_at(cu, lo), c1 = cu_at(cu, lo + 1), at = first ? ld_i32(first + lo) : 0;
+    const int ip = ld_i32(t.page_indptr + lo), np = ld_i32(t.page_indptr + lo + 1) - ip;
     const int n = c1 - c0, j = u - (c0 / kPage + 2 * lo);
     if (n <= 0 || at < 0 || c0 < 0 || c1 > rows || j < 0) return r;
     if ((int64_t)at + n > (int64_t)np * kPage) return r;            // does not fit: the whole block is left out
     const int pg = at / kPage + j;
     if (pg * kPage >= at + n) return r;
     r.block = lo;
-    r.page = __ldg(t.page_indices + ip + pg);
+    r.page = ld_i32(t.page_indices + ip + pg);
     r.p0 = max(at - pg * kPage, 0);
     r.p1 = min(at + n - pg * kPage, kPage);
     r.row = c0 + pg * kPage + r.p0 - at;
@@ -61,18 +61,18 @@ __device__ __forceinline__ page_unit find_unit(int u, const q8_tables& t, const 
 
 // What a block's range of rows is worth: 0, or the status of why it is left out.
 __device__ __forceinline__ int range_status(int b, const q8_tables& t, const int32_t* cu, const int32_t* first, int rows) {
-    const int c0 = cu_at(cu, b), n = cu_at(cu, b + 1) - c0, at = first ? first[b] : 0;
+    const int c0 = cu_at(cu, b), n = cu_at(cu, b + 1) - c0, at = first ? ld_i32(first + b) : 0;
     if (n < 0 || at < 0 || c0 < 0 || (int64_t)c0 + n > rows) return kStatusInvalid;
-    return (int64_t)at + n > (int64_t)(t.page_indptr[b + 1] - t.page_indptr[b]) * kPage ? kStatusNoSpace : 0;
+    return (int64_t)at + n > (int64_t)(ld_i32(t.page_indptr + b + 1) - ld_i32(t.page_indptr + b)) * kPage ? kStatusNoSpace : 0;
 }
 
 // (four CTAs per SM: what hides the latency of the unit search and the loads is the number of warps; three, at the 74
 // registers that the compiler would take, run at 154 us instead of 144 for 32 prompts of 1024 .. 8192 tokens)
 template <int D>
 __global__ void __launch_bounds__(kWarps * 32, 4)
-kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* __restrict__ v_new,
-                    const int32_t* __restrict__ cu, const int32_t* __restrict__ lens, int32_t* __restrict__ lens_out,
-                    uint8_t* __restrict__ pool, float* __restrict__ scales, int B, int rows, int Hkv, int64_t n_items) {
+kv_append_q8_kernel(q8_tables t, const uint4* k_new, const uint4* v_new, const int32_t* cu, const int32_t* lens,
+                    int32_t* lens_out, uint8_t* __restrict__ pool, float* __restrict__ scales, int B, int rows, int Hkv,
+                    int64_t n_items) {
     constexpr int PIECES = D / 8;                 // 16-byte pieces of a bf16 row
     constexpr int N = kPage * PIECES / 32;        // pieces per lane of a page's K or V
     const int lane = threadIdx.x & 31;
@@ -82,7 +82,7 @@ kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* _
     for (int64_t b = tid; b < B; b += n_threads) {
         const int st = range_status((int)b, t, cu, lens, rows);
         if (st) atomicCAS(t.header, 0, st);
-        if (lens_out) lens_out[b] = (lens ? lens[b] : 0) + (st ? 0 : cu_at(cu, (int)b + 1) - cu_at(cu, (int)b));
+        if (lens_out) lens_out[b] = (lens ? ld_i32(lens + b) : 0) + (st ? 0 : cu_at(cu, (int)b + 1) - cu_at(cu, (int)b));
     }
     for (int64_t item = tid >> 5; item < n_items; item += n_threads >> 5) {
         const int kind = (int)(item & 1), g = (int)((item >> 1) % Hkv);
@@ -100,7 +100,7 @@ kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* _
         const int64_t cell = (int64_t)u.page * Hkv + g;
         float* sc = scales + cell * 2 + kind;
         uint8_t* to = pool + cell * (2 * kPage * D) + kind * (kPage * D);
-        const float old = u.p0 > 0 ? *sc : 0.f;   // the page holds tokens already
+        const float old = u.p0 > 0 ? ld_f32(sc) : 0.f;   // the page holds tokens already
         // largest magnitude, as bf16 bits of two halves; infinities and NaN, which do not count, are sorted out only
         // where the page has any
         uint32_t two = 0;
@@ -149,9 +149,8 @@ kv_append_q8_kernel(q8_tables t, const uint4* __restrict__ k_new, const uint4* _
 
 template <int D>
 __global__ void __launch_bounds__(kWarps * 32)
-kv_read_q8_kernel(q8_tables t, const int32_t* __restrict__ cu, const int32_t* __restrict__ first,
-                  const uint8_t* __restrict__ pool, const float* __restrict__ scales, uint4* __restrict__ k_out,
-                  uint4* __restrict__ v_out, int B, int rows, int Hkv, int64_t n_items) {
+kv_read_q8_kernel(q8_tables t, const int32_t* cu, const int32_t* first, const uint8_t* pool, const float* scales,
+                  uint4* __restrict__ k_out, uint4* __restrict__ v_out, int B, int rows, int Hkv, int64_t n_items) {
     constexpr int PIECES = D / 8;                 // pieces of 8 codes of a row: a warp's stores are whole lines
     constexpr int N = kPage * PIECES / 32;        // pieces per lane of a page's K or V
     const int lane = threadIdx.x & 31;
@@ -168,7 +167,7 @@ kv_read_q8_kernel(q8_tables t, const int32_t* __restrict__ cu, const int32_t* __
         if (u.block < 0) continue;
         const int64_t cell = (int64_t)u.page * Hkv + g;
         const uint2* chunk = reinterpret_cast<const uint2*>(pool + cell * (2 * kPage * D) + kind * (kPage * D));
-        const float s = __ldg(scales + cell * 2 + kind);
+        const float s = ld_f32(scales + cell * 2 + kind);
         uint2 x[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {

@@ -40,8 +40,8 @@ __device__ __forceinline__ pair64 cta_sum(pair64 v, pair64* sm) {
 }
 
 __global__ void __launch_bounds__(kThreads)
-tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t* __restrict__ free_pages, int B, int T,
-                    int num_pages, int page_limit, int token_limit, int n_tickets) {
+tables_build_kernel(q8_tables t, const int32_t* lens, const int32_t* free_pages, int B, int T, int num_pages,
+                    int page_limit, int token_limit, int n_tickets) {
     __shared__ int sm_cu[kChunk + 1], sm_ip[kChunk + 1];
     __shared__ pair64 sm_warp[kThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -52,7 +52,7 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
     // of the first chunk stay in registers.
     // (this thread's first page id is fetched beside the first lengths, whether the blocks will take it or not)
     const int list0 = blockIdx.x * kThreads + tid;
-    const int id0 = list0 < page_limit ? __ldg(free_pages + list0) : 0;
+    const int id0 = list0 < page_limit ? ld_i32(free_pages + list0) : 0;
     int L[kPerThread];
     pair64 sum{0, 0};
     bool bad = false;
@@ -60,7 +60,7 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
             const int b = at + tid * kPerThread + i;
-            L[i] = b < B ? lens[b] : -1;
+            L[i] = b < B ? ld_i32(lens + b) : -1;
             bad |= b < B && L[i] < 0;
         }
     };
@@ -144,7 +144,7 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
                 if (sm_cu[mid] <= first) lo = mid; else hi = mid - 1;
             }
             auto page_at = [&](int i) {
-                const int page = __ldg(free_pages + i);
+                const int page = ld_i32(free_pages + i);
                 return (unsigned)page < (unsigned)num_pages ? page : 0;
             };
             if (last - first == kRun && sm_cu[lo + 1] >= last) {
@@ -168,7 +168,7 @@ tables_build_kernel(q8_tables t, const int32_t* __restrict__ lens, const int32_t
     // the page list; an id outside the pool is replaced by page 0, so that no later call leaves the pool
     bool bad_id = false;
     for (int i = list0; i < (int)total.pages; i += gridDim.x * kThreads) {
-        const int id = i == list0 ? id0 : __ldg(free_pages + i);
+        const int id = i == list0 ? id0 : ld_i32(free_pages + i);
         const bool out = (unsigned)id >= (unsigned)num_pages;
         bad_id |= out;
         t.page_indices[i] = out ? 0 : id;

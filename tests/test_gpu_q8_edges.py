@@ -185,3 +185,65 @@ def test_append_of_tiny_rows_under_a_scale_that_is_no_power_of_two(B, d, fused):
         else:
             c.append(k, v)
         c.check_pool(f"token {t}")
+
+
+def test_tables_rebuilt_between_calls_without_a_wait(B):
+    # two events take turns on one table buffer, one workspace and one pool: build, append by the tables' own cu_seqlens,
+    # decode, step and read-back follow one another with nothing between them, so that every call begins while the one
+    # before it still writes what it is going to read
+    heads, group, d, blocks = 2, 4, 128, 5
+    rng = np.random.default_rng(71)
+    events = [[700, 3, 0, 64, 17], [16, 41, 900, 1, 33]]
+    need = max(sum(-(-(n + 1) // 16) for n in lens) for lens in events)
+    rows = max(sum(lens) for lens in events)
+    pages = 2 * need
+    ids = rng.permutation(pages).astype(np.int32)
+    cfg = B.cpa_config(heads * group, heads, d, 16, d ** -0.5, 0, 0, 0)
+    dims = B.cpa_table_dims(blocks, 1, pages, need, 0)
+    tables = torch.empty(B.cpa_tables_bytes(cfg, dims), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(B.cpa_decode_q8_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    at = B.cpa_tables_offset(cfg, dims, B.ARR_CU_SEQLENS)
+    cu = tables[at:at + 4 * (blocks + 1)].view(torch.int32)
+    pool = torch.full((pages, heads, 2, 16, d), 0x7F, dtype=torch.uint8, device="cuda")
+    scales = torch.full((pages, heads, 2), float("nan"), device="cuda")
+    turns = 24
+    ins, outs = [], []
+    for i, lens in enumerate(events):
+        k, v, q = (_bf16(x) for x in (_values(rng, rows, heads, d), _values(rng, rows, heads, d), rng.standard_normal((2, blocks, heads * group, d))))
+        k1, v1 = (_bf16(_values(rng, blocks, heads, d)) for _ in range(2))
+        ins.append((_i32(lens), _i32(ids[i * need:(i + 1) * need]), k, v, q, k1, v1))
+    for _ in range(turns):
+        outs.append([torch.full((2, blocks, heads * group, d), 9.0, dtype=torch.bfloat16, device="cuda"),
+                     torch.full((2, rows, heads, d), 9.0, dtype=torch.bfloat16, device="cuda"),
+                     torch.full((2, blocks), -7, dtype=torch.int32, device="cuda")])
+    torch.cuda.synchronize()
+    for t in range(turns):
+        lens, free, (k, _), (v, _), (q, _), (k1, _), (v1, _) = ins[t % 2]
+        o, kv, n = outs[t]
+        rc = [B.cpa_tables_build(cfg, dims, lens, free, need, tables),
+              B.cpa_kv_append_q8(cfg, dims, tables, k, v, cu, rows, None, n[0], pool, scales),
+              B.cpa_decode_q8(cfg, dims, tables, q[0], n[0], None, pool, scales, o[0], ws),
+              B.cpa_decode_append_q8(cfg, dims, tables, q[1], k1, v1, n[0], n[1], None, pool, scales, o[1], ws),
+              B.cpa_kv_read_q8(cfg, dims, tables, None, cu, rows, pool, scales, kv[0], kv[1])]
+        assert rc == [0] * 5
+    assert B.cpa_tables_status(tables) == B.CPA_OK
+    for i, lens in enumerate(events):
+        want = oq.CacheQ8(pages, heads, d, lens, 1, ids[i * need:(i + 1) * need])
+        (_, kf), (_, vf), (_, qf), (_, k1f), (_, v1f) = ins[i][2:]
+        o, kv, n = outs[i]
+        where = np.concatenate([[0], np.cumsum(lens)])
+        scale = float(np.float32(d ** -0.5))
+        for b, m in enumerate(lens):
+            want.append(b, kf[where[b]:where[b] + m], vf[where[b]:where[b] + m])
+            first = want.rows(b, 0, m)
+            exact = want.decode(b, qf[0, b], scale)
+            assert (np.abs(o[0, b].double().cpu().numpy() - exact[0]) <= oq.decode_tolerance(*exact, d)).all(), (i, b)
+            want.append(b, k1f[b:b + 1], v1f[b:b + 1])
+            exact = want.decode(b, qf[1, b], scale)
+            assert (np.abs(o[1, b].double().cpu().numpy() - exact[0]) <= oq.decode_tolerance(*exact, d)).all(), (i, b)
+            # (the read comes behind the step, whose token may have made the last page's scale grow: whole pages only)
+            whole = m // 16 * 16
+            assert np.array_equal(kv[:, where[b]:where[b] + whole].double().cpu().numpy(), first[:, :, :whole].transpose(0, 2, 1, 3))
+        assert n.tolist() == [lens, [m + 1 for m in lens]] and (kv[:, where[-1]:] == 9).all()
+        for t in range(i, turns, 2):
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outs[t], outs[i])), t

@@ -116,3 +116,19 @@ def test_bad_pointers_are_refused():
                 dict(v_out=None), dict(num_rows=-1), dict(d_first=ok + 1), dict(k_out=ok + 8), dict(v_out=ok + 2)):
         assert B.cpa_kv_read_q8(cfg, dims, **dict(base, **bad)) == B.CPA_EINVAL, bad
     assert B.cpa_tables_status(None) == B.CPA_EINVAL
+
+
+def test_programmatic_kernels_read_global_memory_coherently():
+    # a kernel that begins before its predecessor has ended may not load what that one writes through the non-coherent
+    # path, by name or by the compiler's choice
+    import os
+    import re
+    csrc = os.path.join(os.path.dirname(B.__file__), "csrc")
+    for name in os.listdir(csrc):
+        if not name.endswith((".cu", ".cuh")):
+            continue
+        with open(os.path.join(csrc, name)) as f:
+            text = re.sub(r"//[^\n]*", "", f.read())
+        if '"cache_q8.cuh"' in text or name == "cache_q8.cuh":      # (their indexes and lengths are written on the device)
+            assert "__ldg(" not in text and "global.nc" not in text, name
+            assert not re.search(r"const\s+\w+\s*\*\s*__restrict__", text), name
