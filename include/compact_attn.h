@@ -665,8 +665,8 @@ CPA_API int cpa_decode_append_q8(const cpa_config* cfg, const cpa_table_dims* di
  * i < d_cu[b+1] - d_cu[b] (to hand a history on to calls that take bf16 rows).
  *   d_first      : device int32 [B], NULL = 0 everywhere;  d_cu: device int32 [B+1], at most num_rows rows in all
  *   k_out, v_out : device bf16 [num_rows, num_kv_heads, head_dim]; rows behind the last stay as they were
- * A block whose range leaves its pages is left out (status as for the append); that the positions have been written is
- * the caller's contract.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED, CPA_ECUDA.
+ * A block whose range leaves its pages or is bad is left out (status as for the append); a packed row that the ranges of
+ * two blocks share holds the row of either.  That the positions have been written is the caller's contract.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED, CPA_ECUDA.
  */
 CPA_API int cpa_kv_read_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const int32_t* d_first,
                            const int32_t* d_cu, int32_t num_rows, const void* kv_pool, const float* kv_scales,

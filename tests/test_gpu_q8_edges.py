@@ -247,3 +247,48 @@ def test_tables_rebuilt_between_calls_without_a_wait(B):
         assert n.tolist() == [lens, [m + 1 for m in lens]] and (kv[:, where[-1]:] == 9).all()
         for t in range(i, turns, 2):
             assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outs[t], outs[i])), t
+
+
+RANGES = {"far back": [0, 320, 16, 160], "to the start": [0, 1000, 0, 16], "into the one before": [0, 100, 50, 150],
+          "twice": [0, 500, 500, 20, 300, 10, 10, 700], "first not at 0": [64, 100, 37, 37, 90], "past the end": [0, 200, 5000, 100, 260],
+          "negative": [0, 100, -50, 300, 400], "in order": [0, 100, 100, 117, 400]}
+for _seed, _blocks in ((1, 40), (2, 40), (3, 33), (4, 1100)):
+    RANGES[f"{_blocks} at random, {_seed}"] = [int(x) for x in np.random.default_rng(_seed).integers(0, 500, _blocks + 1)]
+_r = [16 * i for i in range(1101)]
+_r[600], _r[17], _r[1000] = 40, 17600, 0
+RANGES["few of many"] = _r
+
+
+@pytest.mark.parametrize("name", list(RANGES))
+def test_a_bad_range_costs_no_other_block_its_rows(B, name):
+    cu = RANGES[name]
+    rows = max(1000, max(x for x in cu if x < 5000)) if "past" in name else max(max(cu), 1)
+    blocks, d, heads = len(cu) - 1, 64, 1
+    n = [b - a for a, b in zip(cu, cu[1:])]
+    good = [b for b in range(blocks) if n[b] >= 0 and cu[b] >= 0 and cu[b + 1] <= rows]
+    c = Cache(B, [5 + (n[b] if b in set(good) else 0) for b in range(blocks)], 0, heads, d, 1)
+    rng = np.random.default_rng(61)
+    c.append(_values(rng, 5 * blocks, heads, d), _values(rng, 5 * blocks, heads, d), [5] * blocks)
+    (kd, kf), (vd, vf) = (_bf16(_values(rng, rows, heads, d)) for _ in range(2))
+    out = torch.full_like(c.lens, -7)
+    assert B.cpa_kv_append_q8(c.cfg, c.dims, c.tables, kd, vd, _i32(cu), rows, c.lens, out, c.pool, c.scales) == 0
+    assert c.status() == (B.CPA_OK if len(good) == blocks else B.CPA_EINVAL)
+    for b in good:
+        c.want.append(b, kf[cu[b]:cu[b + 1]], vf[cu[b]:cu[b + 1]])
+    c.lens = out
+    c.check_pool()                       # every good block has its rows and its length, every other one what it had
+    # the same ranges read back; a row that two blocks' ranges share may hold either's
+    first = [5 if b in set(good) else 0 for b in range(blocks)]
+    k_out, v_out = (torch.full((rows + 2, heads, d), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert B.cpa_kv_read_q8(c.cfg, c.dims, c.tables, _i32(first), _i32(cu), rows, c.pool, c.scales, k_out, v_out) == 0
+    owners = np.zeros(rows + 2, dtype=int)
+    for b in good:
+        owners[cu[b]:cu[b + 1]] += 1
+    got = [t.double().cpu().numpy() for t in (k_out, v_out)]
+    for b in good:
+        want = c.want.rows(b, 5, 5 + n[b])
+        alone = np.flatnonzero(owners[cu[b]:cu[b + 1]] == 1)
+        for i in range(2):
+            assert np.array_equal(got[i][cu[b] + alone], want[i].transpose(1, 0, 2)[alone]), b
+    for i in range(2):
+        assert (got[i][owners == 0] == 9).all() and (got[i][owners > 0] != 9).any(axis=(1, 2)).all()
