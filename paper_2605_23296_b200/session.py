@@ -166,15 +166,23 @@ class CompactionSession:
 
     def read_cache(self, first: Sequence[int], counts: Sequence[int]):
         """K and V rows [sum(counts), Hkv, d] in bf16 of positions first[b] .. first[b] + counts[b] of every block of an
-        8-bit cache (to hand a history on to calls that take bf16 rows)."""
+        8-bit cache (to hand a history on to calls that take bf16 rows).  The range has to lie in the block's pages;
+        positions behind the block's tokens (`lens`, which live on the device and are not looked at here) have no
+        defined value."""
         self._only(8, "read_cache")
-        if len(counts) != self.B or len(first) != self.B or min(counts) < 0 or min(first) < 0:
-            raise ValueError(f"first and counts: {self.B} numbers each, none negative")
+        first, counts = np.asarray(first), np.asarray(counts)
+        if any(a.shape != (self.B,) or a.dtype.kind not in "iu" or (a < 0).any() or (a > 2 ** 31).any() for a in (first, counts)):
+            raise ValueError(f"first and counts: {self.B} whole numbers each, none negative or beyond int32")
+        first, counts = first.astype(np.int64), counts.astype(np.int64)
+        room = (self.block_lens.astype(np.int64) + self.dims.max_new_tokens + self.P - 1) // self.P * self.P
+        if (first > room).any() or (counts > room - first).any():
+            b = int(np.argmax((first > room) | (counts > room - first)))
+            raise ValueError(f"block {b}: {counts[b]} positions from {first[b]} on leave its pages, which hold {room[b]}")
         cu = torch.as_tensor(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32), device=self.device)
-        rows = int(np.sum(counts))
+        rows = int(counts.sum())
         k, v = (torch.empty((rows, self.Hkv, self.d), dtype=torch.bfloat16, device=self.device) for _ in range(2))
-        self._q8("cpa_kv_read_q8", torch.as_tensor(np.asarray(first, dtype=np.int32), device=self.device), cu, rows,
-                 self.kv_pool, self.kv_scales, k, v)
+        self._q8("cpa_kv_read_q8", torch.as_tensor(first.astype(np.int32), device=self.device), cu, rows, self.kv_pool,
+                 self.kv_scales, k, v)
         return k, v
 
     def _only(self, bits: int, what: str) -> None:

@@ -113,3 +113,21 @@ def test_refusals():
     with pytest.raises(B.CpaError):
         s.decode(good_q, active=torch.ones(2, dtype=torch.int32, device="cuda"))
     s.close()
+
+
+def test_read_back_refuses_ranges_outside_the_blocks_pages():
+    from paper_2605_23296_b200.session import CompactionSession
+
+    s = CompactionSession([30, 4], 2, 8, 2, 64, np.arange(8), 8, kv_bits=8, poison_pools=True)     # pages for 32 and 16 tokens
+    rows = torch.ones(34, 2, 64, dtype=torch.bfloat16, device="cuda")
+    s.append(rows, rows, [30, 4])
+    for first, counts in (([0, 0], [33, 1]), ([0, 0], [1, 17]), ([31, 0], [2, 0]), ([33, 0], [0, 0]), ([0, 17], [1, 0]),
+                          ([0, -1], [1, 1]), ([0, 0], [1, -1]), ([2 ** 40, 0], [1, 1]), ([0, 0], [2 ** 40, 1]),
+                          ([2 ** 62, 0], [2 ** 62, 0]), ([0], [1, 1]), ([0, 0], [1]), ([0.0, 0.0], [1, 1])):
+        with pytest.raises(ValueError):
+            s.read_cache(first, counts)
+    for first, counts in (([0, 0], [30, 4]), ([29, 3], [1, 1]), ([30, 4], [0, 0]), (np.array([7, 0]), torch.tensor([3, 4]))):
+        k, v = s.read_cache(first, counts)
+        assert k.shape == v.shape == (int(sum(counts)), 2, 64) and (k == 1).all() and (v == 1).all()
+    assert s.read_cache([32, 16], [0, 0])[0].shape[0] == 0 and s.status() == 0
+    s.close()
