@@ -270,10 +270,13 @@ class CompactionSession:
 
     def decode_append_steps(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """q/out [n,B,Hq,d], k_new/v_new [n,B,Hkv,d]: n consecutive fused decode steps enqueued by one call."""
+        """q/out [n,B,Hq,d], k_new/v_new [n,B,Hkv,d]: n consecutive fused decode steps (enqueued by one call of the library
+        for the bf16 cache, by one call per step for the 8-bit cache)."""
         if out is None:
             out = torch.empty_like(q)
         if self.kv_bits == 8:
+            if not q.shape[0] == k_new.shape[0] == v_new.shape[0] == out.shape[0]:
+                raise ValueError(f"steps: {q.shape[0]} of q, {k_new.shape[0]} of k_new, {v_new.shape[0]} of v_new, {out.shape[0]} of out")
             for t in range(q.shape[0]):
                 self._decode_q8(q[t], k_new[t], v_new[t], None, out[t])
             return out

@@ -131,3 +131,17 @@ def test_read_back_refuses_ranges_outside_the_blocks_pages():
         assert k.shape == v.shape == (int(sum(counts)), 2, 64) and (k == 1).all() and (v == 1).all()
     assert s.read_cache([32, 16], [0, 0])[0].shape[0] == 0 and s.status() == 0
     s.close()
+
+
+def test_steps_of_different_counts_are_refused_before_any_is_taken():
+    from paper_2605_23296_b200.session import CompactionSession
+
+    s = CompactionSession([30, 4], 4, 8, 2, 64, np.arange(8), 8, kv_bits=8)
+    q, k = (torch.zeros(3, 2, h, 64, dtype=torch.bfloat16, device="cuda") for h in (8, 2))
+    for args in ((q, k[:2], k), (q, k, k[:1]), (q[:2], k, k), (q, k, k, torch.empty_like(q)[:2])):
+        with pytest.raises(ValueError):
+            s.decode_append_steps(*args)
+    assert s.lens.tolist() == [0, 0]
+    s.decode_append_steps(q, k, k)
+    assert s.lens.tolist() == [3, 3] and s.status() == 0
+    s.close()
