@@ -639,8 +639,11 @@ CPA_API int64_t cpa_decode_q8_workspace_bytes(const cpa_config* cfg);
  *   d_lens      : device int32 [B]; 0 gives a row of zeros
  *   d_active    : device int32 [B] or NULL = all; a block with flag 0 sits out, its rows of o are not written
  *   d_workspace : device scratch, cpa_decode_q8_workspace_bytes, 16-byte aligned, needs no initialisation
- * A block whose length is negative or beyond its pages sits out too (status CPA_EINVAL, CPA_ENOSPC).  Errors:
- * CPA_EINVAL, CPA_EUNSUPPORTED, CPA_ECUDA.
+ * A block whose length is negative or beyond its pages sits out too (status CPA_EINVAL, CPA_ENOSPC).
+ * Precision: scores, sums and the softmax's denominator are held in fp32, weights and queries in f16.  A weight, which
+ * carries V's scale, is off by 2^-11 of itself and 2^-31 of the largest weight * scale of its head at most, so tokens
+ * below 2^-31 of that add nothing; a query element is off by 2^-32 of its row's largest at most.  Scores are taken within
+ * fp32's range: beyond it they count as infinities.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED, CPA_ECUDA.
  */
 CPA_API int cpa_decode_q8(const cpa_config* cfg, const cpa_table_dims* dims, void* d_tables, const void* q,
                           const int32_t* d_lens, const int32_t* d_active, const void* kv_pool, const float* kv_scales,

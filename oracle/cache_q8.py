@@ -107,13 +107,36 @@ class CacheQ8:
         shaken = scale * (np.abs(qh) @ np.abs(k).transpose(0, 2, 1)).max(2)
         return (w @ v).reshape(-1, d), (w @ np.abs(v)).reshape(-1, d), shaken.reshape(-1, 1)
 
+    def floors(self, b, q, scale):
+        """(score_floor, weight_floor) for q over the block's tokens: what a kernel may be off on top of decode_tolerance's
+        relative terms if it holds queries and weights in f16.
 
-def decode_tolerance(o, spread, shaken, d):
+        Queries: scaled by a power of two so that the row's largest magnitude is at least 2^7; an element then is off by
+        half of f16's smallest step, 2^-25, at most, which is 2^-32 of the row's largest, times |k| in the score.
+        Weights: with V's scale and with 2^6 at the largest p_j * scale_j that the sum has met, off by 2^-25 at most where
+        they are subnormal: 2^-31 max_j(p_j scale_j) in all, times |code| in the sum."""
+        n, (heads, d) = int(self.lens[b]), (self.codes.shape[1], self.codes.shape[-1])
+        qh = np.asarray(q, dtype=np.float64).reshape(heads, -1, d)
+        k, _ = self.rows(b, 0, n)
+        pages = [self.page_of(b, i) for i in range(n)]
+        codes = np.stack([self.codes[p, :, 1, i % P] for i, p in enumerate(pages)], 1)       # [heads, n, d]
+        vs = np.stack([self.scales[p, :, 1] for p in pages], 1)                              # [heads, n]
+        s = scale * (qh @ k.transpose(0, 2, 1))
+        w = np.exp(s - s.max(2, keepdims=True))
+        w /= w.sum(2, keepdims=True)
+        top = (w * vs[:, None]).max(2)                                                       # [heads, group]
+        weight = 2.0 ** -31 * top[..., None] * np.abs(codes).sum(1)[:, None]
+        score = 2.0 ** -32 * scale * np.abs(qh).max(2) * np.abs(k).sum(2).max(1)[:, None]
+        return score.reshape(-1, 1), weight.reshape(-1, d)
+
+
+def decode_tolerance(o, spread, shaken, d, score_floor=0.0, weight_floor=0.0):
     """How far a decode kernel with bf16 output, 32-bit sums and 11-bit weights may be off, element by element.
 
     bf16 output: half a step, 2^-8 |o|.  Weights rounded to f16: 2^-11 of each term.  A score is a sum of d products in
     32 bits, off by at most d 2^-24 of the sum of magnitudes, and its scaling and shift before the exponential add a few
     2^-24 of the score: its error e enters numerator and denominator, 2 e of each term.  The exponential itself and the
-    32-bit sums and joins of the partials: 2^-18 of each term."""
-    e = (d + 8) * 2.0 ** -24 * shaken
-    return 2.0 ** -8 * np.abs(o) + (2.0 ** -11 + 2 * e + 2.0 ** -18) * spread + 2.0 ** -133
+    32-bit sums and joins of the partials: 2^-18 of each term.  The floors are those of CacheQ8.floors, for inputs whose
+    large values do not meet the dimension looked at."""
+    e = (d + 8) * 2.0 ** -24 * shaken + score_floor
+    return 2.0 ** -8 * np.abs(o) + (2.0 ** -11 + 2 * e + 2.0 ** -18) * spread + weight_floor + 2.0 ** -133

@@ -6,7 +6,7 @@
 // of one kv head (16 tokens, 4 KB at head_dim 128) every 90 ns, so the arithmetic per page has to stay below that:
 //   - codes go to the warp-level MMA (m16n8k16, f16 in, fp32 sums) as f16, which holds an e4m3 value exactly; the page
 //     scale of K multiplies the finished score.  The queries are made f16 by a power of two per head, exactly but for
-//     elements 2^-22 of the row's largest.  (The tensor cores of the fifth generation would take the codes as they are,
+//     elements below 2^-22 of the row's largest, which are off by 2^-32 of it at most.  (The tensor cores of the fifth generation would take the codes as they are,
 //     but want 128 rows of one operand and an 8-bit other one: at most 8 query heads share a page, and rounding
 //     queries and weights to 8 bits costs more than the cache's own rounding.)
 //   - keys are the M side of both products: S^T[16 keys x 8 heads] = K Q^T, O^T[dims x 8 heads] += V^T P^T, so that up to
@@ -18,8 +18,11 @@
 //     that both read patterns touch every bank once (key_of_row).
 //   - the running maxima are raised only when a score passes them by 2^9: weights have headroom in f16, and the
 //     reduction over the lanes and the rescaling of the accumulators are rare.
-// Weights carry V's page scale into f16, w_j = 2^(s_j + log2 vs - m_o), with a maximum m_o of their own, so that pages
-// whose scales lie far apart neither overflow nor vanish; the denominator keeps the plain maximum m_l.
+// Weights carry V's page scale into f16, w_j = 2^(6 + s_j + log2 vs - m_o), with a maximum m_o of their own, so that large
+// scales do not overflow and what small ones lose is small beside what large ones add: a weight below 2^-20 of the largest
+// loses bits, one below 2^-31 is zero, 2^-31 of the largest is the most that any is off.  (A dimension in which all that
+// is large holds zeros shows it.  Weights in more bits would want a product and an accumulation per page: by count 60
+// instructions on top of 270, and 32 registers that are not there; not built.)  The denominator keeps the plain maximum m_l, in fp32.
 //
 // Work: the (block, kv head, page) triples of all blocks are laid end to end and cut into ranges from the lengths on the
 // device: one equal range per CTA of the one wave.  (Handing the last sixth out in small ranges as CTAs finish was slower,

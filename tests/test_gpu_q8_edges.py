@@ -292,3 +292,70 @@ def test_a_bad_range_costs_no_other_block_its_rows(B, name):
             assert np.array_equal(got[i][cu[b] + alone], want[i].transpose(1, 0, 2)[alone]), b
     for i in range(2):
         assert (got[i][owners == 0] == 9).all() and (got[i][owners > 0] != 9).any(axis=(1, 2)).all()
+
+
+def _check_with_floors(c, o, qf, what):
+    for b in range(len(c.lens0)):
+        want = c.want.decode(b, qf[b], c.scale)
+        tol = oq.decode_tolerance(*want, c.d, *c.want.floors(b, qf[b], c.scale))
+        off = np.abs(o[b].double().cpu().numpy() - want[0])
+        assert (off <= tol).all(), f"{what}: off {off.max():.3g}, {(off / tol).max():.2f} of the bound"
+    return want[0]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gap", [4, 12, 16, 20, 24, 32, 60])
+def test_small_scales_beside_large_ones_in_other_dimensions(B, d, gap):
+    # page 0 of each round holds 2^gap in dimension 0 alone, the others 1 in dimension 1 alone, at equal scores: dimension 1
+    # is what the small scales add.  Up to 2^20 no weight is subnormal (the scales lie 2^gap apart), and nothing is lost
+    c = Cache(B, [320], 0, 1, d, 2)
+    rng = np.random.default_rng(81)
+    v = np.zeros((320, 1, d))
+    large = np.arange(320) // 16 % 4 == 0
+    v[large, 0, 0], v[~large, 0, 1] = 2.0 ** gap, 1.0
+    c.append(np.zeros((320, 1, d)), v, [320])
+    o, qf = c.decode(rng.standard_normal((1, 2, d)))
+    want = _check_with_floors(c, o, qf, gap)
+    if gap <= 20:
+        assert (np.abs(o[0, :, 1].double().cpu().numpy() / want[:, 1] - 1) <= 2.0 ** -8 + 2.0 ** -10).all()
+    # all 320 tokens small but the page of one warp: the others do not share its maximum
+    c = Cache(B, [320], 0, 1, d, 2, num_sms=1)
+    v = rng.standard_normal((320, 1, d))
+    v[:16] = 0.0
+    v[:16, 0, 0] = 2.0 ** gap
+    c.append(rng.standard_normal((320, 1, d)), v, [320])
+    o, qf = c.decode(rng.standard_normal((1, 2, d)))
+    _check_with_floors(c, o, qf, gap)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gap", [4, 12, 18, 22, 28, 34, 60])
+def test_small_weights_beside_a_large_one_in_other_dimensions(B, d, gap):
+    # one key outweighs every other by 2^gap and has values in dimension 0 alone
+    for at in (0, 17, 200, 319):
+        c = Cache(B, [320], 0, 1, d, 1, scale=float(np.log(2)))
+        rng = np.random.default_rng(82)
+        k, v = np.zeros((320, 1, d)), rng.standard_normal((320, 1, d))
+        k[at, 0, 0] = gap
+        v[:, 0, 0], v[at] = 0.0, 0.0
+        v[at, 0, 0] = 1.0
+        c.append(k, v, [320])
+        q = np.zeros((1, 1, d))
+        q[0, 0, 0] = 1.0
+        o, qf = c.decode(q)
+        _check_with_floors(c, o, qf, (gap, at))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gap", [10, 18, 22, 24, 26, 30, 34])
+def test_small_query_elements_beside_a_large_one(B, d, gap):
+    # the row's largest element meets keys of zeros: the scores come from elements 2^gap below it
+    c = Cache(B, [150, 33], 0, 1, d, 2, scale=1.0)
+    rng = np.random.default_rng(83)
+    k = rng.standard_normal((183, 1, d)) * 2.0 ** (gap - 4)
+    k[:, 0, 0] = 0.0
+    c.append(k, rng.standard_normal((183, 1, d)), [150, 33])
+    q = rng.standard_normal((2, 2, d)) * 2.0 ** -gap
+    q[:, :, 0] = 1.5
+    o, qf = c.decode(q)
+    _check_with_floors(c, o, qf, gap)
