@@ -22,7 +22,8 @@
 // scales do not overflow and what small ones lose is small beside what large ones add: a weight below 2^-20 of the largest
 // loses bits, one below 2^-31 is zero, 2^-31 of the largest is the most that any is off.  (A dimension in which all that
 // is large holds zeros shows it.  Weights in more bits would want a product and an accumulation per page: by count 60
-// instructions on top of 270, and 32 registers that are not there; not built.)  The denominator keeps the plain maximum m_l, in fp32.
+// instructions on top of 270, and 32 registers that are not there; not built.)  The denominator keeps the plain maximum
+// m_l, in fp32.
 //
 // Work: the (block, kv head, page) triples of all blocks are laid end to end and cut into ranges from the lengths on the
 // device: one equal range per CTA of the one wave.  (Handing the last sixth out in small ranges as CTAs finish was slower,
@@ -35,7 +36,7 @@
 // and the merger that arrives last (a counter in the tables) joins them in the order of the ranges.
 //
 // Measured (one wave of 2 x 148 CTAs): 32 blocks of 1024 .. 8192 tokens, 32 heads over 8 of 128, 337 MB: 60 us, of which
-// the stream 48 us (7.0 TB/s) and start and merge the rest; one block of 131072: 51 us; 192 blocks of 512 .. 1024 with
+// the stream 48 us (7.0 TB/s) and start and merge the rest; one block of 131072: 50 us; 192 blocks of 512 .. 1024 with
 // their append: 58 us; 16 blocks of 8192, 64 heads over 8 of 64, with append, 133 MB: 32 us; 4 blocks of 96 .. 288: 8 us.
 #include <algorithm>
 #include <atomic>
@@ -66,7 +67,9 @@ struct Q8Shape {
     static constexpr int TP = D == 128 ? 2 : 4;       // pages per consumer warp and round
     static constexpr int kRound = kCons * TP;         // pages of a round
     // What starting and ending a (block, kv head) costs, in pages: the cut counts it, so that CTAs with many short blocks
-    // get fewer pages (192 short sequences: 62.5 us without, 59.8 at 10, 57.4 at 12, 58.1 at 20).
+    // get fewer pages (192 short sequences: 62.5 us without, 59.8 at 10, 57.4 at 12, 58.1 at 20; at head_dim 64, 16 blocks
+    // of 8192 with 8 kv heads: 33.5 at 6, 31.9 at 12, 31.5 at 18 and 24, and 16 blocks of 96 .. 288: 12.4 at 6, 8.9 from
+    // 12 to 24, 9.4 at 30).
     static constexpr int kUnitCost = D == 128 ? 12 : 18;
     static constexpr int kPageBytes = 2 * kPage * D;  // K and V codes of a (page, kv head)
     static constexpr int kData = kRound * kPageBytes;
@@ -953,6 +956,9 @@ int launch_q8(const cpa_config* cfg, const cpa_table_dims* dims, q8_args& a, cud
     if (fn(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, a.pool, size, stride, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return CPA_ECUDA;
+    // Cells of a range at least.  Short blocks want many ranges, though a round would hold them whole: 4 blocks of 96 .. 288
+    // tokens, one kv head of 64, take 7.8 us at 8 and at 16, 9.3 at 24, 9.6 at 40; 16 such blocks, 8 kv heads of 128, 9.4,
+    // 12.5, 11.8 and 12.5.  (One block of one such head alone would have 24: 6.1 us for 7.3.)
     a.min_quota = 8;
     a.slots = partial_slots(cfg);
     a.list_len = dims->page_capacity;

@@ -359,3 +359,67 @@ def test_small_query_elements_beside_a_large_one(B, d, gap):
     q[:, :, 0] = 1.5
     o, qf = c.decode(q)
     _check_with_floors(c, o, qf, gap)
+
+
+def test_a_capture_with_copies_and_a_second_stream(B):
+    # copies in front of the calls, a fork to another stream and a join: programmatic launches behind nodes of every kind
+    rng = np.random.default_rng(91)
+    lens = [200, 33]
+    caches = []
+    for i in range(2):
+        c = Cache(B, lens, 8, 2, 64, seed=i)
+        c.append(*(_values(rng, sum(lens), 2, 64) for _ in range(2)), lens)
+        caches.append(c)
+    src = [torch.zeros(2, h, 64, dtype=torch.bfloat16, device="cuda") for h in (8, 2, 2)]
+    buf = [torch.zeros_like(t) for t in src]
+    new = [torch.zeros_like(c.lens) for c in caches]
+    o = [torch.zeros(2, 2, 8, 64, dtype=torch.bfloat16, device="cuda") for _ in caches]
+    total = torch.zeros(2, 8, 64, device="cuda")
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def step(i, on):
+        c = caches[i]
+        assert B.cpa_decode_append_q8(c.cfg, c.dims, c.tables, *buf, c.lens, new[i], None, c.pool, c.scales, o[i][0], c.ws, on.cuda_stream) == 0
+
+    def decode(i, on):
+        c = caches[i]
+        assert B.cpa_decode_q8(c.cfg, c.dims, c.tables, buf[0], new[i], None, c.pool, c.scales, o[i][1], c.ws, on.cuda_stream) == 0
+
+    def both():
+        for a, b in zip(buf, src):
+            a.copy_(b)
+        step(0, main)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            step(1, side)
+            caches[1].lens.copy_(new[1])
+        decode(0, main)
+        caches[0].lens.copy_(new[0])
+        main.wait_stream(side)
+        decode(1, main)
+        total.copy_(o[0][1].float() + o[1][1].float())
+
+    torch.cuda.synchronize()
+    keep = [(c.pool.clone(), c.scales.clone(), c.lens.clone()) for c in caches]
+    with torch.cuda.stream(main):
+        both()
+    torch.cuda.synchronize()
+    for c, (pool, scales, n) in zip(caches, keep):
+        c.pool.copy_(pool), c.scales.copy_(scales), c.lens.copy_(n)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=main):
+        both()
+    for r in range(4):
+        vals = [_bf16(x) for x in (rng.standard_normal((2, 8, 64)), _values(rng, 2, 2, 64), _values(rng, 2, 2, 64))]
+        for t, (x, _) in zip(src, vals):
+            t.copy_(x)
+        graph.replay()
+        for i, c in enumerate(caches):
+            for b in range(2):
+                c.want.append(b, vals[1][1][b:b + 1], vals[2][1][b:b + 1])
+            c.check_rows(o[i][0], vals[0][1], what=f"replay {r} step {i}")
+            assert torch.equal(o[i][0], o[i][1])
+            c.check_pool(f"replay {r} cache {i}")
+        assert torch.equal(total, o[0][1].float() + o[1][1].float())
+    assert all(c.status() == B.CPA_OK for c in caches)

@@ -145,3 +145,37 @@ def test_steps_of_different_counts_are_refused_before_any_is_taken():
     s.decode_append_steps(q, k, k)
     assert s.lens.tolist() == [3, 3] and s.status() == 0
     s.close()
+
+
+def test_an_event_in_8_bits_beside_one_in_bf16_on_one_stream():
+    # the two caches' steps alternate without a wait: both kinds of launch begin before the other kind has ended
+    from paper_2605_23296_b200.session import CompactionSession, bits_to_tensor
+
+    T, hq, hkv, d = 10, 16, 2, 128
+    w = wl.custom([300, 17, 64, 900], hq, hkv, d, steps=T, seed=5).materialise()
+    dev = lambda a: bits_to_tensor(a, "cuda:0")
+    k, v, q_dec, k_dec, v_dec = (dev(a) for a in (w.k, w.v, w.q_dec, w.k_dec, w.v_dec))
+
+    def run(kinds):
+        s = [CompactionSession(w.block_lens, T, hq, hkv, d, w.free_pages, w.num_pages, scale=w.scale, kv_bits=bits) for bits in kinds]
+        out = [torch.zeros(T, 4, hq, d, dtype=torch.bfloat16, device="cuda") for _ in s]
+        for x in s:
+            x.append_prefill(k, v)
+        for t in range(T):
+            for x, o in zip(s, out):
+                if t % 2:
+                    x.append(k_dec[t], v_dec[t])
+            for x, o in zip(s, out):
+                if t % 2:
+                    x.decode(q_dec[t], o[t])
+                else:
+                    x.decode_append(q_dec[t], k_dec[t], v_dec[t], o[t])
+        assert all(x.status() == 0 for x in s)
+        for x in s:
+            x.close()
+        return out
+
+    alone = [run([bits])[0] for bits in (8, 16)]
+    for kinds in ((8, 16), (16, 8), (16, 8, 16, 8)):
+        for bits, o in zip(kinds, run(kinds)):
+            assert torch.equal(o, alone[0 if bits == 8 else 1]), (kinds, bits)
