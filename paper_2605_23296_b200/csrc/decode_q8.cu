@@ -6,9 +6,10 @@
 // of one kv head (16 tokens, 4 KB at head_dim 128) every 90 ns, so the arithmetic per page has to stay below that:
 //   - codes go to the warp-level MMA (m16n8k16, f16 in, fp32 sums) as f16, which holds an e4m3 value exactly; the page
 //     scale of K multiplies the finished score.  The queries are made f16 by a power of two per head, exactly but for
-//     elements below 2^-22 of the row's largest, which are off by 2^-32 of it at most.  (The tensor cores of the fifth generation would take the codes as they are,
-//     but want 128 rows of one operand and an 8-bit other one: at most 8 query heads share a page, and rounding
-//     queries and weights to 8 bits costs more than the cache's own rounding.)
+//     elements below 2^-22 of the row's largest, which are off by 2^-32 of it at most.  (The tensor cores of the fifth
+//     generation would take the codes as they are, with the keys of eight pages as their 128 rows, a query as the sum of
+//     two 8-bit parts and a weight of 11 bits as that of three.  Not built: the stream of pages already runs at the
+//     memory's rate, and what is left over it, start and join, is not in the products.)
 //   - keys are the M side of both products: S^T[16 keys x 8 heads] = K Q^T, O^T[dims x 8 heads] += V^T P^T, so that up to
 //     8 heads fill the N side and no row is wasted.  S^T comes out with keys along the lanes, P^T is wanted with keys
 //     along the registers: one 8x8 transpose (movmatrix) per eight keys.

@@ -33,7 +33,13 @@ class CompactionSession:
     decode workspace.  All calls are enqueued on the current torch stream of
     `device` unless a stream is given.  With kv_bits = 8 the cache holds e4m3 codes with a scale per page, head and K or
     V (half the bytes of a decode step, twice the tokens in a pool of given size); append, decode, decode_append and
-    append_prefill are then the calls of that cache, and lengths live on the device (`lens`).
+    append_prefill are then the calls of that cache, and lengths live on the device.  What differs from the bf16 cache:
+      - `lens` is another tensor after every append and every fused step, and the one before is overwritten by the next:
+        read it anew, and let a captured graph that is replayed as a loop hold an even number of such calls;
+      - a block without room for its rows is left out and its length stays; status() says so (CPA_ENOSPC), where the bf16
+        cache's call raises;
+      - the decode's split is made on the device, pages_per_split is not used;
+      - decode_append_steps makes one call per step.
     """
 
     def __init__(self, block_lens: Sequence[int], max_new_tokens: int, num_q_heads: int,
