@@ -676,6 +676,187 @@ CPA_API int cpa_kv_read_q8(const cpa_config* cfg, const cpa_table_dims* dims, vo
                            const int32_t* d_cu, int32_t num_rows, const void* kv_pool, const float* kv_scales,
                            void* k_out, void* v_out, void* stream);
 
+/*
+ * Rotary positions.  A head's rotated part of R elements is R/2 pairs; pair i of a token at position p is turned by the
+ * angle p * f_i,
+ *     (u, v) -> (u cos a - v sin a, v cos a + u sin a),      a = p * f_i,   f_i = base^(-2 i / R) before scaling.
+ * The paper says nothing about positions; the attention calls above take queries and keys that carry theirs.
+ */
+enum { CPA_ROPE_HALF = 0,           /* pair i = elements i and i + R/2 of the rotated part */
+       CPA_ROPE_INTERLEAVED = 1 };  /* pair i = elements 2 i and 2 i + 1 */
+enum {
+    CPA_ROPE_UNSCALED = 0,
+    CPA_ROPE_SCALED_ALL = 1,    /* f_i / factor: positions pressed together */
+    CPA_ROPE_SCALED_BASE = 2,   /* base * factor^(R / (R - 2)) in place of base: the slowest pair is divided by the factor, the
+                                   fastest is not (R > 2) */
+    CPA_ROPE_SCALED_PARTS = 3,  /* f_i / factor for pairs from the one on that turns `slow` times over trained_len positions,
+                                   f_i up to the one that turns `fast` times, blended linearly in i in between: with
+                                   i(t) = R ln(trained_len / (2 pi t)) / (2 ln base), from max(floor(i(fast)), 0) to
+                                   min(ceil(i(slow)), R - 1) (base > 1) */
+    CPA_ROPE_SCALED_WAVES = 4   /* the same, blended linearly in the number of turns trained_len * f_i / (2 pi) itself: f_i / factor
+                                   up to `slow` turns, f_i from `fast` turns on */
+};
+typedef struct cpa_rope_config {
+    int32_t rope_dim;    /* R: even, 2 .. 256 */
+    int32_t layout;      /* CPA_ROPE_HALF, CPA_ROPE_INTERLEAVED */
+    int32_t scaling;     /* one of the above; the fields below base that it does not name are not looked at */
+    int32_t trained_len; /* positions that the unscaled frequencies were trained over, >= 1 */
+    double  base;        /* > 0, at most 1e30 */
+    double  factor;      /* > 0, at most 1e6 */
+    double  fast, slow;  /* turns, 0 < slow < fast <= 1e9 */
+    double  amplitude;   /* multiplies sines and cosines; 1 for none (0 < amplitude <= 1e4) */
+} cpa_rope_config;
+
+/*
+ * cpa_rope_turns -- the frequencies of a configuration, host arithmetic only: turns[i], i < R/2, is f_i / (2 pi) without its
+ * whole turns as a binary fraction of 64 bits.  The caller copies them to the device once.  (Position times fraction modulo
+ * 2^64 is the angle of any int32 position, reduced exactly; the fraction is off by 2^-64 turns at most.)
+ * Errors: CPA_EINVAL.
+ */
+CPA_API int cpa_rope_turns(const cpa_rope_config* cfg, uint64_t* turns);
+
+/* Rows of heads that cpa_rope turns: element e of head h of row r is x[r * x_row_stride + h * x_head_stride + e]. */
+typedef struct cpa_rope_rows {
+    const void* x;                           /* device bf16 */
+    void* out;                               /* device bf16, apart from x, or x itself with the same strides (in place) */
+    int64_t x_row_stride, x_head_stride;     /* in elements */
+    int64_t out_row_stride, out_head_stride; /* heads of out must not share elements */
+    int32_t heads, head_dim;
+    int32_t offset;                          /* the rotated part is elements offset .. offset + R of a head; the others are
+                                                copied where out is not x */
+} cpa_rope_rows;
+
+/*
+ * cpa_rope -- turn the query rows q and the key rows k (NULL = none) of num_rows tokens to their positions, in one launch.
+ *   d_turns     : device uint64 [R/2], from cpa_rope_turns of the same configuration
+ *   d_positions : device int32 [num_rows]; negative ones turn the other way
+ *   inverse     : 0, or 1 to turn back by the same angles (and amplitude)
+ * Angles are exact to 2^-32 turns, products in fp32, outputs rounded once.  16-byte aligned tensors with strides, offset and
+ * head_dim of whole 8 elements and R of whole 16 (interleaved: 8) move in 16-byte pieces, others by element.  A tensor of no
+ * heads and a call of no rows do nothing.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED (more than 2^24 elements a row), CPA_ECUDA.
+ */
+CPA_API int cpa_rope(const cpa_rope_config* cfg, const uint64_t* d_turns, const int32_t* d_positions, int32_t num_rows,
+                     const cpa_rope_rows* q, const cpa_rope_rows* k, int inverse, void* stream);
+
+/*
+ * Latent attention: keys and values of all heads come from one row per token, [c | r] with a latent vector c of latent_dim
+ * elements and a positional key r of 64.  With a head's up projections U_h [nope_dim, latent_dim] and W_h [v_dim, latent_dim],
+ * its key is [U_h c | r] and its value W_h c.  Two forms of the same attention:
+ *   expanded  keys and values are multiplied out by the caller; for prompts, where every key meets many queries
+ *             (cpa_latent_prefill)
+ *   absorbed  the query is taken to the latent side instead, q_c = U_h^T q_nope, and the output comes back as
+ *             sum_j p_j c_j, which the caller multiplies with W_h; for decode, which then reads one row of latent_dim + 64
+ *             elements per token for all heads (cpa_latent_decode, cpa_latent_step)
+ * The paper says nothing about it; everything below is this library's own.
+ *
+ * The cache: pool is device bf16 [num_pages, 16, latent_dim + 64], 16-byte aligned, rows in order.  Its tables are those of
+ * cpa_tables_build, with the cpa_config that cpa_latent_tables_config gives (cpa_tables_bytes, cpa_tables_offset,
+ * cpa_tables_build, cpa_tables_status); lengths live on the device, no call reads them back, and every launch depends on its
+ * arguments alone, so that a sequence of calls can be captured into a CUDA graph.  Slots behind a block's length may hold
+ * anything.
+ *
+ * Streams: as for the 8-bit cache: calls on the same tables must not overlap on the device, nor calls on the same workspace.
+ */
+typedef struct cpa_latent_config {
+    int32_t num_heads;   /* query heads, 1 .. 128 */
+    int32_t latent_dim;  /* 128, 256, 384, 512 */
+    int32_t rope_dim;    /* 64 */
+    int32_t nope_dim;    /* expanded form: elements of a head's key without position, 128 */
+    int32_t v_dim;       /* expanded form: elements of a head's value, 128 */
+    int32_t page_size;   /* 16 */
+    float   scale;       /* softmax scale, normally 1 / sqrt(nope_dim + rope_dim) */
+    float   norm_eps;    /* added to the mean square of a new latent part, >= 0 */
+    int32_t num_sms;     /* SMs a launch of the decode may fill, 0 = all; at most 4095 */
+} cpa_latent_config;
+
+/* The cpa_config that the calls on the tables of a latent cache take.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
+CPA_API int cpa_latent_tables_config(const cpa_latent_config* cfg, cpa_config* out);
+
+/* The cpa_config that the plan of a cpa_latent_prefill is created with.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
+CPA_API int cpa_latent_plan_config(const cpa_latent_config* cfg, cpa_config* out);
+
+/*
+ * cpa_latent_append -- new rows x = [latent part | positional part] into the blocks' pages, behind the tokens that they have:
+ *     c = x_c / sqrt(mean(x_c^2) + norm_eps) * weight,      r = x_r turned to position first[b] + (place in the block),
+ * in fp32, rounded once.
+ *   rope, d_turns : configuration (rope_dim 64) and device frequencies; both NULL: x_r is stored as it is
+ *   x             : device bf16, row i at x + i * x_row_stride (elements, >= latent_dim + 64), packed block-major rows
+ *   norm_weight   : device bf16 [latent_dim], 16-byte aligned, or NULL: x_c is stored as it is
+ *   d_cu_new      : device int32 [B+1], block b's rows are [cu[b], cu[b+1]), at most num_rows in all.  NULL = one row per block
+ *                   (num_rows = B)
+ *   d_first       : device int32 [B], position of every block's first token, NULL = 0 everywhere
+ *   d_lens        : device int32 [B] tokens cached before the call, NULL = 0 everywhere
+ *   d_lens_out    : device int32 [B], written with the tokens cached after it; not d_lens itself; may be NULL
+ *   packed        : device bf16 [num_rows, latent_dim + 64], the stored rows again (what the up projections and
+ *                   cpa_latent_prefill read); rows that are not stored stay as they were; 16-byte aligned; may be NULL, or x
+ *                   itself where x_row_stride is latent_dim + 64
+ * A block whose rows do not fit its pages is left out (its length stays, CPA_ENOSPC in the tables' status), as is one with a
+ * bad range or a negative length (CPA_EINVAL).  The same call repeated stores the same cache.  Errors: CPA_EINVAL,
+ * CPA_EUNSUPPORTED, CPA_ECUDA.
+ */
+CPA_API int cpa_latent_append(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tables,
+                              const cpa_rope_config* rope, const uint64_t* d_turns, const void* x, int64_t x_row_stride,
+                              const void* norm_weight, const int32_t* d_cu_new, int32_t num_rows, const int32_t* d_first,
+                              const int32_t* d_lens, int32_t* d_lens_out, void* pool, void* packed, void* stream);
+
+/* Queries and outputs of the decode calls, device bf16, strides in elements (a multiple of 8 each, pointers 16-byte aligned):
+ * element e of head h of block b is at b * block_stride + h * head_stride + e. */
+typedef struct cpa_latent_io {
+    const void* q_latent;                    /* [B, num_heads, latent_dim] */
+    int64_t q_latent_block_stride, q_latent_head_stride;
+    const void* q_rope;                      /* [B, num_heads, 64] */
+    int64_t q_rope_block_stride, q_rope_head_stride;
+    void* o;                                 /* [B, num_heads, latent_dim]; heads must not share elements */
+    int64_t o_block_stride, o_head_stride;
+} cpa_latent_io;
+
+/* Size of the decode calls' device workspace in bytes, or a negative cpa_status.  Depends on cfg alone. */
+CPA_API int64_t cpa_latent_decode_workspace_bytes(const cpa_latent_config* cfg);
+
+/*
+ * cpa_latent_decode -- absorbed form, one query token per block over the block's first d_lens[b] tokens:
+ *     s_j = scale (q_latent . c_j + q_rope . r_j),      o = sum_j softmax(s)_j c_j.
+ * The split over the cached length is made on the device from the lengths.
+ *   d_lens      : device int32 [B]; 0 gives rows of zeros
+ *   d_active    : device int32 [B] or NULL = all; a block with flag 0 sits out, its rows of o are not written
+ *   d_workspace : device scratch, cpa_latent_decode_workspace_bytes, 16-byte aligned, needs no initialisation
+ * A block whose length is negative or beyond its pages sits out too (status CPA_EINVAL, CPA_ENOSPC).
+ * Precision: scores, sums and outputs are accumulated in fp32; the weights are rounded to bf16 for their product with c, and
+ * the denominator sums the rounded ones.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED, CPA_ECUDA.
+ */
+CPA_API int cpa_latent_decode(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tables,
+                              const cpa_latent_io* io, const int32_t* d_lens, const int32_t* d_active, const void* pool,
+                              void* d_workspace, void* stream);
+
+/*
+ * cpa_latent_step -- one decode step: cpa_latent_append of one row per block, then cpa_latent_decode over the cache with that
+ * row in it (as it was stored), the query's positional part turned to the new token's position (and rounded to bf16) on the
+ * way.
+ *   x, norm_weight, rope, d_turns, d_first : as for the append, one row per block; without rope q_rope is taken as it is
+ *   d_lens, d_lens_out : device int32 [B] tokens cached before and after the step, two arrays; a block that sits out keeps
+ *                        its length (a captured graph that is replayed as a loop holds an even number of steps)
+ * Everything else as for cpa_latent_decode.
+ */
+CPA_API int cpa_latent_step(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tables,
+                            const cpa_rope_config* rope, const uint64_t* d_turns, const cpa_latent_io* io, const void* x,
+                            int64_t x_row_stride, const void* norm_weight, const int32_t* d_first, const int32_t* d_lens,
+                            int32_t* d_lens_out, const int32_t* d_active, void* pool, void* d_workspace, void* stream);
+
+/*
+ * cpa_latent_prefill -- expanded form, causal attention of every block over itself (the prefill of cpa_prefill):
+ *     s_ij = scale (q_nope . k_nope_j + q_rope . r_j), j <= i,      o = sum_j softmax(s)_j v_j      per head.
+ *   plan   : from cpa_plan_create with cpa_latent_plan_config's configuration, uploaded
+ *   q      : device bf16 [total_tokens, num_heads, 128 + 64], positional part last (turned already)
+ *   kv     : device bf16 [total_tokens, num_heads, 128 + 128], a head's key part and value (one product gives both)
+ *   k_rope : device bf16, row i at k_rope + i * k_rope_row_stride (elements, a multiple of 8, >= 64): the positional keys, turned
+ *            already, as they lie behind the latent part of cpa_latent_append's packed rows
+ *   o      : device bf16 [total_tokens, num_heads, 128]
+ * All 16-byte aligned; o must not alias the inputs.  Errors: CPA_EINVAL (also: a plan of another configuration),
+ * CPA_EUNSUPPORTED (a plan with cached prefixes), CPA_ESTATE (not uploaded), CPA_ECUDA.
+ */
+CPA_API int cpa_latent_prefill(const cpa_latent_config* cfg, const cpa_plan* plan, const void* q, const void* kv,
+                               const void* k_rope, int64_t k_rope_row_stride, void* o, void* stream);
+
 /* Static text for a cpa_status value. */
 CPA_API const char* cpa_strerror(int status);
 

@@ -51,6 +51,34 @@ class cpa_table_dims(ctypes.Structure):
                 ("token_capacity", ctypes.c_int32)]
 
 
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_UNSCALED, ROPE_SCALED_ALL, ROPE_SCALED_BASE, ROPE_SCALED_PARTS, ROPE_SCALED_WAVES = 0, 1, 2, 3, 4
+
+
+class cpa_rope_config(ctypes.Structure):
+    _fields_ = [("rope_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("trained_len", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("fast", ctypes.c_double), ("slow", ctypes.c_double), ("amplitude", ctypes.c_double)]
+
+
+class cpa_rope_rows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("x_row_stride", ctypes.c_int64),
+                ("x_head_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("offset", ctypes.c_int32)]
+
+
+class cpa_latent_config(ctypes.Structure):
+    _fields_ = [("num_heads", ctypes.c_int32), ("latent_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32),
+                ("nope_dim", ctypes.c_int32), ("v_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("norm_eps", ctypes.c_float), ("num_sms", ctypes.c_int32)]
+
+
+class cpa_latent_io(ctypes.Structure):
+    _fields_ = [("q_latent", ctypes.c_void_p), ("q_latent_block_stride", ctypes.c_int64), ("q_latent_head_stride", ctypes.c_int64),
+                ("q_rope", ctypes.c_void_p), ("q_rope_block_stride", ctypes.c_int64), ("q_rope_head_stride", ctypes.c_int64),
+                ("o", ctypes.c_void_p), ("o_block_stride", ctypes.c_int64), ("o_head_stride", ctypes.c_int64)]
+
+
 class CpaError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -139,6 +167,26 @@ _lib.cpa_decode_append_q8.argtypes = [_cfgp, _dimsp] + [_vp] * 12
 _lib.cpa_decode_append_q8.restype = ctypes.c_int
 _lib.cpa_kv_read_q8.argtypes = [_cfgp, _dimsp, _vp, _vp, _vp, _c32] + [_vp] * 5
 _lib.cpa_kv_read_q8.restype = ctypes.c_int
+_ropep, _rowsp = ctypes.POINTER(cpa_rope_config), ctypes.POINTER(cpa_rope_rows)
+_latp, _iop = ctypes.POINTER(cpa_latent_config), ctypes.POINTER(cpa_latent_io)
+_lib.cpa_rope_turns.argtypes = [_ropep, ctypes.POINTER(ctypes.c_uint64)]
+_lib.cpa_rope_turns.restype = ctypes.c_int
+_lib.cpa_rope.argtypes = [_ropep, _vp, _vp, _c32, _rowsp, _rowsp, ctypes.c_int, _vp]
+_lib.cpa_rope.restype = ctypes.c_int
+_lib.cpa_latent_tables_config.argtypes = [_latp, _cfgp]
+_lib.cpa_latent_tables_config.restype = ctypes.c_int
+_lib.cpa_latent_plan_config.argtypes = [_latp, _cfgp]
+_lib.cpa_latent_plan_config.restype = ctypes.c_int
+_lib.cpa_latent_append.argtypes = [_latp, _dimsp, _vp, _ropep, _vp, _vp, ctypes.c_int64, _vp, _vp, _c32] + [_vp] * 6
+_lib.cpa_latent_append.restype = ctypes.c_int
+_lib.cpa_latent_decode_workspace_bytes.argtypes = [_latp]
+_lib.cpa_latent_decode_workspace_bytes.restype = ctypes.c_int64
+_lib.cpa_latent_decode.argtypes = [_latp, _dimsp, _vp, _iop] + [_vp] * 5
+_lib.cpa_latent_decode.restype = ctypes.c_int
+_lib.cpa_latent_step.argtypes = [_latp, _dimsp, _vp, _ropep, _vp, _iop, _vp, ctypes.c_int64] + [_vp] * 8
+_lib.cpa_latent_step.restype = ctypes.c_int
+_lib.cpa_latent_prefill.argtypes = [_latp, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp, _vp]
+_lib.cpa_latent_prefill.restype = ctypes.c_int
 _lib.cpa_strerror.argtypes = [ctypes.c_int]
 _lib.cpa_strerror.restype = ctypes.c_char_p
 
@@ -420,3 +468,90 @@ def cpa_kv_read_q8(cfg: cpa_config, dims: cpa_table_dims, d_tables, d_first, d_c
                    k_out, v_out, stream: int = 0) -> int:
     return _lib.cpa_kv_read_q8(cfg, dims, _ptr(d_tables), _ptr(d_first), _ptr(d_cu),
                                int(num_rows), _ptr(kv_pool), _ptr(kv_scales), _ptr(k_out), _ptr(v_out), stream or None)
+
+
+# ---- rotary positions and latent attention (no plan, but for the prefill)
+
+def cpa_rope_turns(cfg: cpa_rope_config, check: bool = True):
+    """Frequencies of a configuration as uint64 binary fractions of a turn; with check=False (status, array)."""
+    n = int(cfg.rope_dim) // 2
+    turns = np.zeros(max(1, min(n, 128)), dtype=np.uint64)
+    rc = _lib.cpa_rope_turns(cfg, turns.ctypes.data_as(ctypes.POINTER(ctypes.c_uint64)))
+    if not check:
+        return rc, turns
+    if rc != CPA_OK:
+        raise CpaError(rc, "cpa_rope_turns")
+    return turns
+
+
+def rope_rows(x, out=None, rope_dim: int = 0, offset: Optional[int] = None) -> cpa_rope_rows:
+    """The rows of a tensor [rows, heads, head_dim] (any strides but the last), for cpa_rope: into `out` (None: in place), the
+    rotated part at `offset`, or the last `rope_dim` elements of every head."""
+    out = x if out is None else out
+    for t in (x, out):
+        if t.dim() != 3 or str(t.dtype) != "torch.bfloat16" or (t.numel() and t.shape[2] > 1 and t.stride(2) != 1) or t.shape != x.shape:
+            raise ValueError(f"bf16 [rows, heads, head_dim] with whole heads is wanted, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    if out.device != x.device:
+        raise ValueError(f"out lies on {out.device}, x on {x.device}")
+    return cpa_rope_rows(x.data_ptr(), out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), x.shape[1], x.shape[2],
+                         x.shape[2] - rope_dim if offset is None else offset)
+
+
+def cpa_rope(cfg: cpa_rope_config, d_turns, d_positions, num_rows: int, q: cpa_rope_rows, k: Optional[cpa_rope_rows] = None,
+             inverse: bool = False, stream: int = 0) -> int:
+    return _lib.cpa_rope(cfg, _ptr(d_turns), _ptr(d_positions), int(num_rows), q, k, int(inverse), stream or None)
+
+
+def cpa_latent_tables_config(cfg: cpa_latent_config) -> cpa_config:
+    out = cpa_config()
+    rc = _lib.cpa_latent_tables_config(cfg, out)
+    if rc != CPA_OK:
+        raise CpaError(rc, "cpa_latent_tables_config")
+    return out
+
+
+def cpa_latent_plan_config(cfg: cpa_latent_config) -> cpa_config:
+    out = cpa_config()
+    rc = _lib.cpa_latent_plan_config(cfg, out)
+    if rc != CPA_OK:
+        raise CpaError(rc, "cpa_latent_plan_config")
+    return out
+
+
+def cpa_latent_append(cfg: cpa_latent_config, dims: cpa_table_dims, d_tables, rope: Optional[cpa_rope_config], d_turns, x,
+                      x_row_stride: int, norm_weight, d_cu_new, num_rows: int, d_first, d_lens, d_lens_out, pool, packed=None,
+                      stream: int = 0) -> int:
+    return _lib.cpa_latent_append(cfg, dims, _ptr(d_tables), rope, _ptr(d_turns), _ptr(x), int(x_row_stride), _ptr(norm_weight),
+                                  _ptr(d_cu_new), int(num_rows), _ptr(d_first), _ptr(d_lens), _ptr(d_lens_out), _ptr(pool),
+                                  _ptr(packed), stream or None)
+
+
+def latent_io(q_latent, q_rope, o) -> cpa_latent_io:
+    """Queries [B, heads, latent_dim] and [B, heads, 64] and outputs [B, heads, latent_dim] (any strides but the last)."""
+    for t in (q_latent, q_rope, o):
+        if t.dim() != 3 or str(t.dtype) != "torch.bfloat16" or t.stride(2) != 1 or t.shape[:2] != q_latent.shape[:2]:
+            raise ValueError(f"bf16 [blocks, heads, elements] with whole heads is wanted, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    return cpa_latent_io(q_latent.data_ptr(), q_latent.stride(0), q_latent.stride(1), q_rope.data_ptr(), q_rope.stride(0),
+                         q_rope.stride(1), o.data_ptr(), o.stride(0), o.stride(1))
+
+
+def cpa_latent_decode_workspace_bytes(cfg: cpa_latent_config) -> int:
+    return int(_lib.cpa_latent_decode_workspace_bytes(cfg))
+
+
+def cpa_latent_decode(cfg: cpa_latent_config, dims: cpa_table_dims, d_tables, io: cpa_latent_io, d_lens, d_active, pool,
+                      d_workspace, stream: int = 0) -> int:
+    return _lib.cpa_latent_decode(cfg, dims, _ptr(d_tables), io, _ptr(d_lens), _ptr(d_active), _ptr(pool), _ptr(d_workspace),
+                                  stream or None)
+
+
+def cpa_latent_step(cfg: cpa_latent_config, dims: cpa_table_dims, d_tables, rope: Optional[cpa_rope_config], d_turns,
+                    io: cpa_latent_io, x, x_row_stride: int, norm_weight, d_first, d_lens, d_lens_out, d_active, pool, d_workspace,
+                    stream: int = 0) -> int:
+    return _lib.cpa_latent_step(cfg, dims, _ptr(d_tables), rope, _ptr(d_turns), io, _ptr(x), int(x_row_stride), _ptr(norm_weight),
+                                _ptr(d_first), _ptr(d_lens), _ptr(d_lens_out), _ptr(d_active), _ptr(pool), _ptr(d_workspace),
+                                stream or None)
+
+
+def cpa_latent_prefill(cfg: cpa_latent_config, plan: int, q, kv, k_rope, k_rope_row_stride: int, o, stream: int = 0) -> int:
+    return _lib.cpa_latent_prefill(cfg, plan, _ptr(q), _ptr(kv), _ptr(k_rope), int(k_rope_row_stride), _ptr(o), stream or None)

@@ -93,10 +93,11 @@ __device__ __forceinline__ float ld_f32(const float* p) {
 // A programmatic launch: the grid may be made ready while the stream's earlier work ends; the kernel waits for that
 // work (griddepcontrol.wait) before it reads anything.
 template <class... P, class... A>
-int q8_launch(void (*kernel)(P...), int grid, int threads, cudaStream_t st, A... args) {
+int q8_launch_smem(void (*kernel)(P...), int grid, int threads, int smem, cudaStream_t st, A... args) {
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)grid);
     lc.blockDim = dim3((unsigned)threads);
+    lc.dynamicSmemBytes = (size_t)smem;
     lc.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -108,6 +109,10 @@ int q8_launch(void (*kernel)(P...), int grid, int threads, cudaStream_t st, A...
         return CPA_ECUDA;
     }
     return CPA_OK;
+}
+template <class... P, class... A>
+int q8_launch(void (*kernel)(P...), int grid, int threads, cudaStream_t st, A... args) {
+    return q8_launch_smem(kernel, grid, threads, 0, st, args...);
 }
 
 // ---------------------------------------------------------------- number format
