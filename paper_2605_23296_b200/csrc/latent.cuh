@@ -97,10 +97,127 @@ __device__ __forceinline__ uint32_t rope_turn(uint32_t w, float2 cs) {
     return bf_pack(turn_first(u, v, cs), turn_second(u, v, cs));
 }
 
-}  // namespace
+// ---------------------------------------------------------------- one latent row, by a warp
+// How a row becomes a cached one.
+struct row_recipe {
+    const __nv_bfloat16* weight;      // nullptr: the latent part is stored as it is
+    const uint64_t* turns;            // nullptr: so is the positional part
+    float eps, amplitude;
+    int interleaved;
+};
+// One row's pieces of a lane.
+template <int L> struct row_pieces {
+    static constexpr int C = L / 8, N = C + kRopeDim / 8, K = (N + 31) / 32;   // pieces of the latent part, of the row; per lane
+    uint4 v[K];
+};
+template <int L, bool WIDE>
+__device__ __forceinline__ void load_row(row_pieces<L>& r, const __nv_bfloat16* x, int lane) {
+#pragma unroll
+    for (int k = 0; k < row_pieces<L>::K; ++k) {
+        const int p = lane + 32 * k;
+        r.v[k] = make_uint4(0, 0, 0, 0);
+        if (p < row_pieces<L>::N) r.v[k] = WIDE ? ld_v4(x + 8 * p) : ld_8x16(x + 8 * p);
+    }
+}
+// The row as it is cached, in place.
+template <int L>
+__device__ __forceinline__ void make_row(row_pieces<L>& r, const row_recipe& a, int position, int lane) {
+    constexpr int C = row_pieces<L>::C, K = row_pieces<L>::K;
+    if (a.weight) {
+        float ss = 0.f;
+        auto add = [&](const uint4& v, float f) {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float lo = bf_lo(w[i]) * f, hi = bf_hi(w[i]) * f;
+                ss = fmaf(lo, lo, fmaf(hi, hi, ss));
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (lane + 32 * k < C) add(r.v[k], 1.f);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        float pre = 1.f, inv = rsqrtf(ss * (1.f / L) + a.eps);
+        // squares beyond fp32's range, or below it where nothing is added to them: taken of the row over a power of two
+        if (!(ss <= 1e37f) || (ss < 1e-30f && a.eps < 1e-30f)) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (lane + 32 * k < C) top = max(top, q8_amax8(r.v[k]));
+            top = __reduce_max_sync(0xffffffffu, top);
+            const int e = min(max((int)(max(top, __float_as_uint(sqrtf(a.eps))) >> 23), 1), 253);
+            pre = __uint_as_float((uint32_t)(254 - e) << 23);      // 2^(127 - e)
+            ss = 0.f;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (lane + 32 * k < C) {
+                    const uint32_t w[4] = {r.v[k].x, r.v[k].y, r.v[k].z, r.v[k].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float lo = mul_keep(bf_lo(w[i]), pre), hi = mul_keep(bf_hi(w[i]), pre);
+                        ss = fmaf(lo, lo, fmaf(hi, hi, ss));
+                    }
+                }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            inv = rsqrtf(ss * (1.f / L) + mul_keep(mul_keep(a.eps, pre), pre));
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int p = lane + 32 * k;
+            if (p >= C) continue;
+            const uint4 g = ld_v4(a.weight + 8 * p);
+            auto two = [&](uint32_t x, uint32_t w) {
+                return bf_pack(mul_keep(mul_keep(mul_keep(bf_lo(x), pre), inv), bf_lo(w)),
+                               mul_keep(mul_keep(mul_keep(bf_hi(x), pre), inv), bf_hi(w)));
+            };
+            r.v[k] = make_uint4(two(r.v[k].x, g.x), two(r.v[k].y, g.y), two(r.v[k].z, g.z), two(r.v[k].w, g.w));
+        }
+    }
+    if (a.turns) {
+        constexpr int k = C / 32;                        // the pieces behind the latent part are all in this round
+        static_assert(C % 32 + kRopeDim / 8 <= 32, "");
+        const float2 cs = rope_cos_sin(ld_u64(a.turns + lane), position, a.amplitude);     // pair `lane`
+        const int p = lane + 32 * k - C;                 // piece of the positional part, where 0 <= p < 8
+        uint32_t w[4] = {r.v[k].x, r.v[k].y, r.v[k].z, r.v[k].w};
+        auto pair = [&](int i) {
+            return make_float2(__shfl_sync(0xffffffffu, cs.x, i & 31), __shfl_sync(0xffffffffu, cs.y, i & 31));
+        };
+        if (a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 c = pair(4 * p + i);
+                w[i] = rope_turn(w[i], c);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                // the partner's elements are in the lane four on (or back)
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, w[i], 4);
+                const float2 c0 = pair(8 * p + 2 * i), c1 = pair(8 * p + 2 * i + 1);
+                w[i] = (p & 4) ? bf_pack(turn_second(bf_lo(other), bf_lo(w[i]), c0), turn_second(bf_hi(other), bf_hi(w[i]), c1))
+                               : bf_pack(turn_first(bf_lo(w[i]), bf_lo(other), c0), turn_first(bf_hi(w[i]), bf_hi(other), c1));
+            }
+        }
+        if (p >= 0 && p < kRopeDim / 8) r.v[k] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <int L>
+__device__ __forceinline__ void store_row(const row_pieces<L>& r, __nv_bfloat16* to, int lane) {
+#pragma unroll
+    for (int k = 0; k < row_pieces<L>::K; ++k) {
+        const int p = lane + 32 * k;
+        if (p < row_pieces<L>::N) *reinterpret_cast<uint4*>(to + 8 * p) = r.v[k];
+    }
+}
+// The row x, wherever it lies, to `to`.
+template <int L>
+__device__ __forceinline__ void put_new_row(const __nv_bfloat16* x, const row_recipe& a, int position, __nv_bfloat16* to, int lane) {
+    row_pieces<L> r;
+    if (__cvta_generic_to_global(x) % 16 == 0) load_row<L, true>(r, x, lane);
+    else load_row<L, false>(r, x, lane);
+    make_row<L>(r, a, position, lane);
+    store_row<L>(r, to, lane);
+}
 
-// cpa_latent_append over the blocks whose flag in d_active is not 0 (nullptr: all).
-int cpa_latent_append_rows(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tables, const cpa_rope_config* rope,
-                           const uint64_t* d_turns, const void* x, int64_t x_row_stride, const void* norm_weight,
-                           const int32_t* d_cu_new, int32_t num_rows, const int32_t* d_first, const int32_t* d_lens,
-                           int32_t* d_lens_out, const int32_t* d_active, void* pool, void* packed, void* stream);
+}  // namespace

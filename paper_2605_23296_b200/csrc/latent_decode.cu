@@ -1,101 +1,750 @@
-// Absorbed latent attention of one query token per block over the paged latent cache.
+// Absorbed latent attention of one query token per block over the paged latent cache, on the tensor cores.
+//
+//     S^T = K Q^T            [tokens, heads]     K: 64 rows of the cache, all latent_dim + 64 elements
+//     P^T = exp2(S^T - m)    m: a running reference of each head's maximum
+//     O^T += C^T P^T         [latent elements, heads]     C: the same 64 rows without their positional part
+//
+// The rows are staged once (TMA, one copy per page) and serve both products: as the K-major operand of the first and the
+// MN-major operand of the second.  Tokens and latent elements are on the M side, so 16, 32 or 64 heads fill N without waste, and
+// O^T (latent_dim / 128 accumulators of 128 lanes x heads columns) leaves room in tensor memory for two score buffers at 64
+// heads; with the heads on the M side the 512-wide outputs of 128 rows would take all of it.  More than 64 heads are two groups
+// on two CTAs that walk the same tokens.
+//
+// A CTA owns an equal share of all blocks' 64-token tiles, cut on the device from the lengths; a block that is cut leaves
+// partial sums in the workspace, which a second kernel joins.  Twelve warps with fixed roles:
+//   0-3   softmax: warp w holds tokens 16 w .. 16 w + 15 of a tile in the fragment layout of a 16-lane TMEM load; epilogue
+//   4-7   queries of the next segment into shared memory (turned, if asked for), a step's new row; rows of zeros
+//   8     TMA producer, one lane per page of a tile
+//   9     issuer of the score products; owner of the tensor memory
+//   10    issuer of the output products (a warp of its own, so that neither product waits behind the other's operands)
+//   11    walks the blocks and hands out the segments (block, first tile, tiles)
+// The reference m of a head stays as long as no score passes it by more than 2^8 (what it is cancels in the division); all
+// four softmax warps learn of that by one barrier with an OR, so a tile usually costs no exchange of maxima at all.
+//
+// Every mbarrier wait is bounded: when one gives up the CTA records it in the status word, stops waiting, still frees its
+// tensor memory and returns.
 #include <algorithm>
+#include <atomic>
 
 #include "latent.cuh"
+#include "cpa_tcgen05.cuh"
 
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kTile = 64;                       // tokens per tile
+constexpr int kTilePages = kTile / kPage;
+constexpr int kDecodeThreads = 384;
+constexpr int kSms = 148;                       // of a B200; CTAs do not wait for one another, so any device will do
+constexpr int kSegRing = 4;
+constexpr int kMaxDecodeStages = 6;
+constexpr int kBlockCost = 1;                   // what a block costs beside its tiles, in tiles (its queries, its output)
+constexpr int kMinRange = 4;                    // cost of a CTA's share, at least
+constexpr float kLowest = -3e38f;
+constexpr uint32_t kPBytes = kTile * 128;
 
 struct decode_args {
     q8_tables t;
     cpa_latent_io io;
     const uint64_t* turns;            // step: the query's positional part is turned; nullptr: taken as it is
-    const int32_t *first, *lens, *lens_before, *active;   // lens_before: step, blocks that have not grown sit out
-    const __nv_bfloat16* pool;
-    int B, H, interleaved;
-    float scale, amplitude;
+    const int32_t *first, *lens, *active;
+    // step (x given): the new token's row is made and stored first
+    const __nv_bfloat16 *x, *weight;
+    int64_t x_row;
+    int32_t* lens_out;
+    __nv_bfloat16* pool;
+    float2* part_ml;                  // [slots, head groups, 64]
+    float* part_o;                    // [slots, head groups, 64, L]
+    int2* cuts;                       // [groups] (block, parts) of the block that starts in a group and goes on behind it
+    int B, H, L, groups, head_groups, group_heads, stages, interleaved;
+    float scale_log2, amplitude, eps;
 };
 
-// One CTA per (block, head), a warp per token, lanes over the row's 16-byte pieces.
-template <int L>
-__global__ void __launch_bounds__(kWarps * 32) latent_decode_kernel(const __grid_constant__ decode_args a) {
-    constexpr int C = L / 8, N = C + kRopeDim / 8, K = (N + 31) / 32;
-    __shared__ float sm_o[kWarps][L], sm_m[kWarps], sm_l[kWarps], sm_rope[kRopeDim];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    const int b = blockIdx.x / a.H, h = blockIdx.x % a.H;
-    const int len = ld_i32(a.lens + b), ip = ld_i32(a.t.page_indptr + b), np = ld_i32(a.t.page_indptr + b + 1) - ip;
-    if (a.active && ld_i32(a.active + b) == 0) return;
-    if (a.lens_before && ld_i32(a.lens_before + b) == len) return;
-    if (len < 0 || len > (int64_t)np * kPage) {
-        if (threadIdx.x == 0) atomicCAS(a.t.header, 0, len < 0 ? kStatusInvalid : kStatusNoSpace);
+// A block's part in a launch.
+struct block_state { int len, ip, status; bool on; };
+__device__ __forceinline__ block_state block_of(int b, const decode_args& a) {
+    block_state r;
+    const int before = ld_i32(a.lens + b), np0 = ld_i32(a.t.page_indptr + b), np1 = ld_i32(a.t.page_indptr + b + 1);
+    const bool active = a.active == nullptr || ld_i32(a.active + b) != 0;
+    const int64_t len = (int64_t)before + (a.x ? 1 : 0), room = (int64_t)(np1 - np0) * kPage;
+    r.ip = np0;
+    r.status = !active ? 0 : before < 0 ? kStatusInvalid : len > room ? kStatusNoSpace : 0;
+    r.on = active && r.status == 0;
+    r.len = r.on ? (int)len : 0;
+    return r;
+}
+
+struct segment {
+    int block, tile0, tiles, len;     // block -1: no more; tiles [tile0, tile0 + tiles) of a block of `len` tokens
+    int ip, slot;                     // its first page in the list; partial slot, -1: the whole block
+    int pad[2];
+};
+
+__device__ __forceinline__ row_recipe new_row_of(const decode_args& a) {
+    return {a.weight, a.turns, a.eps, a.amplitude, a.interleaved};
+}
+__device__ __forceinline__ __nv_bfloat16* slot_of(const decode_args& a, const segment& g) {
+    const int at = g.len - 1, page = ld_i32(a.t.page_indices + g.ip + at / kPage);
+    return a.pool + ((int64_t)page * kPage + at % kPage) * (a.L + kRopeDim);
+}
+
+struct __align__(8) DecodeBarriers {
+    uint64_t kv_full[kMaxDecodeStages], kv_empty[kMaxDecodeStages][kTilePages];
+    uint64_t s_full[2], s_empty[2], p_full, pv_done, q_full, q_empty, o_empty, drain_s, drain_p;
+    uint64_t row_ready[2];            // of a CTA's growing segments in turn: their rows are made up to one segment ahead of the copies
+    uint64_t seg_full[kSegRing], seg_empty[kSegRing];
+    uint32_t tmem_base;
+};
+
+template <int N>
+struct DecodeShared {
+    DecodeBarriers bars;
+    segment seg[kSegRing];
+    float2 turn[kRopeDim / 2];
+    float column[4][N];               // per warp and head: maxima, sums
+    float factor[N];
+    int64_t scan[kDecodeThreads / 32];
+    int64_t start_cost;
+    int start_block;
+};
+
+// ---------------------------------------------------------------- PTX
+__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, int group, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %3}], [%4];\n"
+        :: "r"(dst), "l"(map), "r"(0), "r"(group), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+        :: "r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+// Whether `x` holds in any of the 128 threads that meet at barrier `id`.
+__device__ __forceinline__ bool any_of_128(int id, bool x) {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+                 : "=r"(r) : "r"((uint32_t)x), "r"(id) : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ void sync_128(int id) { asm volatile("barrier.cta.sync %0, 128;\n" :: "r"(id) : "memory"); }
+// Columns of 16 lanes in fragment layout: per 8 columns four words, of lane / 4 (words 0, 1) and lane / 4 + 8 (words 2, 3),
+// columns 2 (lane % 4) and the next.
+template <int N> __device__ __forceinline__ void tc_ld_frag(uint32_t taddr, float (&v)[N / 2]);
+template <> __device__ __forceinline__ void tc_ld_frag<16>(uint32_t taddr, float (&v)[8]) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+template <> __device__ __forceinline__ void tc_ld_frag<32>(uint32_t taddr, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+template <> __device__ __forceinline__ void tc_ld_frag<64>(uint32_t taddr, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+// 16 columns of this thread's lane
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// First cost of group g's share when `total` is dealt to `groups`.
+__device__ __forceinline__ int64_t share_start(int64_t total, int g, int groups) { return (total * g + groups - 1) / groups; }
+__device__ __forceinline__ int tiles_of(int len) { return (int)(((int64_t)len + kTile - 1) / kTile); }
+
+// A step's new row of block g, to its slot, by a warp (see latent_append.cu for the arithmetic).
+__device__ __forceinline__ void make_new_row(const decode_args& a, const segment& g, int position, int lane) {
+    switch (a.L) {
+        case 128: put_new_row<128>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of(a, g), lane); break;
+        case 256: put_new_row<256>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of(a, g), lane); break;
+        case 384: put_new_row<384>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of(a, g), lane); break;
+        default: put_new_row<512>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of(a, g), lane); break;
+    }
+}
+
+template <int N>
+__global__ void __launch_bounds__(kDecodeThreads, 1)
+latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ decode_args a) {
+    extern __shared__ __align__(1024) unsigned char gen[];       // (the kernel has no other shared memory, so this is its start)
+    const uint32_t base = smem_u32(gen);
+    if (base & 1023u) {              // swizzled tiles would be misread
+        if (threadIdx.x == 0) atomicCAS(a.t.header, 0, kStatusInvalid);
         return;
     }
-    const __nv_bfloat16* qc = (const __nv_bfloat16*)a.io.q_latent + b * a.io.q_latent_block_stride + h * a.io.q_latent_head_stride;
-    const __nv_bfloat16* qr = (const __nv_bfloat16*)a.io.q_rope + b * a.io.q_rope_block_stride + h * a.io.q_rope_head_stride;
-    if (threadIdx.x < 32) {
-        const int u = a.interleaved ? 2 * lane : lane, v = a.interleaved ? 2 * lane + 1 : lane + 32;
-        uint32_t w = ld_u16(qr + u) | ld_u16(qr + v) << 16;
-        if (a.turns) w = rope_turn(w, rope_cos_sin(ld_u64(a.turns + lane), (a.first ? ld_i32(a.first + b) : 0) + len - 1, a.amplitude));
-        sm_rope[u] = bf_lo(w);
-        sm_rope[v] = bf_hi(w);
+    const int nc = a.L / 64 + 1, nm = a.L / 128;              // column blocks of a row, 128-element blocks of the output
+    const uint32_t page_bytes = (uint32_t)nc * 2048, q_bytes = (uint32_t)nc * N * 128;
+    const uint32_t s_kv = base, s_q = s_kv + a.stages * kTilePages * page_bytes, s_p = s_q + q_bytes;
+    DecodeShared<N>& sm = *reinterpret_cast<DecodeShared<N>*>(gen + (s_p + kPBytes - base));
+    DecodeBarriers& bars = sm.bars;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int group = blockIdx.x / a.head_groups, hg = blockIdx.x - group * a.head_groups;
+    const int h0 = hg * a.group_heads, heads = min(a.group_heads, a.H - h0);
+    auto bar = [](uint64_t* p) { return smem_u32(p); };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(bar(&bars.kv_full[s]), kTilePages);
+            for (int p = 0; p < kTilePages; ++p) mbar_init(bar(&bars.kv_empty[s][p]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(&bars.s_full[i]), 1);
+            mbar_init(bar(&bars.s_empty[i]), 4);
+            mbar_init(bar(&bars.row_ready[i]), 1);
+        }
+        mbar_init(bar(&bars.p_full), 4);
+        mbar_init(bar(&bars.pv_done), 1);
+        mbar_init(bar(&bars.q_full), 4);
+        mbar_init(bar(&bars.q_empty), 1);
+        mbar_init(bar(&bars.o_empty), 4);
+        mbar_init(bar(&bars.drain_s), 1);
+        mbar_init(bar(&bars.drain_p), 1);
+        for (int i = 0; i < kSegRing; ++i) {
+            mbar_init(bar(&bars.seg_full[i]), 1);
+            mbar_init(bar(&bars.seg_empty[i]), 11);      // every warp but the one that hands out
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     }
-    __syncthreads();
-    float q[K][8], o[K][8], m = -3e38f, l = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int p = lane + 32 * k;
-        const uint4 w = p < C ? ld_v4(qc + 8 * p) : make_uint4(0, 0, 0, 0);
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { q[k][2 * i] = bf_lo(ww[i]); q[k][2 * i + 1] = bf_hi(ww[i]); }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (p >= C && p < N) q[k][i] = sm_rope[8 * (p - C) + i];
-            o[k][i] = 0.f;
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" :: "r"(smem_u32(&bars.tmem_base)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+
+    // ---- the cut: every CTA sums the cost of all blocks and finds where its share begins
+    const int per = (a.B + kDecodeThreads - 1) / kDecodeThreads, b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
+    int64_t cost = 0;
+    for (int b = b0; b < b1; ++b) {
+        const block_state s = block_of(b, a);
+        if (s.len > 0) cost += tiles_of(s.len) + kBlockCost;
+        if (b % (int)gridDim.x == (int)blockIdx.x) {     // the blocks' books are shared out
+            if (s.status) atomicCAS(a.t.header, 0, s.status);
+            if (a.x) a.lens_out[b] = ld_i32(a.lens + b) + (s.on ? 1 : 0);
         }
     }
-    for (int j = warp; j < len; j += kWarps) {
-        const __nv_bfloat16* row = a.pool + ((int64_t)ld_i32(a.t.page_indices + ip + j / kPage) * kPage + j % kPage) * (L + kRopeDim);
-        float x[K][8], s = 0.f;
+    int64_t inc = cost;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int p = lane + 32 * k;
-            const uint4 w = p < N ? ld_v4(row + 8 * p) : make_uint4(0, 0, 0, 0);
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { x[k][2 * i] = bf_lo(ww[i]); x[k][2 * i + 1] = bf_hi(ww[i]); }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(q[k][i], x[k][i], s);
-        }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        s *= a.scale * 1.4426950408889634f;
-        const float m2 = fmaxf(m, s), f = exp2f(m - m2), e = exp2f(s - m2);
-        m = m2;
-        l = l * f + e;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[k][i] = o[k][i] * f + e * x[k][i];
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
     }
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (lane + 32 * k < C) sm_o[warp][8 * (lane + 32 * k) + i] = o[k][i];
-    if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; }
+    if (lane == 31) sm.scan[warp] = inc;
+    if (threadIdx.x == 0) sm.start_block = a.B;
+    tc_fence_before();
     __syncthreads();
-    float mm = -3e38f, ll = 0.f;
-    for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, sm_m[w]);
-    for (int w = 0; w < kWarps; ++w) ll += sm_l[w] * exp2f(sm_m[w] - mm);
-    __nv_bfloat16* out = (__nv_bfloat16*)a.io.o + b * a.io.o_block_stride + h * a.io.o_head_stride;
-    for (int e = threadIdx.x; e < L; e += kWarps * 32) {
-        float v = 0.f;
-        for (int w = 0; w < kWarps; ++w) v += sm_o[w][e] * exp2f(sm_m[w] - mm);
-        out[e] = __float2bfloat16(len == 0 ? 0.f : v / ll);
+    tc_fence_after();
+    int64_t before = inc - cost, total = 0;
+    for (int w = 0; w < kDecodeThreads / 32; ++w) {
+        if (w < warp) before += sm.scan[w];
+        total += sm.scan[w];
+    }
+    const int used = (int)max((int64_t)1, min((int64_t)a.groups, total / kMinRange));     // groups that get a share
+    const int64_t lo = group < used ? share_start(total, group, used) : total, hi = group < used ? share_start(total, group + 1, used) : total;
+    if (cost > 0 && before <= lo && lo < before + cost) {
+        sm.start_block = b0;
+        sm.start_cost = before;
+    }
+    __syncthreads();
+    const uint32_t tmem = bars.tmem_base;
+    constexpr uint32_t kColO = 2 * N;
+    bool dead = false;
+    int32_t* const status = a.t.header;
+    auto wait = [&](uint64_t* p, uint32_t parity) { mbar_wait(bar(p), parity, dead, status, kSpinLimit); };
+    // segment i of this CTA, by a whole warp
+    auto get_segment = [&](int i) {
+        wait(&bars.seg_full[i % kSegRing], (uint32_t)(i / kSegRing) & 1u);
+        dead = __any_sync(0xffffffffu, dead);
+        segment s = sm.seg[i % kSegRing];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(&bars.seg_empty[i % kSegRing]));
+        if (dead) s.block = -1;
+        return s;
+    };
+
+    if (warp == 11) {
+        // ------------------------------------------------------------ segments
+        int n = 0;
+        int2 cut = make_int2(-1, 0);
+        int64_t c = sm.start_cost;
+        auto put = [&](const segment& s) {
+            wait(&bars.seg_empty[n % kSegRing], ((uint32_t)(n / kSegRing) & 1u) ^ 1u);
+            sm.seg[n % kSegRing] = s;
+            mbar_arrive(bar(&bars.seg_full[n % kSegRing]));
+            ++n;
+        };
+        if (lo < hi)
+            for (int b = sm.start_block; b < a.B && c < hi; b += 32) {
+                block_state s{0, 0, 0, false};
+                if (b + lane < a.B) s = block_of(b + lane, a);
+                const int tiles = tiles_of(s.len);
+                const int64_t mine = s.len > 0 ? tiles + kBlockCost : 0;
+                int64_t at = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t v = __shfl_up_sync(0xffffffffu, at, o);
+                    if (lane >= o) at += v;
+                }
+                const int64_t first = c + at - mine + kBlockCost;      // cost at which the block's first tile lies
+                c += __shfl_sync(0xffffffffu, at, 31);
+                const int j0 = (int)min((int64_t)tiles, max((int64_t)0, lo - first)), j1 = (int)min((int64_t)tiles, max((int64_t)0, hi - first));
+                uint32_t todo = __ballot_sync(0xffffffffu, s.len > 0 && j1 > j0);
+                while (todo) {
+                    const int who = __ffs(todo) - 1;
+                    todo &= todo - 1;
+                    if (lane == who) {
+                        const bool whole = j0 == 0 && j1 == tiles;
+                        put({b + lane, j0, j1 - j0, s.len, s.ip, whole ? -1 : 2 * group + (j0 == 0 ? 1 : 0), {0, 0}});
+                        if (j0 == 0 && j1 < tiles) cut = make_int2(b + lane, (int)((first + tiles - 1) * used / total) - group + 1);
+                    }
+                    n = __shfl_sync(0xffffffffu, n, who);
+                }
+                dead = __any_sync(0xffffffffu, dead);
+                if (dead) break;
+            }
+        if (lane == 0) put({-1, 0, 0, 0, 0, 0, {0, 0}});
+        const uint32_t has = __ballot_sync(0xffffffffu, cut.x >= 0);
+        const int who = has ? __ffs(has) - 1 : 0;
+        if (hg == 0 && lane == who) a.cuts[group] = cut;
+    } else if (warp == 8) {
+        // ------------------------------------------------------------ TMA producer, a lane per page
+        int it = 0, fresh = 0;
+        for (int i = 0;; ++i) {
+            const segment g = get_segment(i);
+            if (g.block < 0) break;
+            if (lane < kTilePages) {
+                const int pages = (int)(((int64_t)g.len + kPage - 1) / kPage);
+                int at = g.tile0 * kTilePages + lane;
+                int page = at < pages ? ld_i32(a.t.page_indices + g.ip + at) : 0;
+                const bool grows = a.x && (g.tile0 + g.tiles) * (int64_t)kTile >= g.len;    // holds the step's new token
+                for (int j = 0; j < g.tiles && !dead; ++j, at += kTilePages) {
+                    const int s = (it + j) % a.stages, my = page;
+                    const uint32_t par = (uint32_t)((it + j) / a.stages) & 1u;
+                    if (j + 1 < g.tiles && at + kTilePages < pages) page = ld_i32(a.t.page_indices + g.ip + at + kTilePages);
+                    wait(&bars.kv_empty[s][lane], par ^ 1u);
+                    if (dead) break;
+                    if (at >= pages) {
+                        mbar_arrive(bar(&bars.kv_full[s]));
+                        continue;
+                    }
+                    if (grows && at == pages - 1) {
+                        wait(&bars.row_ready[fresh & 1], (uint32_t)(fresh >> 1) & 1u);
+                        if (dead) break;
+                        asm volatile("fence.proxy.async;\n" ::: "memory");
+                    }
+                    mbar_expect_tx(bar(&bars.kv_full[s]), page_bytes);
+                    tma_load_page(s_kv + (s * kTilePages + lane) * page_bytes, &map, my * 2, bar(&bars.kv_full[s]));
+                }
+                if (grows) ++fresh;
+            }
+            it += g.tiles;
+            dead = __any_sync(0xffffffffu, dead);
+            if (dead) break;
+        }
+        // After a wait gave up: copies issued last may still be on their way into this CTA's shared memory.
+        if (__any_sync(0xffffffffu, dead) && lane == 0)
+            for (int s = 0; s < a.stages; ++s)
+                for (uint32_t par = 0; par < 2; ++par) mbar_drain(bar(&bars.kv_full[s]), par, kDrainLimit);
+    } else if (warp == 9) {
+        // ------------------------------------------------------------ score products
+        uint32_t leader = lane == 0;
+        constexpr uint32_t idesc = instr_desc(kTile, N, false);
+        const uint64_t da = smem_desc(s_kv, 16, (uint32_t)nc * 1024), db = smem_desc(s_q, 16, 1024);
+        int it = 0;
+        for (int i = 0;; ++i) {
+            const segment g = get_segment(i);
+            if (g.block < 0) break;
+            wait(&bars.q_full, (uint32_t)i & 1u);
+            for (int j = 0; j < g.tiles; ++j, ++it) {
+                const int s = it % a.stages;
+                wait(&bars.kv_full[s], (uint32_t)(it / a.stages) & 1u);
+                wait(&bars.s_empty[it & 1], ((uint32_t)(it >> 1) & 1u) ^ 1u);
+                if (dead) leader = 0;
+                tc_fence_after();
+                const uint64_t ta = da + ((uint32_t)s * kTilePages * page_bytes >> 4);
+                const uint32_t d = tmem + (it & 1) * N;
+                for (int c = 0; c < nc; ++c) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        tc_mma_ss(d, ta + (c * 1024 + k * 32 >> 4), db + (c * (N * 128) + k * 32 >> 4), idesc, (c | k) != 0, leader);
+                }
+                tc_commit(bar(&bars.s_full[it & 1]), leader);
+            }
+            tc_commit(bar(&bars.q_empty), leader);
+            dead = __any_sync(0xffffffffu, dead);
+            if (dead) break;
+        }
+        if (dead) {      // products queued before may still be running; tensor memory is not freed under them
+            tc_commit(bar(&bars.drain_s), (uint32_t)(lane == 0));
+            if (lane == 0) mbar_drain(bar(&bars.drain_s), 0u, kDrainLimit);
+        }
+    } else if (warp == 10) {
+        // ------------------------------------------------------------ output products
+        uint32_t leader = lane == 0;
+        constexpr uint32_t idesc = instr_desc(128, N, true) | (1u << 15);       // both operands MN-major
+        const uint64_t da = smem_desc(s_kv, 1024, (uint32_t)nc * 1024), db = smem_desc(s_p, 16, 1024);
+        int it = 0;
+        for (int i = 0;; ++i) {
+            const segment g = get_segment(i);
+            if (g.block < 0) break;
+            if (i > 0) wait(&bars.o_empty, (uint32_t)(i - 1) & 1u);
+            for (int j = 0; j < g.tiles; ++j, ++it) {
+                const int s = it % a.stages;
+                const int pages = (int)min((int64_t)kTilePages, ((int64_t)g.len - (int64_t)(g.tile0 + j) * kTile + kPage - 1) / kPage);
+                wait(&bars.p_full, (uint32_t)it & 1u);
+                if (dead) leader = 0;
+                tc_fence_after();
+                const uint64_t ta = da + ((uint32_t)s * kTilePages * page_bytes >> 4);
+#pragma unroll
+                for (int p = 0; p < kTilePages; ++p) {
+                    if (p < pages)
+                        for (int m = 0; m < nm; ++m)
+                            tc_mma_ss(tmem + kColO + m * N, ta + (p * page_bytes + m * 2048 >> 4), db + (p * 2048 >> 4), idesc, (j | p) != 0, leader);
+                    tc_commit(bar(&bars.kv_empty[s][p]), leader);
+                }
+                tc_commit(bar(&bars.pv_done), leader);
+            }
+            dead = __any_sync(0xffffffffu, dead);
+            if (dead) break;
+        }
+        if (dead) {
+            tc_commit(bar(&bars.drain_p), (uint32_t)(lane == 0));
+            if (lane == 0) mbar_drain(bar(&bars.drain_p), 0u, kDrainLimit);
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------ queries, a step's new row, rows of zeros
+        const int tid = threadIdx.x - 128, pieces = nc * 8, latent_pieces = a.L / 8;
+        int fresh = 0;
+        for (int i = 0;; ++i) {
+            const segment g = get_segment(i);
+            if (any_of_128(2, g.block < 0)) break;
+            const int position = (a.first ? ld_i32(a.first + g.block) : 0) + g.len - 1;
+            if (warp == 4 && a.x && (g.tile0 + g.tiles) * (int64_t)kTile >= g.len) {
+                // (the row before last has been loaded: its segment's scores are through, or the queries of the last segment
+                // could not have been stored)
+                make_new_row(a, g, position, lane);
+                asm volatile("fence.proxy.async;\n" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&bars.row_ready[fresh & 1]));
+                ++fresh;
+            }
+            if (a.turns) {
+                if (tid >= 32 && tid < 64) sm.turn[lane] = rope_cos_sin(ld_u64(a.turns + lane), position, a.amplitude);
+                sync_128(2);
+            }
+            const __nv_bfloat16* qc = (const __nv_bfloat16*)a.io.q_latent + g.block * a.io.q_latent_block_stride;
+            const __nv_bfloat16* qr = (const __nv_bfloat16*)a.io.q_rope + g.block * a.io.q_rope_block_stride;
+            constexpr int kBatch = 12;
+            bool free_yet = i == 0;
+            for (int at = tid; at < N * pieces; at += 128 * kBatch) {
+                uint4 v[kBatch];
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const int e = at + k * 128, h = e / pieces, p = e - h * pieces;
+                    v[k] = make_uint4(0, 0, 0, 0);
+                    if (e >= N * pieces || h >= heads) continue;
+                    if (p < latent_pieces) {
+                        v[k] = ld_v4(qc + (h0 + h) * a.io.q_latent_head_stride + 8 * p);
+                        continue;
+                    }
+                    const __nv_bfloat16* src = qr + (h0 + h) * a.io.q_rope_head_stride;
+                    const int r = p - latent_pieces;
+                    v[k] = ld_v4(src + 8 * r);
+                    if (a.turns == nullptr) continue;
+                    if (a.interleaved) {
+                        v[k] = make_uint4(rope_turn(v[k].x, sm.turn[4 * r]), rope_turn(v[k].y, sm.turn[4 * r + 1]),
+                                          rope_turn(v[k].z, sm.turn[4 * r + 2]), rope_turn(v[k].w, sm.turn[4 * r + 3]));
+                    } else {
+                        const uint4 o = ld_v4(src + 8 * (r ^ 4));      // the partner's elements
+                        const float2* c = sm.turn + 8 * (r & 3);
+                        auto two = [&](uint32_t own, uint32_t other, int q) {
+                            return r < 4 ? bf_pack(turn_first(bf_lo(own), bf_lo(other), c[q]), turn_first(bf_hi(own), bf_hi(other), c[q + 1]))
+                                         : bf_pack(turn_second(bf_lo(other), bf_lo(own), c[q]), turn_second(bf_hi(other), bf_hi(own), c[q + 1]));
+                        };
+                        v[k] = make_uint4(two(v[k].x, o.x, 0), two(v[k].y, o.y, 2), two(v[k].z, o.z, 4), two(v[k].w, o.w, 6));
+                    }
+                }
+                if (!free_yet) wait(&bars.q_empty, (uint32_t)(i - 1) & 1u);
+                free_yet = true;
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const int e = at + k * 128, h = e / pieces, p = e - h * pieces;
+                    if (e < N * pieces)
+                        *reinterpret_cast<uint4*>(gen + (s_q - base) + (p >> 3) * (N * 128) + h * 128 + (((p & 7) ^ (h & 7)) << 4)) = v[k];
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(&bars.q_full));
+            if (a.turns) sync_128(2);          // everyone is through with the angles
+        }
+        // blocks without a token: rows of zeros
+        for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+            const block_state s = block_of(b, a);
+            if (!s.on || s.len > 0) continue;
+            __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + b * a.io.o_block_stride;
+            for (int e = tid; e < a.H * latent_pieces; e += 128)
+                *reinterpret_cast<uint4*>(o + (e / latent_pieces) * a.io.o_head_stride + 8 * (e % latent_pieces)) = make_uint4(0, 0, 0, 0);
+        }
+    } else {
+        // ------------------------------------------------------------ softmax and epilogue
+        constexpr int J = N / 8;               // groups of eight heads; this thread has two heads and two tokens of each
+        const int token = 16 * warp + (lane >> 2), col = 2 * (lane & 3);
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        int it = 0;
+        for (int i = 0;; ++i) {
+            const segment g = get_segment(i);
+            if (any_of_128(1, g.block < 0)) break;
+            float m[2 * J], l[2 * J];
+#pragma unroll
+            for (int k = 0; k < 2 * J; ++k) { m[k] = kLowest; l[k] = 0.f; }
+            for (int j = 0; j < g.tiles; ++j, ++it) {
+                const int valid = (int)min((int64_t)kTile, (int64_t)g.len - (int64_t)(g.tile0 + j) * kTile);
+                wait(&bars.s_full[it & 1], (uint32_t)(it >> 1) & 1u);
+                tc_fence_after();
+                float s[4 * J];
+                tc_ld_frag<N>(tmem + lanes + (it & 1) * N, s);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&bars.s_empty[it & 1]));
+                if (valid < kTile) {
+#pragma unroll
+                    for (int k = 0; k < J; ++k) {
+                        if (token >= valid) s[4 * k] = s[4 * k + 1] = -INFINITY;
+                        if (token + 8 >= valid) s[4 * k + 2] = s[4 * k + 3] = -INFINITY;
+                    }
+                    // rows behind the length hold anything, and their weights of zero would not silence an infinity or a NaN
+                    const int stage = it % a.stages, row16 = a.L / 8;
+                    for (int e = threadIdx.x; e < (kTile - valid) * row16; e += 128) {
+                        const int t = valid + e / row16, p = e % row16;
+                        *reinterpret_cast<uint4*>(gen + stage * kTilePages * page_bytes + (t >> 3) * (nc * 1024) + (p >> 3) * 1024 + (t & 7) * 128 +
+                                                  ((p & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+                bool high = false;
+#pragma unroll
+                for (int k = 0; k < J; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) high |= fmaf(s[4 * k + e], a.scale_log2, -m[2 * k + (e & 1)]) > 8.f;
+                if (any_of_128(1, high || dead)) {
+                    if (any_of_128(1, dead)) { dead = true; break; }
+                    // some score is far above its head's reference: new references, and what was summed so far is scaled to them
+#pragma unroll
+                    for (int k = 0; k < J; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float x = fmaxf(s[4 * k + e], s[4 * k + e + 2]);
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                            if (lane < 4) sm.column[warp][8 * k + col + e] = x;
+                        }
+                    sync_128(1);
+#pragma unroll
+                    for (int k = 0; k < J; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int h = 8 * k + col + e;
+                            const float x = a.scale_log2 * fmaxf(fmaxf(sm.column[0][h], sm.column[1][h]), fmaxf(sm.column[2][h], sm.column[3][h]));
+                            float& r = m[2 * k + e];
+                            float f = 1.f;
+                            if (x - r > 8.f) {
+                                f = exp2f(r - x);
+                                r = x;
+                            }
+                            l[2 * k + e] *= f;
+                            if (warp == 0 && lane < 4) sm.factor[h] = f;
+                        }
+                    sync_128(1);
+                    if (j > 0) {
+                        wait(&bars.pv_done, (uint32_t)(it - 1) & 1u);
+                        tc_fence_after();
+                        for (int c = 0; c < nm * N; c += 8) {
+                            float v[8];
+                            tc_ld8(tmem + lanes + kColO + c, v);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] *= sm.factor[(c + e) % N];
+                            tc_st8(tmem + lanes + kColO + c, v);
+                        }
+                        tc_wait_st();
+                    }
+                }
+                // the weights' buffer is free once the previous tile's products have run
+                if (it > 0) wait(&bars.pv_done, (uint32_t)(it - 1) & 1u);
+#pragma unroll
+                for (int k = 0; k < J; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {       // token, token + 8
+                        const uint32_t w = bf_pack(exp2f(fmaf(s[4 * k + 2 * e], a.scale_log2, -m[2 * k])),
+                                                   exp2f(fmaf(s[4 * k + 2 * e + 1], a.scale_log2, -m[2 * k + 1])));
+                        l[2 * k] += bf_lo(w);
+                        l[2 * k + 1] += bf_hi(w);
+                        const int t = token + 8 * e;
+                        *reinterpret_cast<uint32_t*>(gen + (s_p - base) + t * 128 + ((k ^ (t & 7)) << 4) + 2 * col) = w;
+                    }
+                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&bars.p_full));
+            }
+            if (any_of_128(1, dead)) break;
+            // ---- the segment's end: sums over the tokens, then the outputs or the partial
+#pragma unroll
+            for (int k = 0; k < 2 * J; ++k) {
+                float x = l[k];
+                x += __shfl_xor_sync(0xffffffffu, x, 4);
+                x += __shfl_xor_sync(0xffffffffu, x, 8);
+                x += __shfl_xor_sync(0xffffffffu, x, 16);
+                if (lane < 4) sm.column[warp][8 * (k >> 1) + col + (k & 1)] = x;
+            }
+            sync_128(1);
+            const int64_t part = ((int64_t)g.slot * a.head_groups + hg) * 64;
+            if (warp == 0 && lane < 4)
+#pragma unroll
+                for (int k = 0; k < 2 * J; ++k) {
+                    const int h = 8 * (k >> 1) + col + (k & 1);
+                    const float x = (sm.column[0][h] + sm.column[1][h]) + (sm.column[2][h] + sm.column[3][h]);
+                    sm.factor[h] = g.slot < 0 ? 1.f / x : 1.f;
+                    if (g.slot >= 0 && h < heads) a.part_ml[part + h] = make_float2(m[k], x);
+                }
+            wait(&bars.pv_done, (uint32_t)(it - 1) & 1u);
+            dead = any_of_128(1, dead);
+            tc_fence_after();
+            for (int mb = 0; mb < nm; ++mb) {
+                const int dim = mb * 128 + 32 * warp + lane;
+                __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + g.block * a.io.o_block_stride + h0 * a.io.o_head_stride + (dim & ~1);
+#pragma unroll
+                for (int c = 0; c < N; c += 16) {
+                    float v[16];
+                    tc_ld16(tmem + lanes + kColO + mb * N + c, v);
+                    if (dead) continue;
+                    if (g.slot >= 0) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (c + e < heads) a.part_o[(part + c + e) * a.L + dim] = v[e];
+                    } else {
+                        // two heads at a time: an even lane takes its own and its neighbour's element of the first, an odd one
+                        // of the second
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) {
+                            const float x = mul_keep(v[e], sm.factor[c + e]), y = mul_keep(v[e + 1], sm.factor[c + e + 1]);
+                            const float other = __shfl_xor_sync(0xffffffffu, (lane & 1) ? x : y, 1);
+                            const uint32_t w = (lane & 1) ? bf_pack(other, y) : bf_pack(x, other);
+                            const int h = c + e + (lane & 1);
+                            if (h < heads) *reinterpret_cast<uint32_t*>(o + h * a.io.o_head_stride) = w;
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(&bars.o_empty));
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" :: "r"(tmem) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------- joining a cut block's parts
+// One unit = (cut block, head): four warps per quarter of the parts, each thread four latent elements; factors 2^(m_k - m) of
+// the parts' references.
+constexpr int kJoinThreads = 512, kJoinParts = kSms;
+__global__ void __launch_bounds__(kJoinThreads) latent_join_kernel(const __grid_constant__ decode_args a) {
+    __shared__ int2 list[kSms];
+    __shared__ int list_group[kSms], n_list;
+    __shared__ __align__(16) float acc[3][kMaxLatent];
+    __shared__ float factor[kJoinParts + 1];
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) n_list = 0;
+    __syncthreads();
+    if (warp == 0)
+        for (int g = lane; g - lane < a.groups; g += 32) {
+            int2 c = make_int2(-1, 0);
+            if (g < a.groups) {
+                c.x = ld_i32(&a.cuts[g].x);
+                c.y = ld_i32(&a.cuts[g].y);
+            }
+            const uint32_t has = __ballot_sync(0xffffffffu, c.x >= 0);
+            const int at = n_list + __popc(has & ((1u << lane) - 1));
+            if (c.x >= 0) { list[at] = c; list_group[at] = g; }
+            __syncwarp();
+            if (lane == 0) n_list += __popc(has);
+            __syncwarp();
+        }
+    __syncthreads();
+    const int quarter = tid / 128, e = (tid % 128) * 4;
+    for (int unit = blockIdx.x; unit < n_list * a.H; unit += gridDim.x) {
+        const int at = unit / a.H, head = unit - at * a.H, hg = head / a.group_heads, h = head - hg * a.group_heads;
+        const int n = list[at].y, g0 = list_group[at];
+        auto slot = [&](int k) { return ((int64_t)(k == 0 ? 2 * g0 + 1 : 2 * (g0 + k)) * a.head_groups + hg) * 64 + h; };
+        if (warp == 0) {
+            float top = kLowest, sum = 0.f;
+            for (int k = lane; k < n; k += 32) top = fmaxf(top, ld_f32(&a.part_ml[slot(k)].x));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            for (int k = lane; k < n; k += 32) {
+                const float f = exp2f(ld_f32(&a.part_ml[slot(k)].x) - top);
+                factor[k] = f;
+                sum += f * ld_f32(&a.part_ml[slot(k)].y);
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) factor[kJoinParts] = 1.f / sum;
+        }
+        __syncthreads();
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (e < a.L)
+#pragma unroll 8
+            for (int k = quarter; k < n; k += 4) {
+                const uint4 w = ld_v4(a.part_o + slot(k) * a.L + e);
+                const float f = factor[k];
+                v.x = fmaf(f, __uint_as_float(w.x), v.x);
+                v.y = fmaf(f, __uint_as_float(w.y), v.y);
+                v.z = fmaf(f, __uint_as_float(w.z), v.z);
+                v.w = fmaf(f, __uint_as_float(w.w), v.w);
+            }
+        if (quarter > 0 && e < a.L) *reinterpret_cast<float4*>(&acc[quarter - 1][e]) = v;
+        __syncthreads();
+        if (quarter == 0 && e < a.L) {
+            const float4 p = *reinterpret_cast<float4*>(&acc[0][e]), q = *reinterpret_cast<float4*>(&acc[1][e]),
+                         r = *reinterpret_cast<float4*>(&acc[2][e]);
+            const float f = factor[kJoinParts];
+            const uint2 w = make_uint2(bf_pack(mul_keep((v.x + p.x) + (q.x + r.x), f), mul_keep((v.y + p.y) + (q.y + r.y), f)),
+                                       bf_pack(mul_keep((v.z + p.z) + (q.z + r.z), f), mul_keep((v.w + p.w) + (q.w + r.w), f)));
+            *reinterpret_cast<uint2*>((__nv_bfloat16*)a.io.o + list[at].x * a.io.o_block_stride + head * a.io.o_head_stride + e) = w;
+        }
+        __syncthreads();
     }
 }
 
@@ -112,28 +761,106 @@ bool io_ok(const cpa_latent_io* io, int B, int H, int L) {
     return B == 1 || H == 1 || bs >= (H - 1) * hs + L || hs >= (B - 1) * bs + L;
 }
 
+// The pool as page-wise boxes: 64 elements x 8 tokens x column blocks x 2 groups of 8 tokens, which lands as
+// [group of 8 tokens][column block][8 rows of 128 bytes, swizzled]: uniform strides in tokens and in elements for both products.
+bool make_page_map(CUtensorMap* map, const void* pool, int64_t pages, int L) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    const cuuint64_t row = (cuuint64_t)(L + kRopeDim) * 2, nc = (cuuint64_t)L / 64 + 1;
+    const cuuint64_t dims[4] = {64, 8, nc, (cuuint64_t)pages * 2};
+    const cuuint64_t strides[3] = {row, 128, row * 8};
+    const cuuint32_t box[4] = {64, 8, (cuuint32_t)nc, 2};
+    const cuuint32_t elem[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, elem,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct decode_shape { int groups, head_groups, group_heads, n; };
+decode_shape shape_of(const cpa_latent_config& c) {
+    decode_shape s;
+    s.head_groups = c.num_heads > 64 ? 2 : 1;
+    s.group_heads = (c.num_heads + s.head_groups - 1) / s.head_groups;
+    s.n = s.group_heads <= 16 ? 16 : s.group_heads <= 32 ? 32 : 64;
+    const int sms = c.num_sms ? std::min(c.num_sms, kSms) : kSms;
+    s.groups = std::max(1, sms / s.head_groups);
+    return s;
+}
+struct workspace { int64_t ml, o, cuts, bytes; };
+workspace workspace_of(const cpa_latent_config& c) {
+    const decode_shape s = shape_of(c);
+    const int64_t rows = (int64_t)s.groups * 2 * s.head_groups * 64;
+    workspace w;
+    w.ml = 0;
+    w.o = rows * 8;
+    w.cuts = w.o + rows * c.latent_dim * 4;
+    w.bytes = (w.cuts + s.groups * 8 + 255) / 256 * 256;
+    return w;
+}
+
+template <int N>
+int launch(const CUtensorMap& map, decode_args& a, int max_smem, cudaStream_t st) {
+    const int nc = a.L / 64 + 1, tile = kTilePages * nc * 2048;
+    const int fixed = nc * N * 128 + (int)kPBytes + (int)sizeof(DecodeShared<N>);
+    a.stages = std::min(kMaxDecodeStages, (max_smem - fixed) / tile);
+    if (a.stages < 2) return CPA_EUNSUPPORTED;
+    const int smem = fixed + a.stages * tile;
+    static std::atomic<bool> configured_dev[64];
+    int dev_id = 0;
+    if (cudaGetDevice(&dev_id) != cudaSuccess || dev_id < 0 || dev_id >= 64) {
+        (void)cudaGetLastError();
+        return CPA_ECUDA;
+    }
+    if (!configured_dev[dev_id].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(latent_decode_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, max_smem) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return CPA_ECUDA;
+        }
+        configured_dev[dev_id].store(true, std::memory_order_relaxed);
+    }
+    return q8_launch_smem(latent_decode_kernel<N>, a.groups * a.head_groups, kDecodeThreads, smem, st, map, a);
+}
+
 int decode(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tables, const cpa_rope_config* rope,
-           const uint64_t* d_turns, const cpa_latent_io* io, const int32_t* d_first, const int32_t* d_lens,
-           const int32_t* d_before, const int32_t* d_active, const void* pool, void* stream) {
+           const uint64_t* d_turns, const cpa_latent_io* io, const void* x, int64_t x_row, const void* weight, const int32_t* d_first,
+           const int32_t* d_lens, int32_t* d_lens_out, const int32_t* d_active, const void* pool, void* d_workspace, void* stream) {
+    const decode_shape s = shape_of(*cfg);
+    const workspace w = workspace_of(*cfg);
     decode_args a = {};
     a.t = q8_view(latent_tables_cfg(*cfg), *dims, d_tables);
     a.io = *io;
     a.turns = d_turns;
     a.first = d_first;
     a.lens = d_lens;
-    a.lens_before = d_before;
     a.active = d_active;
-    a.pool = (const __nv_bfloat16*)pool;
+    a.x = (const __nv_bfloat16*)x;
+    a.weight = (const __nv_bfloat16*)weight;
+    a.x_row = x_row;
+    a.lens_out = d_lens_out;
+    a.pool = (__nv_bfloat16*)const_cast<void*>(pool);
+    char* ws = (char*)d_workspace;
+    a.part_ml = (float2*)(ws + w.ml);
+    a.part_o = (float*)(ws + w.o);
+    a.cuts = (int2*)(ws + w.cuts);
     a.B = dims->num_blocks;
     a.H = cfg->num_heads;
+    a.L = cfg->latent_dim;
+    a.groups = s.groups;
+    a.head_groups = s.head_groups;
+    a.group_heads = s.group_heads;
     a.interleaved = rope && rope->layout == CPA_ROPE_INTERLEAVED;
-    a.scale = cfg->scale;
+    a.scale_log2 = cfg->scale * 1.4426950408889634f;
     a.amplitude = rope ? (float)rope->amplitude : 1.f;
-    auto kernel = cfg->latent_dim == 128   ? latent_decode_kernel<128>
-                  : cfg->latent_dim == 256 ? latent_decode_kernel<256>
-                  : cfg->latent_dim == 384 ? latent_decode_kernel<384>
-                                           : latent_decode_kernel<512>;
-    return q8_launch(kernel, a.B * a.H, kWarps * 32, (cudaStream_t)stream, a);
+    a.eps = cfg->norm_eps;
+    CUtensorMap map;
+    if (!make_page_map(&map, pool, dims->num_pages, a.L)) return CPA_ECUDA;
+    constexpr int kMaxSmem = 232448;              // 227 KB, what a CTA can have on sm_100
+    cudaStream_t st = (cudaStream_t)stream;
+    const int rc = s.n == 16   ? launch<16>(map, a, kMaxSmem, st)
+                   : s.n == 32 ? launch<32>(map, a, kMaxSmem, st)
+                               : launch<64>(map, a, kMaxSmem, st);
+    if (rc != CPA_OK) return rc;
+    return q8_launch(latent_join_kernel, kSms * 2, kJoinThreads, st, a);
 }
 
 int check(const cpa_latent_config* cfg, const cpa_table_dims* dims, const void* d_tables, const cpa_latent_io* io,
@@ -154,7 +881,7 @@ int check(const cpa_latent_config* cfg, const cpa_table_dims* dims, const void* 
 
 extern "C" int64_t cpa_latent_decode_workspace_bytes(const cpa_latent_config* cfg) {
     const int rc = latent_check(cfg);
-    return rc != CPA_OK ? rc : 256;
+    return rc != CPA_OK ? rc : workspace_of(*cfg).bytes;
 }
 
 extern "C" int cpa_latent_decode(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tables,
@@ -162,7 +889,8 @@ extern "C" int cpa_latent_decode(const cpa_latent_config* cfg, const cpa_table_d
                                  void* d_workspace, void* stream) {
     const int rc = check(cfg, dims, d_tables, io, d_lens, d_active, pool, d_workspace);
     if (rc != CPA_OK) return rc;
-    return decode(cfg, dims, d_tables, nullptr, nullptr, io, nullptr, d_lens, nullptr, d_active, pool, stream);
+    return decode(cfg, dims, d_tables, nullptr, nullptr, io, nullptr, 0, nullptr, nullptr, d_lens, nullptr, d_active, pool, d_workspace,
+                  stream);
 }
 
 extern "C" int cpa_latent_step(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tables,
@@ -171,9 +899,11 @@ extern "C" int cpa_latent_step(const cpa_latent_config* cfg, const cpa_table_dim
                                int32_t* d_lens_out, const int32_t* d_active, void* pool, void* d_workspace, void* stream) {
     int rc = check(cfg, dims, d_tables, io, d_lens, d_active, pool, d_workspace);
     if (rc != CPA_OK) return rc;
-    if (!d_lens_out) return CPA_EINVAL;
-    rc = cpa_latent_append_rows(cfg, dims, d_tables, rope, d_turns, x, x_row_stride, norm_weight, nullptr, dims->num_blocks, d_first,
-                                d_lens, d_lens_out, d_active, pool, nullptr, stream);
-    if (rc != CPA_OK) return rc;
-    return decode(cfg, dims, d_tables, rope, d_turns, io, d_first, d_lens_out, d_lens, d_active, pool, stream);
+    if (!x || !d_lens_out || d_lens_out == d_lens || !latent_aligned(x, 2) || !latent_aligned(norm_weight, 16) ||
+        !latent_aligned(d_turns, 8) || !latent_aligned(d_first, 4) || !latent_aligned(d_lens_out, 4) ||
+        (d_turns != nullptr) != (rope != nullptr) || (rope && (!rope_config_ok(rope) || rope->rope_dim != kRopeDim)) ||
+        (dims->num_blocks > 1 && x_row_stride < cfg->latent_dim + kRopeDim))
+        return CPA_EINVAL;
+    return decode(cfg, dims, d_tables, rope, d_turns, io, x, x_row_stride, norm_weight, d_first, d_lens, d_lens_out, d_active, pool,
+                  d_workspace, stream);
 }
