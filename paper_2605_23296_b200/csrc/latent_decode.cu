@@ -39,8 +39,9 @@ constexpr int kSegRing = 4;
 constexpr int kMaxDecodeStages = 6;
 constexpr int kBlockCost = 1;                   // what a block costs beside its tiles, in tiles (its queries, its output)
 constexpr int kMinRange = 4;                    // cost of a CTA's share, at least
-constexpr float kLowest = -3e38f;
+constexpr float kLowest = -3e38f, kFirstMargin = 6.f;
 constexpr uint32_t kPBytes = kTile * 128;
+constexpr int kMaxSmem = 232448;                // 227 KB, what a CTA can have on sm_100
 
 struct decode_args {
     q8_tables t;
@@ -55,7 +56,8 @@ struct decode_args {
     float2* part_ml;                  // [slots, head groups, 64]
     float* part_o;                    // [slots, head groups, 64, L]
     int2* cuts;                       // [groups] (block, parts) of the block that starts in a group and goes on behind it
-    int B, H, L, groups, head_groups, group_heads, stages, interleaved;
+    int B, H, L, groups, head_groups, group_heads, interleaved;
+    int list_words;                   // of the page list, for a look ahead
     float scale_log2, amplitude, eps;
 };
 
@@ -82,15 +84,15 @@ struct segment {
 __device__ __forceinline__ row_recipe new_row_of(const decode_args& a) {
     return {a.weight, a.turns, a.eps, a.amplitude, a.interleaved};
 }
+template <int L>
 __device__ __forceinline__ __nv_bfloat16* slot_of(const decode_args& a, const segment& g) {
     const int at = g.len - 1, page = ld_i32(a.t.page_indices + g.ip + at / kPage);
-    return a.pool + ((int64_t)page * kPage + at % kPage) * (a.L + kRopeDim);
+    return a.pool + ((int64_t)page * kPage + at % kPage) * (L + kRopeDim);
 }
 
 struct __align__(8) DecodeBarriers {
     uint64_t kv_full[kMaxDecodeStages], kv_empty[kMaxDecodeStages][kTilePages];
-    uint64_t s_full[2], s_empty[2], p_full, pv_done, q_full, q_empty, o_empty, drain_s, drain_p;
-    uint64_t row_ready[2];            // of a CTA's growing segments in turn: their rows are made up to one segment ahead of the copies
+    uint64_t s_full[2], s_empty[2], p_full, pv_done, q_full, q_empty, o_empty, row_ready, drain_s, drain_p;
     uint64_t seg_full[kSegRing], seg_empty[kSegRing];
     uint32_t tmem_base;
 };
@@ -107,17 +109,47 @@ struct DecodeShared {
     int start_block;
 };
 
+template <int L, int N>
+struct DecodeShape {
+    static constexpr int kColumns = L / 64 + 1;                              // 64-element column blocks of a row
+    static constexpr uint32_t kPageBytes = kColumns * 2048, kQBytes = kColumns * N * 128;
+    static constexpr int kFixed = (int)(kQBytes + kPBytes) + (int)sizeof(DecodeShared<N>);
+    static constexpr int kFit = (kMaxSmem - kFixed) / (int)(kTilePages * kPageBytes);
+    static constexpr int kStages = kFit < kMaxDecodeStages ? kFit : kMaxDecodeStages;
+    static constexpr int kSmem = kFixed + kStages * kTilePages * (int)kPageBytes;
+    static_assert(kStages >= 2, "two tiles have to fit");
+    static_assert(2 * N + L / 128 * N <= 512, "tensor memory");
+};
+
 // ---------------------------------------------------------------- PTX
 __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, int group, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %3}], [%4];\n"
         :: "r"(dst), "l"(map), "r"(0), "r"(group), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
+__device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map, int head, int block, uint32_t bar) {
     asm volatile(
-        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
-        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-        :: "r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4}], [%5];\n"
+        :: "r"(dst), "l"(map), "r"(0), "r"(head), "r"(block), "r"(bar) : "memory");
+}
+// By one thread; descriptors as halves, of which the lower one holds the address.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                          uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n .reg .b64 da, db;\n setp.ne.b32 p, %6, 0;\n mov.b64 da, {%1, %2};\n mov.b64 db, {%3, %4};\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n}\n"
+        :: "r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+// One lane of the warp, chosen in the form that lets the compiler keep the operands of what that lane runs on the uniform
+// datapath: an MMA of 64 x 64 x 16 then goes out every 32 cycles, which is what its operands take out of shared memory, and
+// every 46 under a test of the lane's number (58 with the instruction alone predicated on it).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ void tc_commit_one(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" :: "r"(bar) : "memory");
 }
 // Whether `x` holds in any of the 128 threads that meet at barrier `id`.
 __device__ __forceinline__ bool any_of_128(int id, bool x) {
@@ -176,28 +208,21 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, float (&v)[16]) {
 __device__ __forceinline__ int64_t share_start(int64_t total, int g, int groups) { return (total * g + groups - 1) / groups; }
 __device__ __forceinline__ int tiles_of(int len) { return (int)(((int64_t)len + kTile - 1) / kTile); }
 
-// A step's new row of block g, to its slot, by a warp (see latent_append.cu for the arithmetic).
-__device__ __forceinline__ void make_new_row(const decode_args& a, const segment& g, int position, int lane) {
-    switch (a.L) {
-        case 128: put_new_row<128>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of(a, g), lane); break;
-        case 256: put_new_row<256>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of(a, g), lane); break;
-        case 384: put_new_row<384>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of(a, g), lane); break;
-        default: put_new_row<512>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of(a, g), lane); break;
-    }
-}
-
-template <int N>
+template <int L, int N>
 __global__ void __launch_bounds__(kDecodeThreads, 1)
-latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ decode_args a) {
+latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_qc,
+                     const __grid_constant__ CUtensorMap map_qr, const __grid_constant__ decode_args a) {
     extern __shared__ __align__(1024) unsigned char gen[];       // (the kernel has no other shared memory, so this is its start)
     const uint32_t base = smem_u32(gen);
     if (base & 1023u) {              // swizzled tiles would be misread
         if (threadIdx.x == 0) atomicCAS(a.t.header, 0, kStatusInvalid);
         return;
     }
-    const int nc = a.L / 64 + 1, nm = a.L / 128;              // column blocks of a row, 128-element blocks of the output
-    const uint32_t page_bytes = (uint32_t)nc * 2048, q_bytes = (uint32_t)nc * N * 128;
-    const uint32_t s_kv = base, s_q = s_kv + a.stages * kTilePages * page_bytes, s_p = s_q + q_bytes;
+    using Sh = DecodeShape<L, N>;
+    constexpr int nc = Sh::kColumns, nm = L / 128;            // column blocks of a row, 128-element blocks of the output
+    constexpr int kStages = Sh::kStages;
+    constexpr uint32_t page_bytes = Sh::kPageBytes, kTileBytes64 = kTilePages * page_bytes;
+    const uint32_t s_kv = base, s_q = s_kv + kStages * kTileBytes64, s_p = s_q + Sh::kQBytes;
     DecodeShared<N>& sm = *reinterpret_cast<DecodeShared<N>*>(gen + (s_p + kPBytes - base));
     DecodeBarriers& bars = sm.bars;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -206,20 +231,20 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     auto bar = [](uint64_t* p) { return smem_u32(p); };
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < a.stages; ++s) {
+        for (int s = 0; s < kStages; ++s) {
             mbar_init(bar(&bars.kv_full[s]), kTilePages);
             for (int p = 0; p < kTilePages; ++p) mbar_init(bar(&bars.kv_empty[s][p]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(&bars.s_full[i]), 1);
             mbar_init(bar(&bars.s_empty[i]), 4);
-            mbar_init(bar(&bars.row_ready[i]), 1);
         }
         mbar_init(bar(&bars.p_full), 4);
         mbar_init(bar(&bars.pv_done), 1);
-        mbar_init(bar(&bars.q_full), 4);
+        mbar_init(bar(&bars.q_full), a.turns ? 5 : 4);      // warps 4-7, and the copies beside what warp 5 turns
         mbar_init(bar(&bars.q_empty), 1);
         mbar_init(bar(&bars.o_empty), 4);
+        mbar_init(bar(&bars.row_ready), 1);
         mbar_init(bar(&bars.drain_s), 1);
         mbar_init(bar(&bars.drain_p), 1);
         for (int i = 0; i < kSegRing; ++i) {
@@ -234,6 +259,15 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    // What every CTA reads first is brought to L2 ahead of the wait (L2 is coherent: what is written until then is seen), the
+    // lists shared out.
+    for (int64_t i = (int64_t)(threadIdx.x * gridDim.x + blockIdx.x) * 32; i < a.list_words; i += (int64_t)kDecodeThreads * gridDim.x * 32) {
+        asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.t.page_indices + i));
+        if (i < a.B) {
+            asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.lens + i));
+            asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.t.page_indptr + i));
+        }
+    }
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
 
     // ---- the cut: every CTA sums the cost of all blocks and finds where its share begins
@@ -342,8 +376,8 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 int page = at < pages ? ld_i32(a.t.page_indices + g.ip + at) : 0;
                 const bool grows = a.x && (g.tile0 + g.tiles) * (int64_t)kTile >= g.len;    // holds the step's new token
                 for (int j = 0; j < g.tiles && !dead; ++j, at += kTilePages) {
-                    const int s = (it + j) % a.stages, my = page;
-                    const uint32_t par = (uint32_t)((it + j) / a.stages) & 1u;
+                    const int s = (it + j) % kStages, my = page;
+                    const uint32_t par = (uint32_t)((it + j) / kStages) & 1u;
                     if (j + 1 < g.tiles && at + kTilePages < pages) page = ld_i32(a.t.page_indices + g.ip + at + kTilePages);
                     wait(&bars.kv_empty[s][lane], par ^ 1u);
                     if (dead) break;
@@ -352,7 +386,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                         continue;
                     }
                     if (grows && at == pages - 1) {
-                        wait(&bars.row_ready[fresh & 1], (uint32_t)(fresh >> 1) & 1u);
+                        wait(&bars.row_ready, (uint32_t)fresh & 1u);
                         if (dead) break;
                         asm volatile("fence.proxy.async;\n" ::: "memory");
                     }
@@ -367,140 +401,157 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         }
         // After a wait gave up: copies issued last may still be on their way into this CTA's shared memory.
         if (__any_sync(0xffffffffu, dead) && lane == 0)
-            for (int s = 0; s < a.stages; ++s)
+            for (int s = 0; s < kStages; ++s)
                 for (uint32_t par = 0; par < 2; ++par) mbar_drain(bar(&bars.kv_full[s]), par, kDrainLimit);
     } else if (warp == 9) {
-        // ------------------------------------------------------------ score products
-        uint32_t leader = lane == 0;
+        // ------------------------------------------------------------ score products, by one lane
         constexpr uint32_t idesc = instr_desc(kTile, N, false);
-        const uint64_t da = smem_desc(s_kv, 16, (uint32_t)nc * 1024), db = smem_desc(s_q, 16, 1024);
-        int it = 0;
+        const uint64_t da = smem_desc(s_kv, 16, nc * 1024), db = smem_desc(s_q, 16, 1024);
+        const uint32_t a_hi = (uint32_t)(da >> 32), b_hi = (uint32_t)(db >> 32), b_lo = (uint32_t)db;
+        int it0 = 0;
         for (int i = 0;; ++i) {
             const segment g = get_segment(i);
             if (g.block < 0) break;
-            wait(&bars.q_full, (uint32_t)i & 1u);
-            for (int j = 0; j < g.tiles; ++j, ++it) {
-                const int s = it % a.stages;
-                wait(&bars.kv_full[s], (uint32_t)(it / a.stages) & 1u);
-                wait(&bars.s_empty[it & 1], ((uint32_t)(it >> 1) & 1u) ^ 1u);
-                if (dead) leader = 0;
-                tc_fence_after();
-                const uint64_t ta = da + ((uint32_t)s * kTilePages * page_bytes >> 4);
-                const uint32_t d = tmem + (it & 1) * N;
-                for (int c = 0; c < nc; ++c) {
+            if (elect_one()) {
+                int it = it0;
+                wait(&bars.q_full, (uint32_t)i & 1u);
+                for (int j = 0; j < g.tiles && !dead; ++j, ++it) {
+                    const int s = it % kStages;
+                    wait(&bars.kv_full[s], (uint32_t)(it / kStages) & 1u);
+                    wait(&bars.s_empty[it & 1], ((uint32_t)(it >> 1) & 1u) ^ 1u);
+                    if (dead) break;
+                    tc_fence_after();
+                    const uint32_t a_lo = (uint32_t)da + (uint32_t)s * (kTileBytes64 >> 4), d = tmem + (it & 1) * N;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        tc_mma_ss(d, ta + (c * 1024 + k * 32 >> 4), db + (c * (N * 128) + k * 32 >> 4), idesc, (c | k) != 0, leader);
+                    for (int k = 0; k < nc * 4; ++k)
+                        tc_mma_ss(d, a_lo + ((k >> 2) * 1024 + (k & 3) * 32 >> 4), a_hi, b_lo + ((k >> 2) * (N * 128) + (k & 3) * 32 >> 4), b_hi,
+                                  idesc, k != 0);
+                    tc_commit_one(bar(&bars.s_full[it & 1]));
                 }
-                tc_commit(bar(&bars.s_full[it & 1]), leader);
+                if (!dead) tc_commit_one(bar(&bars.q_empty));
             }
-            tc_commit(bar(&bars.q_empty), leader);
+            it0 += g.tiles;
             dead = __any_sync(0xffffffffu, dead);
             if (dead) break;
         }
-        if (dead) {      // products queued before may still be running; tensor memory is not freed under them
-            tc_commit(bar(&bars.drain_s), (uint32_t)(lane == 0));
-            if (lane == 0) mbar_drain(bar(&bars.drain_s), 0u, kDrainLimit);
+        if (dead && lane == 0) {      // products queued before may still be running; tensor memory is not freed under them
+            tc_commit_one(bar(&bars.drain_s));
+            mbar_drain(bar(&bars.drain_s), 0u, kDrainLimit);
         }
     } else if (warp == 10) {
-        // ------------------------------------------------------------ output products
-        uint32_t leader = lane == 0;
+        // ------------------------------------------------------------ output products, by one lane
         constexpr uint32_t idesc = instr_desc(128, N, true) | (1u << 15);       // both operands MN-major
-        const uint64_t da = smem_desc(s_kv, 1024, (uint32_t)nc * 1024), db = smem_desc(s_p, 16, 1024);
-        int it = 0;
+        const uint64_t da = smem_desc(s_kv, 1024, nc * 1024), db = smem_desc(s_p, 16, 1024);
+        const uint32_t a_hi = (uint32_t)(da >> 32), b_hi = (uint32_t)(db >> 32), b_lo = (uint32_t)db;
+        int it0 = 0;
         for (int i = 0;; ++i) {
             const segment g = get_segment(i);
             if (g.block < 0) break;
-            if (i > 0) wait(&bars.o_empty, (uint32_t)(i - 1) & 1u);
-            for (int j = 0; j < g.tiles; ++j, ++it) {
-                const int s = it % a.stages;
-                const int pages = (int)min((int64_t)kTilePages, ((int64_t)g.len - (int64_t)(g.tile0 + j) * kTile + kPage - 1) / kPage);
-                wait(&bars.p_full, (uint32_t)it & 1u);
-                if (dead) leader = 0;
-                tc_fence_after();
-                const uint64_t ta = da + ((uint32_t)s * kTilePages * page_bytes >> 4);
+            if (elect_one()) {
+                int it = it0;
+                if (i > 0) wait(&bars.o_empty, (uint32_t)(i - 1) & 1u);
+                for (int j = 0; j < g.tiles && !dead; ++j, ++it) {
+                    const int s = it % kStages;
+                    const int pages = (int)min((int64_t)kTilePages, ((int64_t)g.len - (int64_t)(g.tile0 + j) * kTile + kPage - 1) / kPage);
+                    wait(&bars.p_full, (uint32_t)it & 1u);
+                    if (dead) break;
+                    tc_fence_after();
+                    const uint32_t a_lo = (uint32_t)da + (uint32_t)s * (kTileBytes64 >> 4);
 #pragma unroll
-                for (int p = 0; p < kTilePages; ++p) {
-                    if (p < pages)
-                        for (int m = 0; m < nm; ++m)
-                            tc_mma_ss(tmem + kColO + m * N, ta + (p * page_bytes + m * 2048 >> 4), db + (p * 2048 >> 4), idesc, (j | p) != 0, leader);
-                    tc_commit(bar(&bars.kv_empty[s][p]), leader);
+                    for (int p = 0; p < kTilePages; ++p) {
+                        if (p < pages) {
+#pragma unroll
+                            for (int m = 0; m < nm; ++m)
+                                tc_mma_ss(tmem + kColO + m * N, a_lo + (p * page_bytes + m * 2048 >> 4), a_hi, b_lo + (p * 2048 >> 4), b_hi, idesc,
+                                          p != 0 || j != 0);
+                        }
+                        tc_commit_one(bar(&bars.kv_empty[s][p]));
+                    }
+                    tc_commit_one(bar(&bars.pv_done));
                 }
-                tc_commit(bar(&bars.pv_done), leader);
             }
+            it0 += g.tiles;
             dead = __any_sync(0xffffffffu, dead);
             if (dead) break;
         }
-        if (dead) {
-            tc_commit(bar(&bars.drain_p), (uint32_t)(lane == 0));
-            if (lane == 0) mbar_drain(bar(&bars.drain_p), 0u, kDrainLimit);
+        if (dead && lane == 0) {
+            tc_commit_one(bar(&bars.drain_p));
+            mbar_drain(bar(&bars.drain_p), 0u, kDrainLimit);
         }
     } else if (warp >= 4) {
         // ------------------------------------------------------------ queries, a step's new row, rows of zeros
-        const int tid = threadIdx.x - 128, pieces = nc * 8, latent_pieces = a.L / 8;
-        int fresh = 0;
+        // (loops are kept short: what a launch runs once or twice costs the fetching of its instructions)
+        constexpr int latent_pieces = L / 8;           // 16-byte pieces of a row's latent part
+        const int tid = threadIdx.x - 128;
+        auto q_at = [&](int h, int p) {                // where piece p of head h's positional part lies (swizzled)
+            return reinterpret_cast<uint4*>(gen + (s_q - base) + (nc - 1) * (N * 128) + h * 128 + ((p ^ (h & 7)) << 4));
+        };
         for (int i = 0;; ++i) {
             const segment g = get_segment(i);
             if (any_of_128(2, g.block < 0)) break;
             const int position = (a.first ? ld_i32(a.first + g.block) : 0) + g.len - 1;
-            if (warp == 4 && a.x && (g.tile0 + g.tiles) * (int64_t)kTile >= g.len) {
-                // (the row before last has been loaded: its segment's scores are through, or the queries of the last segment
-                // could not have been stored)
-                make_new_row(a, g, position, lane);
-                asm volatile("fence.proxy.async;\n" ::: "memory");
+            if (i > 0) wait(&bars.q_empty, (uint32_t)(i - 1) & 1u);
+            if (warp == 5) {
+                // the latent parts, and the positional ones that do not turn; heads behind the last are filled with zeros
+                if (lane == 0 && !dead) {
+                    mbar_expect_tx(bar(&bars.q_full), Sh::kQBytes - (a.turns ? N * 128 : 0));
+                    tma_load_q(s_q, &map_qc, h0, g.block, bar(&bars.q_full));
+                    if (!a.turns) tma_load_3d(s_q + (nc - 1) * (N * 128), &map_qr, 0, h0, g.block, bar(&bars.q_full));
+                }
+                if (a.turns) sm.turn[lane] = rope_cos_sin(ld_u64(a.turns + lane), position, a.amplitude);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&bars.row_ready[fresh & 1]));
-                ++fresh;
             }
             if (a.turns) {
-                if (tid >= 32 && tid < 64) sm.turn[lane] = rope_cos_sin(ld_u64(a.turns + lane), position, a.amplitude);
+                // turned positional parts: a thread takes pieces r and r ^ 4 of a head, each other's partners in the half layout
+                const __nv_bfloat16* qr = (const __nv_bfloat16*)a.io.q_rope + g.block * a.io.q_rope_block_stride + h0 * a.io.q_rope_head_stride;
+                constexpr int kRounds = (N * 4 + 127) / 128;
+                const int r = tid & 3;
+                uint4 x[kRounds], y[kRounds];
+#pragma unroll
+                for (int k = 0; k < kRounds; ++k) {
+                    const int h = (tid >> 2) + 32 * k;
+                    x[k] = y[k] = make_uint4(0, 0, 0, 0);
+                    if (h < heads) {
+                        x[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * r);
+                        y[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * (r + 4));
+                    }
+                }
                 sync_128(2);
-            }
-            const __nv_bfloat16* qc = (const __nv_bfloat16*)a.io.q_latent + g.block * a.io.q_latent_block_stride;
-            const __nv_bfloat16* qr = (const __nv_bfloat16*)a.io.q_rope + g.block * a.io.q_rope_block_stride;
-            constexpr int kBatch = 12;
-            bool free_yet = i == 0;
-            for (int at = tid; at < N * pieces; at += 128 * kBatch) {
-                uint4 v[kBatch];
 #pragma unroll
-                for (int k = 0; k < kBatch; ++k) {
-                    const int e = at + k * 128, h = e / pieces, p = e - h * pieces;
-                    v[k] = make_uint4(0, 0, 0, 0);
-                    if (e >= N * pieces || h >= heads) continue;
-                    if (p < latent_pieces) {
-                        v[k] = ld_v4(qc + (h0 + h) * a.io.q_latent_head_stride + 8 * p);
-                        continue;
-                    }
-                    const __nv_bfloat16* src = qr + (h0 + h) * a.io.q_rope_head_stride;
-                    const int r = p - latent_pieces;
-                    v[k] = ld_v4(src + 8 * r);
-                    if (a.turns == nullptr) continue;
+                for (int k = 0; k < kRounds; ++k) {
+                    const int h = (tid >> 2) + 32 * k;
+                    if (h >= N) break;
+                    uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, w[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
                     if (a.interleaved) {
-                        v[k] = make_uint4(rope_turn(v[k].x, sm.turn[4 * r]), rope_turn(v[k].y, sm.turn[4 * r + 1]),
-                                          rope_turn(v[k].z, sm.turn[4 * r + 2]), rope_turn(v[k].w, sm.turn[4 * r + 3]));
-                    } else {
-                        const uint4 o = ld_v4(src + 8 * (r ^ 4));      // the partner's elements
-                        const float2* c = sm.turn + 8 * (r & 3);
-                        auto two = [&](uint32_t own, uint32_t other, int q) {
-                            return r < 4 ? bf_pack(turn_first(bf_lo(own), bf_lo(other), c[q]), turn_first(bf_hi(own), bf_hi(other), c[q + 1]))
-                                         : bf_pack(turn_second(bf_lo(other), bf_lo(own), c[q]), turn_second(bf_hi(other), bf_hi(own), c[q + 1]));
-                        };
-                        v[k] = make_uint4(two(v[k].x, o.x, 0), two(v[k].y, o.y, 2), two(v[k].z, o.z, 4), two(v[k].w, o.w, 6));
-                    }
-                }
-                if (!free_yet) wait(&bars.q_empty, (uint32_t)(i - 1) & 1u);
-                free_yet = true;
 #pragma unroll
-                for (int k = 0; k < kBatch; ++k) {
-                    const int e = at + k * 128, h = e / pieces, p = e - h * pieces;
-                    if (e < N * pieces)
-                        *reinterpret_cast<uint4*>(gen + (s_q - base) + (p >> 3) * (N * 128) + h * 128 + (((p & 7) ^ (h & 7)) << 4)) = v[k];
+                        for (int e = 0; e < 4; ++e) {
+                            u[e] = rope_turn(u[e], sm.turn[4 * r + e]);
+                            w[e] = rope_turn(w[e], sm.turn[4 * r + 16 + e]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 c0 = sm.turn[8 * r + 2 * e], c1 = sm.turn[8 * r + 2 * e + 1];
+                            const float u0 = bf_lo(u[e]), u1 = bf_hi(u[e]), w0 = bf_lo(w[e]), w1 = bf_hi(w[e]);
+                            u[e] = bf_pack(turn_first(u0, w0, c0), turn_first(u1, w1, c1));
+                            w[e] = bf_pack(turn_second(u0, w0, c0), turn_second(u1, w1, c1));
+                        }
+                    }
+                    *q_at(h, r) = make_uint4(u[0], u[1], u[2], u[3]);
+                    *q_at(h, r + 4) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
+                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                __syncwarp();
             }
-            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(&bars.q_full));
-            if (a.turns) sync_128(2);          // everyone is through with the angles
+            if (lane == 0 && warp != 5) mbar_arrive(bar(&bars.q_full));
+            if (lane == 0 && warp == 5 && a.turns) mbar_arrive(bar(&bars.q_full));
+            // (the last growing segment's row has been loaded: its scores are through, or these queries could not have been stored)
+            if (warp == 4 && a.x && (g.tile0 + g.tiles) * (int64_t)kTile >= g.len) {
+                put_new_row<L>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of<L>(a, g), lane);
+                asm volatile("fence.proxy.async;\n" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&bars.row_ready));
+            }
         }
         // blocks without a token: rows of zeros
         for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
@@ -538,12 +589,30 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                         if (token + 8 >= valid) s[4 * k + 2] = s[4 * k + 3] = -INFINITY;
                     }
                     // rows behind the length hold anything, and their weights of zero would not silence an infinity or a NaN
-                    const int stage = it % a.stages, row16 = a.L / 8;
+                    constexpr int row16 = L / 8;
+                    const int stage = it % kStages;
                     for (int e = threadIdx.x; e < (kTile - valid) * row16; e += 128) {
                         const int t = valid + e / row16, p = e % row16;
-                        *reinterpret_cast<uint4*>(gen + stage * kTilePages * page_bytes + (t >> 3) * (nc * 1024) + (p >> 3) * 1024 + (t & 7) * 128 +
+                        *reinterpret_cast<uint4*>(gen + stage * kTileBytes64 + (t >> 3) * (nc * 1024) + (p >> 3) * 1024 + (t & 7) * 128 +
                                                   ((p & 7) << 4)) = make_uint4(0, 0, 0, 0);
                     }
+                }
+                if (j == 0) {
+                    // The first reference: the first token's score and a margin (with N(0, 2^2) scores the largest of a long block
+                    // is then mostly within 2^8 of it); the true maximum takes over where it is not.
+                    if (warp == 0 && lane < 4)
+#pragma unroll
+                        for (int k = 0; k < J; ++k)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) sm.factor[8 * k + col + e] = s[4 * k + e];
+                    sync_128(1);
+#pragma unroll
+                    for (int k = 0; k < J; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float x = fmaf(sm.factor[8 * k + col + e], a.scale_log2, kFirstMargin);
+                            m[2 * k + e] = fabsf(x) < 1e38f ? x : kLowest;
+                        }
                 }
                 bool high = false;
 #pragma unroll
@@ -583,6 +652,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                     if (j > 0) {
                         wait(&bars.pv_done, (uint32_t)(it - 1) & 1u);
                         tc_fence_after();
+#pragma unroll 1
                         for (int c = 0; c < nm * N; c += 8) {
                             float v[8];
                             tc_ld8(tmem + lanes + kColO + c, v);
@@ -634,6 +704,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             wait(&bars.pv_done, (uint32_t)(it - 1) & 1u);
             dead = any_of_128(1, dead);
             tc_fence_after();
+#pragma unroll 1
             for (int mb = 0; mb < nm; ++mb) {
                 const int dim = mb * 128 + 32 * warp + lane;
                 __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + g.block * a.io.o_block_stride + h0 * a.io.o_head_stride + (dim & ~1);
@@ -645,7 +716,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                     if (g.slot >= 0) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e)
-                            if (c + e < heads) a.part_o[(part + c + e) * a.L + dim] = v[e];
+                            if (c + e < heads) a.part_o[(part + c + e) * L + dim] = v[e];
                     } else {
                         // two heads at a time: an even lane takes its own and its neighbour's element of the first, an odd one
                         // of the second
@@ -675,77 +746,138 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 }
 
 // ---------------------------------------------------------------- joining a cut block's parts
-// One unit = (cut block, head): four warps per quarter of the parts, each thread four latent elements; factors 2^(m_k - m) of
-// the parts' references.
-constexpr int kJoinThreads = 512, kJoinParts = kSms;
-__global__ void __launch_bounds__(kJoinThreads) latent_join_kernel(const __grid_constant__ decode_args a) {
-    __shared__ int2 list[kSms];
-    __shared__ int list_group[kSms], n_list;
-    __shared__ __align__(16) float acc[3][kMaxLatent];
-    __shared__ float factor[kJoinParts + 1];
+// One unit = 128 elements of a (cut block, head), four per lane of a warp; factors 2^(m_k - m) of the parts' references.  Up to
+// kFewParts parts a warp takes a unit by itself, with all its loads in flight at once; if any block has more, a CTA's eight warps
+// share a unit's parts.  (Short code: it runs once, so fetching its instructions is part of its time.)
+constexpr int kJoinWarps = 8, kFewParts = 8, kJoinCtas = 8 * kSms;
+__device__ __forceinline__ void add_part(float4& v, const uint4& w, float f) {
+    v.x = fmaf(f, __uint_as_float(w.x), v.x);
+    v.y = fmaf(f, __uint_as_float(w.y), v.y);
+    v.z = fmaf(f, __uint_as_float(w.z), v.z);
+    v.w = fmaf(f, __uint_as_float(w.w), v.w);
+}
+__device__ __forceinline__ float2 ld_f2(const float2* p) {
+    float2 v;
+    asm volatile("ld.global.v2.f32 {%0,%1}, [%2];\n" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__global__ void __launch_bounds__(kJoinWarps * 32) latent_join_kernel(const __grid_constant__ decode_args a) {
+    __shared__ int list[3][kSms];             // block, parts, group
+    __shared__ int count[kJoinWarps];
+    __shared__ float4 acc[kJoinWarps][32];
+    __shared__ float factor[kSms + 1];
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) n_list = 0;
-    __syncthreads();
-    if (warp == 0)
-        for (int g = lane; g - lane < a.groups; g += 32) {
-            int2 c = make_int2(-1, 0);
-            if (g < a.groups) {
-                c.x = ld_i32(&a.cuts[g].x);
-                c.y = ld_i32(&a.cuts[g].y);
-            }
-            const uint32_t has = __ballot_sync(0xffffffffu, c.x >= 0);
-            const int at = n_list + __popc(has & ((1u << lane) - 1));
-            if (c.x >= 0) { list[at] = c; list_group[at] = g; }
-            __syncwarp();
-            if (lane == 0) n_list += __popc(has);
-            __syncwarp();
-        }
-    __syncthreads();
-    const int quarter = tid / 128, e = (tid % 128) * 4;
-    for (int unit = blockIdx.x; unit < n_list * a.H; unit += gridDim.x) {
-        const int at = unit / a.H, head = unit - at * a.H, hg = head / a.group_heads, h = head - hg * a.group_heads;
-        const int n = list[at].y, g0 = list_group[at];
-        auto slot = [&](int k) { return ((int64_t)(k == 0 ? 2 * g0 + 1 : 2 * (g0 + k)) * a.head_groups + hg) * 64 + h; };
-        if (warp == 0) {
-            float top = kLowest, sum = 0.f;
-            for (int k = lane; k < n; k += 32) top = fmaxf(top, ld_f32(&a.part_ml[slot(k)].x));
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    static_assert(kSms <= kJoinWarps * 32, "a thread per group");
+    int2 cut = make_int2(-1, 0);              // the cuts in their order, which all CTAs have to agree on
+    if ((int)threadIdx.x < a.groups) cut = make_int2(ld_i32(&a.cuts[threadIdx.x].x), ld_i32(&a.cuts[threadIdx.x].y));
+    const uint32_t has = __ballot_sync(0xffffffffu, cut.x >= 0);
+    if (lane == 0) count[warp] = __popc(has);
+    const bool shared = __syncthreads_or(cut.y > kFewParts);
+    int n_list = 0, at = __popc(has & ((1u << lane) - 1));
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            for (int k = lane; k < n; k += 32) {
-                const float f = exp2f(ld_f32(&a.part_ml[slot(k)].x) - top);
-                factor[k] = f;
-                sum += f * ld_f32(&a.part_ml[slot(k)].y);
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if (lane == 0) factor[kJoinParts] = 1.f / sum;
-        }
-        __syncthreads();
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (e < a.L)
-#pragma unroll 8
-            for (int k = quarter; k < n; k += 4) {
-                const uint4 w = ld_v4(a.part_o + slot(k) * a.L + e);
-                const float f = factor[k];
-                v.x = fmaf(f, __uint_as_float(w.x), v.x);
-                v.y = fmaf(f, __uint_as_float(w.y), v.y);
-                v.z = fmaf(f, __uint_as_float(w.z), v.z);
-                v.w = fmaf(f, __uint_as_float(w.w), v.w);
-            }
-        if (quarter > 0 && e < a.L) *reinterpret_cast<float4*>(&acc[quarter - 1][e]) = v;
-        __syncthreads();
-        if (quarter == 0 && e < a.L) {
-            const float4 p = *reinterpret_cast<float4*>(&acc[0][e]), q = *reinterpret_cast<float4*>(&acc[1][e]),
-                         r = *reinterpret_cast<float4*>(&acc[2][e]);
-            const float f = factor[kJoinParts];
-            const uint2 w = make_uint2(bf_pack(mul_keep((v.x + p.x) + (q.x + r.x), f), mul_keep((v.y + p.y) + (q.y + r.y), f)),
-                                       bf_pack(mul_keep((v.z + p.z) + (q.z + r.z), f), mul_keep((v.w + p.w) + (q.w + r.w), f)));
-            *reinterpret_cast<uint2*>((__nv_bfloat16*)a.io.o + list[at].x * a.io.o_block_stride + head * a.io.o_head_stride + e) = w;
-        }
-        __syncthreads();
+    for (int w = 0; w < kJoinWarps; ++w) {
+        if (w < warp) at += count[w];
+        n_list += count[w];
     }
+    if (cut.x >= 0) { list[0][at] = cut.x; list[1][at] = cut.y; list[2][at] = (int)threadIdx.x; }
+    __syncthreads();
+    const int quarters = a.L / 128, units = a.H * quarters;      // per cut block
+    const int per = shared ? units : (units + kJoinWarps - 1) / kJoinWarps, n_work = n_list * per;
+    for (int work = blockIdx.x; work < n_work; work += gridDim.x) {
+        const int c = work / per, unit = shared ? work - c * per : (work - c * per) * kJoinWarps + warp;
+        const int n = list[1][c], g0 = list[2][c];
+        const bool on = unit < units;
+        const int head = on ? unit / quarters : 0, e = (on ? unit % quarters : 0) * 128 + lane * 4;
+        const int hg = head / a.group_heads;
+        const int64_t step = 2 * (int64_t)a.head_groups * 64, row0 = ((int64_t)(2 * g0 + 1) * a.head_groups + hg) * 64 + head - hg * a.group_heads,
+                      row1 = row0 - (int64_t)a.head_groups * 64;            // part 0; part k > 0 is at row1 + k * step
+        auto row = [&](int k) { return k == 0 ? row0 : row1 + k * step; };
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+        if (!shared) {
+            uint4 w[kFewParts];
+#pragma unroll
+            for (int k = 0; k < kFewParts; ++k) {
+                w[k] = make_uint4(0, 0, 0, 0);
+                if (k < n) w[k] = ld_v4(a.part_o + row(k) * a.L + e);
+            }
+            float2 ml = make_float2(kLowest, 0.f);
+            if (lane < n) ml = ld_f2(a.part_ml + row(lane));
+            float top = ml.x;
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = __shfl_sync(0xffffffffu, top, 0);
+            const float f = exp2f(ml.x - top);
+            sum = lane < n ? f * ml.y : 0.f;
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            sum = __shfl_sync(0xffffffffu, sum, 0);
+#pragma unroll
+            for (int k = 0; k < kFewParts; ++k) {
+                const float fk = __shfl_sync(0xffffffffu, f, k);
+                if (k < n) add_part(v, w[k], fk);
+            }
+        } else {
+            if (warp == 0) {
+                float top = kLowest;
+                for (int k = lane; k < n; k += 32) top = fmaxf(top, ld_f32(&a.part_ml[row(k)].x));
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                for (int k = lane; k < n; k += 32) {
+                    const float2 ml = ld_f2(a.part_ml + row(k));
+                    factor[k] = exp2f(ml.x - top);
+                    sum += factor[k] * ml.y;
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            }
+            uint4 w[kFewParts];
+            int k0 = warp;
+            auto load = [&] {
+#pragma unroll
+                for (int k = 0; k < kFewParts; ++k)
+                    if (k0 + k * kJoinWarps < n) w[k] = ld_v4(a.part_o + row(k0 + k * kJoinWarps) * a.L + e);
+            };
+            load();
+            __syncthreads();
+            for (; k0 < n; k0 += kJoinWarps * kFewParts) {
+                if (k0 > warp) load();
+#pragma unroll
+                for (int k = 0; k < kFewParts; ++k)
+                    if (k0 + k * kJoinWarps < n) add_part(v, w[k], factor[k0 + k * kJoinWarps]);
+            }
+            acc[warp][lane] = v;
+            __syncthreads();
+            if (warp == 0)
+#pragma unroll 1
+                for (int k = 1; k < kJoinWarps; ++k) {
+                    const float4 x = acc[k][lane];
+                    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+                }
+        }
+        if (on && (!shared || warp == 0)) {
+            const float f = 1.f / sum;
+            *reinterpret_cast<uint2*>((__nv_bfloat16*)a.io.o + list[0][c] * a.io.o_block_stride + head * a.io.o_head_stride + e) =
+                make_uint2(bf_pack(mul_keep(v.x, f), mul_keep(v.y, f)), bf_pack(mul_keep(v.z, f), mul_keep(v.w, f)));
+        }
+    }
+}
+
+// Queries [B, H, elements] as boxes of N heads: 64 elements x heads (x column blocks) x one block.
+bool make_q_map(CUtensorMap* map, const void* q, int B, int H, int64_t block_stride, int64_t head_stride, int columns, int N) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    const cuuint64_t hs = (cuuint64_t)(H > 1 ? head_stride : 64 * columns) * 2, bs = (cuuint64_t)(B > 1 ? block_stride : 64 * columns) * 2;
+    const cuuint64_t dims4[4] = {64, (cuuint64_t)H, (cuuint64_t)columns, (cuuint64_t)B}, strides4[3] = {hs, 128, bs};
+    const cuuint32_t box4[4] = {64, (cuuint32_t)N, (cuuint32_t)columns, 1}, elem[4] = {1, 1, 1, 1};
+    const cuuint64_t dims3[3] = {64, (cuuint64_t)H, (cuuint64_t)B}, strides3[2] = {hs, bs};
+    const cuuint32_t box3[3] = {64, (cuuint32_t)N, 1};
+    const bool four = columns > 1;
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, four ? 4 : 3, const_cast<void*>(q), four ? dims4 : dims3, four ? strides4 : strides3,
+              four ? box4 : box3, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool io_ok(const cpa_latent_io* io, int B, int H, int L) {
@@ -755,6 +887,10 @@ bool io_ok(const cpa_latent_io* io, int B, int H, int L) {
     for (int64_t s : {io->q_latent_block_stride, io->q_latent_head_stride, io->q_rope_block_stride, io->q_rope_head_stride,
                       io->o_block_stride, io->o_head_stride})
         if (s % 8 != 0) return false;
+    // queries are read through tensor maps: strides that count are positive and below 2^40 bytes
+    for (int64_t s : {B > 1 ? io->q_latent_block_stride : 8, H > 1 ? io->q_latent_head_stride : 8, B > 1 ? io->q_rope_block_stride : 8,
+                      H > 1 ? io->q_rope_head_stride : 8})
+        if (s <= 0 || s >= (int64_t)1 << 39) return false;
     // heads of the output must not share elements: blocks of heads, or heads of blocks
     const int64_t bs = B > 1 ? io->o_block_stride : INT64_MAX, hs = H > 1 ? io->o_head_stride : INT64_MAX;
     if (bs < L || hs < L) return false;
@@ -798,27 +934,32 @@ workspace workspace_of(const cpa_latent_config& c) {
     return w;
 }
 
-template <int N>
-int launch(const CUtensorMap& map, decode_args& a, int max_smem, cudaStream_t st) {
-    const int nc = a.L / 64 + 1, tile = kTilePages * nc * 2048;
-    const int fixed = nc * N * 128 + (int)kPBytes + (int)sizeof(DecodeShared<N>);
-    a.stages = std::min(kMaxDecodeStages, (max_smem - fixed) / tile);
-    if (a.stages < 2) return CPA_EUNSUPPORTED;
-    const int smem = fixed + a.stages * tile;
+template <int L, int N>
+int launch(const CUtensorMap (&map)[3], const decode_args& a, cudaStream_t st) {
     static std::atomic<bool> configured_dev[64];
     int dev_id = 0;
     if (cudaGetDevice(&dev_id) != cudaSuccess || dev_id < 0 || dev_id >= 64) {
         (void)cudaGetLastError();
         return CPA_ECUDA;
     }
+    constexpr int smem = DecodeShape<L, N>::kSmem;
     if (!configured_dev[dev_id].load(std::memory_order_relaxed)) {
-        if (cudaFuncSetAttribute(latent_decode_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, max_smem) != cudaSuccess) {
+        if (cudaFuncSetAttribute(latent_decode_kernel<L, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
             (void)cudaGetLastError();
             return CPA_ECUDA;
         }
         configured_dev[dev_id].store(true, std::memory_order_relaxed);
     }
-    return q8_launch_smem(latent_decode_kernel<N>, a.groups * a.head_groups, kDecodeThreads, smem, st, map, a);
+    return q8_launch_smem(latent_decode_kernel<L, N>, a.groups * a.head_groups, kDecodeThreads, smem, st, map[0], map[1], map[2], a);
+}
+template <int N>
+int launch_latent(const CUtensorMap (&map)[3], const decode_args& a, cudaStream_t st) {
+    switch (a.L) {
+        case 128: return launch<128, N>(map, a, st);
+        case 256: return launch<256, N>(map, a, st);
+        case 384: return launch<384, N>(map, a, st);
+        default: return launch<512, N>(map, a, st);
+    }
 }
 
 int decode(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tables, const cpa_rope_config* rope,
@@ -852,15 +993,18 @@ int decode(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tab
     a.scale_log2 = cfg->scale * 1.4426950408889634f;
     a.amplitude = rope ? (float)rope->amplitude : 1.f;
     a.eps = cfg->norm_eps;
-    CUtensorMap map;
-    if (!make_page_map(&map, pool, dims->num_pages, a.L)) return CPA_ECUDA;
-    constexpr int kMaxSmem = 232448;              // 227 KB, what a CTA can have on sm_100
+    a.list_words = dims->page_capacity;
+    CUtensorMap map[3];
+    if (!make_page_map(&map[0], pool, dims->num_pages, a.L) ||
+        !make_q_map(&map[1], io->q_latent, a.B, a.H, io->q_latent_block_stride, io->q_latent_head_stride, a.L / 64, s.n) ||
+        !make_q_map(&map[2], io->q_rope, a.B, a.H, io->q_rope_block_stride, io->q_rope_head_stride, 1, s.n))
+        return CPA_ECUDA;
     cudaStream_t st = (cudaStream_t)stream;
-    const int rc = s.n == 16   ? launch<16>(map, a, kMaxSmem, st)
-                   : s.n == 32 ? launch<32>(map, a, kMaxSmem, st)
-                               : launch<64>(map, a, kMaxSmem, st);
+    const int rc = s.n == 16   ? launch_latent<16>(map, a, st)
+                   : s.n == 32 ? launch_latent<32>(map, a, st)
+                               : launch_latent<64>(map, a, st);
     if (rc != CPA_OK) return rc;
-    return q8_launch(latent_join_kernel, kSms * 2, kJoinThreads, st, a);
+    return q8_launch(latent_join_kernel, kJoinCtas, kJoinWarps * 32, st, a);
 }
 
 int check(const cpa_latent_config* cfg, const cpa_table_dims* dims, const void* d_tables, const cpa_latent_io* io,

@@ -107,7 +107,8 @@ def test_latent_pointers_and_strides_are_refused():
     step = dict(dec, rope=_rope(), d_turns=ok, x=ok, x_row_stride=576, norm_weight=None, d_first=None, d_lens_out=other)
     bad_io = [dict(q_latent=0), dict(q_rope=0), dict(o=0), dict(q_latent=ok + 8), dict(q_rope=ok + 2), dict(o=ok + 8),
               dict(q_latent_head_stride=516), dict(q_rope_block_stride=1), dict(o_head_stride=504), dict(o_block_stride=4096),
-              dict(o_head_stride=-512), dict(o_block_stride=0)]
+              dict(o_head_stride=-512), dict(o_block_stride=0), dict(q_latent_head_stride=0), dict(q_rope_block_stride=-1024),
+              dict(q_rope_head_stride=0), dict(q_latent_block_stride=1 << 39)]
     for bad in [dict(io=B.cpa_latent_io(**dict(io, **b))) for b in bad_io] + [
             dict(d_tables=None), dict(d_lens=None), dict(pool=None), dict(d_workspace=None), dict(d_lens=ok + 2), dict(d_active=ok + 2),
             dict(pool=ok + 8), dict(d_workspace=ok + 8), dict(d_tables=ok + 4)]:
