@@ -19,7 +19,7 @@ struct append_args {
     int32_t* lens_out;
     __nv_bfloat16 *pool, *packed;
     int64_t x_row;
-    int B, rows, row_ctas;
+    int B, rows, row_ctas, at_once;
 };
 
 __device__ __forceinline__ int cu_at(const int32_t* cu, int b) { return cu ? ld_i32(cu + b) : b; }
@@ -83,11 +83,21 @@ __global__ void __launch_bounds__(kWarps * 32) latent_append_kernel(const __grid
         }
         return;
     }
-    for (int64_t row = (int64_t)blockIdx.x * kWarps + warp; row < a.rows; row += (int64_t)a.row_ctas * kWarps) {
+    // (where there are many rows a warp has two in flight, which mostly are the same block's)
+    row_pieces<L> r2;
+    for (int64_t row = ((int64_t)blockIdx.x * kWarps + warp) * a.at_once; row < a.rows; row += (int64_t)a.row_ctas * kWarps * a.at_once) {
+        const bool two = a.at_once == 2 && row + 1 < a.rows;
         load_row<L, WIDE>(r, a.x + row * a.x_row, lane);
-        const int b = find_block((int)row, a.cu, a.B, lane);
-        const block_rows o = rows_of(b, a);
+        if (two) load_row<L, WIDE>(r2, a.x + (row + 1) * a.x_row, lane);
+        int b = find_block((int)row, a.cu, a.B, lane);
+        block_rows o = rows_of(b, a);
         if (!o.status && row >= o.c0 && row < o.c0 + o.n) put_row<L>(r, (int)row, b, o, a, lane);
+        if (!two) continue;
+        if (row + 1 >= o.c0 + o.n || row + 1 < o.c0) {
+            b = find_block((int)row + 1, a.cu, a.B, lane);
+            o = rows_of(b, a);
+        }
+        if (!o.status && row + 1 >= o.c0 && row + 1 < o.c0 + o.n) put_row<L>(r2, (int)row + 1, b, o, a, lane);
     }
 }
 
@@ -137,7 +147,8 @@ extern "C" int cpa_latent_append(const cpa_latent_config* cfg, const cpa_table_d
     a.x_row = x_row_stride;
     a.B = dims->num_blocks;
     a.rows = num_rows;
-    a.row_ctas = (int)std::min<int64_t>(((int64_t)num_rows + kWarps - 1) / kWarps, 1 << 20);
+    a.at_once = num_rows > 2 * 148 * 64 ? 2 : 1;              // (two waves of warps, by one row each)
+    a.row_ctas = (int)std::min<int64_t>(((int64_t)num_rows + kWarps * a.at_once - 1) / (kWarps * a.at_once), 1 << 20);
     const int grid = a.row_ctas + std::min((a.B + kWarps - 1) / kWarps, 1 << 16);
     const bool wide = latent_aligned(x, 16) && x_row_stride % 8 == 0;
     cudaStream_t st = (cudaStream_t)stream;

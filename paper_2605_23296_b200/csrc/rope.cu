@@ -11,7 +11,19 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTileRows = 8;
+constexpr int kMaxTileRows = 16;
+constexpr int kCtas = 4 * 148;                // resident at a time on a B200
+constexpr int kBatch = 4;                     // pieces of a thread in flight
+
+// n / d for n < 2^31 by a product: m = ceil(2^(31 + s) / d) with 2^s >= d, whose excess over the true factor is below
+// d / 2^(31 + s) <= 2^-31, so n times it never reaches the next whole number.
+struct divisor { uint32_t m, s, d; };
+divisor make_divisor(uint32_t d) {
+    uint32_t s = 0;
+    while ((1u << s) < d) ++s;
+    return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s, d};
+}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const divisor& v) { return (uint32_t)((uint64_t)n * v.m >> 31 >> v.s); }
 
 // One of the call's two tensors, strides in elements.
 struct rope_tensor {
@@ -19,29 +31,68 @@ struct rope_tensor {
     __nv_bfloat16* out;
     int64_t x_row, x_head, out_row, out_head;
     int heads, head_dim, offset, copies;      // copies: whether the elements that do not turn are copied too
+    divisor per_row, per_head;                // pieces
 };
 struct rope_args {
     const uint64_t* turns;
     const int32_t* positions;
     rope_tensor t[2];
-    int rows, R, tile_rows, tensors;
+    int rows, R, tile_rows, tensors, turning; // turning: rotated pieces per head
+    divisor half;
     float amplitude, sign;
 };
 
+__device__ __forceinline__ uint4 ld_once(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
 // Pieces: with VEC eight elements and 16 bytes, else one; a rotated piece of the half layout has its partner R/2 behind it.
+template <bool VEC> struct piece { using type = uint4; };
+template <> struct piece<false> { using type = uint32_t; };
+template <bool VEC> __device__ __forceinline__ typename piece<VEC>::type load_piece(const __nv_bfloat16* p);
+template <> __device__ __forceinline__ uint4 load_piece<true>(const __nv_bfloat16* p) { return ld_once(p); }
+template <> __device__ __forceinline__ uint32_t load_piece<false>(const __nv_bfloat16* p) { return ld_u16(p); }
+__device__ __forceinline__ void store_piece(__nv_bfloat16* p, const uint4& v) { *reinterpret_cast<uint4*>(p) = v; }
+__device__ __forceinline__ void store_piece(__nv_bfloat16* p, uint32_t v) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)v; }
+
+__device__ __forceinline__ void turn_halves(uint4& lo, uint4& hi, const float2* c) {
+    uint32_t u[4] = {lo.x, lo.y, lo.z, lo.w}, v[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float4 cc = *reinterpret_cast<const float4*>(c + 2 * k);
+        const float2 c0 = make_float2(cc.x, cc.y), c1 = make_float2(cc.z, cc.w);
+        const float u0 = bf_lo(u[k]), u1 = bf_hi(u[k]), v0 = bf_lo(v[k]), v1 = bf_hi(v[k]);
+        u[k] = bf_pack(turn_first(u0, v0, c0), turn_first(u1, v1, c1));
+        v[k] = bf_pack(turn_second(u0, v0, c0), turn_second(u1, v1, c1));
+    }
+    lo = make_uint4(u[0], u[1], u[2], u[3]);
+    hi = make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void turn_halves(uint32_t& lo, uint32_t& hi, const float2* c) {
+    const uint32_t w = rope_turn(lo | hi << 16, *c);
+    lo = w & 0xFFFFu;
+    hi = w >> 16;
+}
+__device__ __forceinline__ void turn_pairs(uint4& v, const float2* c) {
+    const float4 a = *reinterpret_cast<const float4*>(c), b = *reinterpret_cast<const float4*>(c + 2);
+    v = make_uint4(rope_turn(v.x, make_float2(a.x, a.y)), rope_turn(v.y, make_float2(a.z, a.w)), rope_turn(v.z, make_float2(b.x, b.y)),
+                   rope_turn(v.w, make_float2(b.z, b.w)));
+}
+
 template <bool HALF, bool VEC>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ rope_args a) {
-    extern __shared__ float2 cs[];            // [tile rows][R / 2]
-    constexpr int E = VEC ? 8 : 1;            // elements per piece
-    const int half = a.R / 2;
+__global__ void __launch_bounds__(kThreads, 4) rope_kernel(const __grid_constant__ rope_args a) {
+    extern __shared__ __align__(16) float2 cs[];          // [tile rows][R / 2]
+    constexpr int E = VEC ? 8 : 1;                        // elements per piece
+    constexpr bool TWO = HALF || !VEC;                    // a rotated item has two pieces: its partner's too
+    const int half = a.R / 2, partner = HALF ? half : 1;
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    const int turning = HALF ? half / E : VEC ? a.R / 8 : half;          // rotated pieces per head
     for (int64_t r0 = (int64_t)blockIdx.x * a.tile_rows; r0 < a.rows; r0 += (int64_t)gridDim.x * a.tile_rows) {
         const int n = (int)min((int64_t)a.tile_rows, a.rows - r0);
         __syncthreads();
         for (int i = threadIdx.x; i < n * half; i += kThreads) {
-            const int r = i / half, p = i - r * half;
+            const int r = (int)divide(i, a.half), p = i - r * half;
             float2 v = rope_cos_sin(ld_u64(a.turns + p), ld_i32(a.positions + r0 + r), a.amplitude);
             v.y *= a.sign;
             cs[i] = v;
@@ -49,50 +100,44 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
         __syncthreads();
         for (int which = 0; which < a.tensors; ++which) {
             const rope_tensor& t = a.t[which];
-            const int rest = t.copies ? (t.head_dim - a.R) / E : 0, per_head = turning + rest, per_row = t.heads * per_head;
-            for (int i = threadIdx.x; i < n * per_row; i += kThreads) {
-                const int r = i / per_row, j = i - r * per_row, h = j / per_head, p = j - h * per_head;
-                const __nv_bfloat16* x = t.x + (r0 + r) * t.x_row + h * t.x_head;
-                __nv_bfloat16* o = t.out + (r0 + r) * t.out_row + h * t.out_head;
-                if (p >= turning) {
-                    int e = (p - turning) * E;
-                    if (e >= t.offset) e += a.R;
-                    if (VEC) *reinterpret_cast<uint4*>(o + e) = ld_v4(x + e);
-                    else *reinterpret_cast<uint16_t*>(o + e) = (uint16_t)ld_u16(x + e);
-                    continue;
-                }
-                const float2* c = cs + r * half;
-                if (HALF) {
-                    const int e = t.offset + p * E;
-                    if (VEC) {
-                        const uint4 u = ld_v4(x + e), v = ld_v4(x + e + half);
-                        const uint32_t lo[4] = {u.x, u.y, u.z, u.w}, hi[4] = {v.x, v.y, v.z, v.w};
-                        uint32_t ol[4], oh[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float2 c0 = c[p * 8 + 2 * k], c1 = c[p * 8 + 2 * k + 1];
-                            const float u0 = bf_lo(lo[k]), u1 = bf_hi(lo[k]), v0 = bf_lo(hi[k]), v1 = bf_hi(hi[k]);
-                            ol[k] = bf_pack(turn_first(u0, v0, c0), turn_first(u1, v1, c1));
-                            oh[k] = bf_pack(turn_second(u0, v0, c0), turn_second(u1, v1, c1));
-                        }
-                        *reinterpret_cast<uint4*>(o + e) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
-                        *reinterpret_cast<uint4*>(o + e + half) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-                    } else {
-                        const uint32_t w = rope_turn(ld_u16(x + e) | ld_u16(x + e + half) << 16, c[p]);
-                        *reinterpret_cast<uint16_t*>(o + e) = (uint16_t)w;
-                        *reinterpret_cast<uint16_t*>(o + e + half) = (uint16_t)(w >> 16);
-                    }
-                } else if (VEC) {
-                    const int e = t.offset + p * 8;
-                    const uint4 u = ld_v4(x + e);
-                    *reinterpret_cast<uint4*>(o + e) =
-                        make_uint4(rope_turn(u.x, c[p * 4]), rope_turn(u.y, c[p * 4 + 1]), rope_turn(u.z, c[p * 4 + 2]),
-                                   rope_turn(u.w, c[p * 4 + 3]));
+            const int per_row = (int)t.per_row.d, per_head = (int)t.per_head.d, total = n * per_row;
+            // item i of the tile: elements `e` (and e + partner) of a head, turned by cs[c ...], or copied where c < 0
+            struct item { const __nv_bfloat16* x; __nv_bfloat16* o; int c; };
+            auto find = [&](int i) {
+                const int r = (int)divide(i, t.per_row), j = i - r * per_row, h = (int)divide(j, t.per_head), p = j - h * per_head;
+                int e, c = -1;
+                if (p < a.turning) {
+                    e = t.offset + (HALF ? p * E : VEC ? p * 8 : p * 2);
+                    c = r * half + (HALF ? p * E : VEC ? p * 4 : p);
                 } else {
-                    const int e = t.offset + p * 2;
-                    const uint32_t w = rope_turn(ld_u16(x + e) | ld_u16(x + e + 1) << 16, c[p]);
-                    *reinterpret_cast<uint16_t*>(o + e) = (uint16_t)w;
-                    *reinterpret_cast<uint16_t*>(o + e + 1) = (uint16_t)(w >> 16);
+                    e = (p - a.turning) * E;
+                    if (e >= t.offset) e += a.R;
+                }
+                return item{t.x + (r0 + r) * t.x_row + h * t.x_head + e, t.out + (r0 + r) * t.out_row + h * t.out_head + e, c};
+            };
+            for (int i0 = threadIdx.x; i0 < total; i0 += kThreads * kBatch) {
+                item it[kBatch];
+                typename piece<VEC>::type u[kBatch], v[kBatch];
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const int i = i0 + k * kThreads;
+                    if (i >= total) continue;
+                    it[k] = find(i);
+                    u[k] = load_piece<VEC>(it[k].x);
+                    if (TWO && it[k].c >= 0) v[k] = load_piece<VEC>(it[k].x + partner);
+                }
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    if (i0 + k * kThreads >= total) continue;
+                    if (it[k].c >= 0) {
+                        if constexpr (TWO) {
+                            turn_halves(u[k], v[k], cs + it[k].c);
+                            store_piece(it[k].o + partner, v[k]);
+                        } else {
+                            turn_pairs(u[k], cs + it[k].c);
+                        }
+                    }
+                    store_piece(it[k].o, u[k]);
                 }
             }
         }
@@ -121,7 +166,7 @@ int make_tensor(const cpa_rope_rows* s, int R, int64_t rows, rope_tensor* t) {
     if (hs < s->head_dim || (rows > 1 && rs < s->head_dim)) return CPA_EINVAL;
     if (rows > 1 && rs < (s->heads - 1) * hs + s->head_dim && hs < (rows - 1) * rs + s->head_dim) return CPA_EINVAL;
     *t = {static_cast<const __nv_bfloat16*>(s->x), static_cast<__nv_bfloat16*>(s->out), s->x_row_stride, s->x_head_stride,
-          s->out_row_stride, s->out_head_stride, s->heads, s->head_dim, s->offset, in_place ? 0 : 1};
+          s->out_row_stride, s->out_head_stride, s->heads, s->head_dim, s->offset, in_place ? 0 : 1, {}, {}};
     return CPA_OK;
 }
 
@@ -184,8 +229,19 @@ extern "C" int cpa_rope(const cpa_rope_config* cfg, const uint64_t* d_turns, con
     a.R = cfg->rope_dim;
     a.amplitude = (float)cfg->amplitude;
     a.sign = inverse ? -1.f : 1.f;
-    a.tile_rows = (int)std::min<int64_t>(kMaxTileRows, std::max<int64_t>(1, num_rows / 592));
-    const int grid = (int)std::min<int64_t>(((int64_t)num_rows + a.tile_rows - 1) / a.tile_rows, 148 * 8);
+    // Rows per tile: enough to fill the batches of a CTA's threads, but no fewer CTAs than the card holds while there are rows
+    // for them (one token of 192 sequences: 192 CTAs of a row).
+    a.tile_rows = (int)std::min<int64_t>(kMaxTileRows, std::max<int64_t>(1, num_rows / kCtas));
+    const int E = vec ? 8 : 1;
+    a.turning = half ? a.R / 2 / E : vec ? a.R / 8 : a.R / 2;
+    a.half = make_divisor((uint32_t)a.R / 2);
+    for (int i = 0; i < a.tensors; ++i) {
+        rope_tensor& t = a.t[i];
+        const uint32_t per_head = (uint32_t)(a.turning + (t.copies ? (t.head_dim - a.R) / E : 0));
+        t.per_head = make_divisor(per_head);
+        t.per_row = make_divisor(per_head * (uint32_t)t.heads);
+    }
+    const int grid = (int)std::min<int64_t>(((int64_t)num_rows + a.tile_rows - 1) / a.tile_rows, kCtas);
     auto kernel = half ? (vec ? rope_kernel<true, true> : rope_kernel<true, false>)
                        : (vec ? rope_kernel<false, true> : rope_kernel<false, false>);
     return q8_launch_smem(kernel, grid, kThreads, a.tile_rows * a.R / 2 * 8, (cudaStream_t)stream, a);
