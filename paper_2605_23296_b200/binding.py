@@ -198,6 +198,18 @@ def _ptr(x) -> Optional[int]:
     return x.data_ptr()
 
 
+def _bf16():
+    """torch.bfloat16, of the torch that the caller's tensors come from."""
+    global _torch_bf16
+    if _torch_bf16 is None:
+        import torch
+        _torch_bf16 = torch.bfloat16
+    return _torch_bf16
+
+
+_torch_bf16 = None
+
+
 def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
@@ -487,14 +499,15 @@ def cpa_rope_turns(cfg: cpa_rope_config, check: bool = True):
 def rope_rows(x, out=None, rope_dim: int = 0, offset: Optional[int] = None) -> cpa_rope_rows:
     """The rows of a tensor [rows, heads, head_dim] (any strides but the last), for cpa_rope: into `out` (None: in place), the
     rotated part at `offset`, or the last `rope_dim` elements of every head."""
-    out = x if out is None else out
-    for t in (x, out):
-        if t.dim() != 3 or str(t.dtype) != "torch.bfloat16" or (t.numel() and t.shape[2] > 1 and t.stride(2) != 1) or t.shape != x.shape:
-            raise ValueError(f"bf16 [rows, heads, head_dim] with whole heads is wanted, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
-    if out.device != x.device:
-        raise ValueError(f"out lies on {out.device}, x on {x.device}")
-    return cpa_rope_rows(x.data_ptr(), out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), x.shape[1], x.shape[2],
-                         x.shape[2] - rope_dim if offset is None else offset)
+    if out is None:
+        out = x
+    shape, xs, os = x.shape, x.stride(), out.stride()
+    if (len(shape) != 3 or x.dtype is not _bf16() or out.dtype is not x.dtype or out.shape != shape or out.device != x.device or
+            ((xs[2] != 1 or os[2] != 1) and shape[2] > 1 and x.numel())):
+        raise ValueError(f"bf16 [rows, heads, head_dim] with whole heads, x and out alike, is wanted, not {x.dtype} {tuple(shape)}, "
+                         f"strides {xs}, on {x.device} and {out.dtype} {tuple(out.shape)}, strides {os}, on {out.device}")
+    return cpa_rope_rows(x.data_ptr(), out.data_ptr(), xs[0], xs[1], os[0], os[1], shape[1], shape[2],
+                         shape[2] - rope_dim if offset is None else offset)
 
 
 def cpa_rope(cfg: cpa_rope_config, d_turns, d_positions, num_rows: int, q: cpa_rope_rows, k: Optional[cpa_rope_rows] = None,
@@ -528,11 +541,17 @@ def cpa_latent_append(cfg: cpa_latent_config, dims: cpa_table_dims, d_tables, ro
 
 def latent_io(q_latent, q_rope, o) -> cpa_latent_io:
     """Queries [B, heads, latent_dim] and [B, heads, 64] and outputs [B, heads, latent_dim] (any strides but the last)."""
-    for t in (q_latent, q_rope, o):
-        if t.dim() != 3 or str(t.dtype) != "torch.bfloat16" or t.stride(2) != 1 or t.shape[:2] != q_latent.shape[:2]:
-            raise ValueError(f"bf16 [blocks, heads, elements] with whole heads is wanted, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
-    return cpa_latent_io(q_latent.data_ptr(), q_latent.stride(0), q_latent.stride(1), q_rope.data_ptr(), q_rope.stride(0),
-                         q_rope.stride(1), o.data_ptr(), o.stride(0), o.stride(1))
+    try:
+        (B, H, L), (b, h, r), bf16 = q_latent.shape, q_rope.shape, q_latent.dtype
+        (qb, qh, q1), (rb, rh, r1), (ob, oh, o1) = q_latent.stride(), q_rope.stride(), o.stride()
+        fine = (bf16 is _bf16() and q_rope.dtype is bf16 and o.dtype is bf16 and q1 == r1 == o1 == 1 and b == B and h == H and r == 64 and
+                o.shape == q_latent.shape)
+    except ValueError:
+        fine = False
+    if not fine:
+        raise ValueError("bf16 [blocks, heads, elements] with whole heads is wanted, not " + ", ".join(
+            f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}" for t in (q_latent, q_rope, o)))
+    return cpa_latent_io(q_latent.data_ptr(), qb, qh, q_rope.data_ptr(), rb, rh, o.data_ptr(), ob, oh)
 
 
 def cpa_latent_decode_workspace_bytes(cfg: cpa_latent_config) -> int:

@@ -11,15 +11,17 @@
 // on two CTAs that walk the same tokens.
 //
 // A CTA owns an equal share of all blocks' 64-token tiles, cut on the device from the lengths; a block that is cut leaves
-// partial sums in the workspace, which a second kernel joins.  Twelve warps with fixed roles:
-//   0-3   softmax: warp w holds tokens 16 w .. 16 w + 15 of a tile in the fragment layout of a 16-lane TMEM load; epilogue
-//   4-7   queries of the next segment into shared memory (turned, if asked for), a step's new row; rows of zeros
-//   8     TMA producer, one lane per page of a tile
-//   9     issuer of the score products; owner of the tensor memory
-//   10    issuer of the output products (a warp of its own, so that neither product waits behind the other's operands)
-//   11    walks the blocks and hands out the segments (block, first tile, tiles)
-// The reference m of a head stays as long as no score passes it by more than 2^8 (what it is cancels in the division); all
-// four softmax warps learn of that by one barrier with an OR, so a tile usually costs no exchange of maxima at all.
+// partial sums in the workspace, which a second kernel joins.  Sixteen warps with fixed roles:
+//   0-3   softmax of the first half of the heads: warp w holds tokens 16 w .. 16 w + 15 of a tile in the fragment layout of a
+//         16-lane TMEM load; epilogue of the same heads
+//   4-7   the same for the second half
+//   8-11  queries of the next segment into shared memory (turned, if asked for), a step's new row; rows of zeros
+//   12    TMA producer, one lane per page of a tile
+//   13    issuer of the score products; owner of the tensor memory
+//   14    issuer of the output products (a warp of its own, so that neither product waits behind the other's operands)
+//   15    walks the blocks and hands out the segments (block, first tile, tiles)
+// The reference m of a head stays as long as no score passes it by more than 2^8 (what it is cancels in the division); the
+// four warps of a half learn of that by one barrier with an OR, so a tile usually costs no exchange of maxima at all.
 //
 // Every mbarrier wait is bounded: when one gives up the CTA records it in the status word, stops waiting, still frees its
 // tensor memory and returns.
@@ -33,7 +35,7 @@ namespace {
 
 constexpr int kTile = 64;                       // tokens per tile
 constexpr int kTilePages = kTile / kPage;
-constexpr int kDecodeThreads = 384;
+constexpr int kDecodeThreads = 512;
 constexpr int kSms = 148;                       // of a B200; CTAs do not wait for one another, so any device will do
 constexpr int kSegRing = 4;
 constexpr int kMaxDecodeStages = 6;
@@ -102,7 +104,7 @@ struct DecodeShared {
     DecodeBarriers bars;
     segment seg[kSegRing];
     float2 turn[kRopeDim / 2];
-    float column[4][N];               // per warp and head: maxima, sums
+    float column[8][N / 2];           // per warp and head: maxima, sums
     float factor[N];
     int64_t scan[kDecodeThreads / 32];
     int64_t start_cost;
@@ -162,6 +164,13 @@ __device__ __forceinline__ void sync_128(int id) { asm volatile("barrier.cta.syn
 // Columns of 16 lanes in fragment layout: per 8 columns four words, of lane / 4 (words 0, 1) and lane / 4 + 8 (words 2, 3),
 // columns 2 (lane % 4) and the next.
 template <int N> __device__ __forceinline__ void tc_ld_frag(uint32_t taddr, float (&v)[N / 2]);
+template <> __device__ __forceinline__ void tc_ld_frag<8>(uint32_t taddr, float (&v)[4]) {
+    uint32_t r[4];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+}
 template <> __device__ __forceinline__ void tc_ld_frag<16>(uint32_t taddr, float (&v)[8]) {
     uint32_t r[8];
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
@@ -178,20 +187,6 @@ template <> __device__ __forceinline__ void tc_ld_frag<32>(uint32_t taddr, float
     tc_wait_ld();
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-template <> __device__ __forceinline__ void tc_ld_frag<64>(uint32_t taddr, float (&v)[32]) {
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr) : "memory");
-    tc_wait_ld();
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 // 16 columns of this thread's lane
 __device__ __forceinline__ void tc_ld16(uint32_t taddr, float (&v)[16]) {
@@ -237,24 +232,24 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(&bars.s_full[i]), 1);
-            mbar_init(bar(&bars.s_empty[i]), 4);
+            mbar_init(bar(&bars.s_empty[i]), 8);
         }
-        mbar_init(bar(&bars.p_full), 4);
+        mbar_init(bar(&bars.p_full), 8);
         mbar_init(bar(&bars.pv_done), 1);
-        mbar_init(bar(&bars.q_full), a.turns ? 5 : 4);      // warps 4-7, and the copies beside what warp 5 turns
+        mbar_init(bar(&bars.q_full), a.turns ? 5 : 4);      // warps 8-11, and the copies beside what warp 9 turns
         mbar_init(bar(&bars.q_empty), 1);
-        mbar_init(bar(&bars.o_empty), 4);
+        mbar_init(bar(&bars.o_empty), 8);
         mbar_init(bar(&bars.row_ready), 1);
         mbar_init(bar(&bars.drain_s), 1);
         mbar_init(bar(&bars.drain_p), 1);
         for (int i = 0; i < kSegRing; ++i) {
             mbar_init(bar(&bars.seg_full[i]), 1);
-            mbar_init(bar(&bars.seg_empty[i]), 11);      // every warp but the one that hands out
+            mbar_init(bar(&bars.seg_empty[i]), 15);      // every warp but the one that hands out
         }
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     }
-    if (warp == 9) {
+    if (warp == 13) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" :: "r"(smem_u32(&bars.tmem_base)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
@@ -320,7 +315,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         return s;
     };
 
-    if (warp == 11) {
+    if (warp == 15) {
         // ------------------------------------------------------------ segments
         int n = 0;
         int2 cut = make_int2(-1, 0);
@@ -364,7 +359,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         const uint32_t has = __ballot_sync(0xffffffffu, cut.x >= 0);
         const int who = has ? __ffs(has) - 1 : 0;
         if (hg == 0 && lane == who) a.cuts[group] = cut;
-    } else if (warp == 8) {
+    } else if (warp == 12) {
         // ------------------------------------------------------------ TMA producer, a lane per page
         int it = 0, fresh = 0;
         for (int i = 0;; ++i) {
@@ -403,7 +398,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         if (__any_sync(0xffffffffu, dead) && lane == 0)
             for (int s = 0; s < kStages; ++s)
                 for (uint32_t par = 0; par < 2; ++par) mbar_drain(bar(&bars.kv_full[s]), par, kDrainLimit);
-    } else if (warp == 9) {
+    } else if (warp == 13) {
         // ------------------------------------------------------------ score products, by one lane
         constexpr uint32_t idesc = instr_desc(kTile, N, false);
         const uint64_t da = smem_desc(s_kv, 16, nc * 1024), db = smem_desc(s_q, 16, 1024);
@@ -438,7 +433,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             tc_commit_one(bar(&bars.drain_s));
             mbar_drain(bar(&bars.drain_s), 0u, kDrainLimit);
         }
-    } else if (warp == 10) {
+    } else if (warp == 14) {
         // ------------------------------------------------------------ output products, by one lane
         constexpr uint32_t idesc = instr_desc(128, N, true) | (1u << 15);       // both operands MN-major
         const uint64_t da = smem_desc(s_kv, 1024, nc * 1024), db = smem_desc(s_p, 16, 1024);
@@ -478,20 +473,20 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             tc_commit_one(bar(&bars.drain_p));
             mbar_drain(bar(&bars.drain_p), 0u, kDrainLimit);
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 8) {
         // ------------------------------------------------------------ queries, a step's new row, rows of zeros
         // (loops are kept short: what a launch runs once or twice costs the fetching of its instructions)
         constexpr int latent_pieces = L / 8;           // 16-byte pieces of a row's latent part
-        const int tid = threadIdx.x - 128;
+        const int tid = threadIdx.x - 256;
         auto q_at = [&](int h, int p) {                // where piece p of head h's positional part lies (swizzled)
             return reinterpret_cast<uint4*>(gen + (s_q - base) + (nc - 1) * (N * 128) + h * 128 + ((p ^ (h & 7)) << 4));
         };
         for (int i = 0;; ++i) {
             const segment g = get_segment(i);
-            if (any_of_128(2, g.block < 0)) break;
+            if (any_of_128(3, g.block < 0)) break;
             const int position = (a.first ? ld_i32(a.first + g.block) : 0) + g.len - 1;
             if (i > 0) wait(&bars.q_empty, (uint32_t)(i - 1) & 1u);
-            if (warp == 5) {
+            if (warp == 9) {
                 // the latent parts, and the positional ones that do not turn; heads behind the last are filled with zeros
                 if (lane == 0 && !dead) {
                     mbar_expect_tx(bar(&bars.q_full), Sh::kQBytes - (a.turns ? N * 128 : 0));
@@ -516,7 +511,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                         y[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * (r + 4));
                     }
                 }
-                sync_128(2);
+                sync_128(3);
 #pragma unroll
                 for (int k = 0; k < kRounds; ++k) {
                     const int h = (tid >> 2) + 32 * k;
@@ -543,10 +538,10 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                 __syncwarp();
             }
-            if (lane == 0 && warp != 5) mbar_arrive(bar(&bars.q_full));
-            if (lane == 0 && warp == 5 && a.turns) mbar_arrive(bar(&bars.q_full));
+            if (lane == 0 && warp != 9) mbar_arrive(bar(&bars.q_full));
+            if (lane == 0 && warp == 9 && a.turns) mbar_arrive(bar(&bars.q_full));
             // (the last growing segment's row has been loaded: its scores are through, or these queries could not have been stored)
-            if (warp == 4 && a.x && (g.tile0 + g.tiles) * (int64_t)kTile >= g.len) {
+            if (warp == 8 && a.x && (g.tile0 + g.tiles) * (int64_t)kTile >= g.len) {
                 put_new_row<L>(a.x + g.block * a.x_row, new_row_of(a), position, slot_of<L>(a, g), lane);
                 asm volatile("fence.proxy.async;\n" ::: "memory");
                 __syncwarp();
@@ -563,13 +558,16 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         }
     } else {
         // ------------------------------------------------------------ softmax and epilogue
-        constexpr int J = N / 8;               // groups of eight heads; this thread has two heads and two tokens of each
-        const int token = 16 * warp + (lane >> 2), col = 2 * (lane & 3);
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        constexpr int NH = N / 2, J = NH / 8;  // heads of a half; groups of eight, of which this thread has two heads and two tokens
+        const int which = warp >> 2, quarter = warp & 3, id = 1 + which, h1 = which * NH;
+        const int token = 16 * quarter + (lane >> 2), col = 2 * (lane & 3);
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        float (*column)[NH] = sm.column + 4 * which;
+        float* factor = sm.factor + h1;
         int it = 0;
         for (int i = 0;; ++i) {
             const segment g = get_segment(i);
-            if (any_of_128(1, g.block < 0)) break;
+            if (any_of_128(id, g.block < 0)) break;
             float m[2 * J], l[2 * J];
 #pragma unroll
             for (int k = 0; k < 2 * J; ++k) { m[k] = kLowest; l[k] = 0.f; }
@@ -578,7 +576,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 wait(&bars.s_full[it & 1], (uint32_t)(it >> 1) & 1u);
                 tc_fence_after();
                 float s[4 * J];
-                tc_ld_frag<N>(tmem + lanes + (it & 1) * N, s);
+                tc_ld_frag<NH>(tmem + lanes + (it & 1) * N + h1, s);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(&bars.s_empty[it & 1]));
@@ -591,7 +589,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                     // rows behind the length hold anything, and their weights of zero would not silence an infinity or a NaN
                     constexpr int row16 = L / 8;
                     const int stage = it % kStages;
-                    for (int e = threadIdx.x; e < (kTile - valid) * row16; e += 128) {
+                    for (int e = threadIdx.x; e < (kTile - valid) * row16; e += 256) {
                         const int t = valid + e / row16, p = e % row16;
                         *reinterpret_cast<uint4*>(gen + stage * kTileBytes64 + (t >> 3) * (nc * 1024) + (p >> 3) * 1024 + (t & 7) * 128 +
                                                   ((p & 7) << 4)) = make_uint4(0, 0, 0, 0);
@@ -600,17 +598,17 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 if (j == 0) {
                     // The first reference: the first token's score and a margin (with N(0, 2^2) scores the largest of a long block
                     // is then mostly within 2^8 of it); the true maximum takes over where it is not.
-                    if (warp == 0 && lane < 4)
+                    if (quarter == 0 && lane < 4)
 #pragma unroll
                         for (int k = 0; k < J; ++k)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) sm.factor[8 * k + col + e] = s[4 * k + e];
-                    sync_128(1);
+                            for (int e = 0; e < 2; ++e) factor[8 * k + col + e] = s[4 * k + e];
+                    sync_128(id);
 #pragma unroll
                     for (int k = 0; k < J; ++k)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float x = fmaf(sm.factor[8 * k + col + e], a.scale_log2, kFirstMargin);
+                            const float x = fmaf(factor[8 * k + col + e], a.scale_log2, kFirstMargin);
                             m[2 * k + e] = fabsf(x) < 1e38f ? x : kLowest;
                         }
                 }
@@ -619,8 +617,8 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 for (int k = 0; k < J; ++k)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) high |= fmaf(s[4 * k + e], a.scale_log2, -m[2 * k + (e & 1)]) > 8.f;
-                if (any_of_128(1, high || dead)) {
-                    if (any_of_128(1, dead)) { dead = true; break; }
+                if (any_of_128(id, high || dead)) {
+                    if (any_of_128(id, dead)) { dead = true; break; }
                     // some score is far above its head's reference: new references, and what was summed so far is scaled to them
 #pragma unroll
                     for (int k = 0; k < J; ++k)
@@ -630,15 +628,15 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                            if (lane < 4) sm.column[warp][8 * k + col + e] = x;
+                            if (lane < 4) column[quarter][8 * k + col + e] = x;
                         }
-                    sync_128(1);
+                    sync_128(id);
 #pragma unroll
                     for (int k = 0; k < J; ++k)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const int h = 8 * k + col + e;
-                            const float x = a.scale_log2 * fmaxf(fmaxf(sm.column[0][h], sm.column[1][h]), fmaxf(sm.column[2][h], sm.column[3][h]));
+                            const float x = a.scale_log2 * fmaxf(fmaxf(column[0][h], column[1][h]), fmaxf(column[2][h], column[3][h]));
                             float& r = m[2 * k + e];
                             float f = 1.f;
                             if (x - r > 8.f) {
@@ -646,19 +644,20 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                                 r = x;
                             }
                             l[2 * k + e] *= f;
-                            if (warp == 0 && lane < 4) sm.factor[h] = f;
+                            if (quarter == 0 && lane < 4) factor[h] = f;
                         }
-                    sync_128(1);
+                    sync_128(id);
                     if (j > 0) {
                         wait(&bars.pv_done, (uint32_t)(it - 1) & 1u);
                         tc_fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < nm * N; c += 8) {
+                        for (int c = 0; c < nm * NH; c += 8) {
+                            const uint32_t at = tmem + lanes + kColO + c / NH * N + h1 + c % NH;
                             float v[8];
-                            tc_ld8(tmem + lanes + kColO + c, v);
+                            tc_ld8(at, v);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] *= sm.factor[(c + e) % N];
-                            tc_st8(tmem + lanes + kColO + c, v);
+                            for (int e = 0; e < 8; ++e) v[e] *= factor[c % NH + e];
+                            tc_st8(at, v);
                         }
                         tc_wait_st();
                     }
@@ -674,14 +673,14 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                         l[2 * k] += bf_lo(w);
                         l[2 * k + 1] += bf_hi(w);
                         const int t = token + 8 * e;
-                        *reinterpret_cast<uint32_t*>(gen + (s_p - base) + t * 128 + ((k ^ (t & 7)) << 4) + 2 * col) = w;
+                        *reinterpret_cast<uint32_t*>(gen + (s_p - base) + t * 128 + (((k + which * J) ^ (t & 7)) << 4) + 2 * col) = w;
                     }
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(&bars.p_full));
             }
-            if (any_of_128(1, dead)) break;
+            if (any_of_128(id, dead)) break;
             // ---- the segment's end: sums over the tokens, then the outputs or the partial
 #pragma unroll
             for (int k = 0; k < 2 * J; ++k) {
@@ -689,44 +688,47 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 x += __shfl_xor_sync(0xffffffffu, x, 4);
                 x += __shfl_xor_sync(0xffffffffu, x, 8);
                 x += __shfl_xor_sync(0xffffffffu, x, 16);
-                if (lane < 4) sm.column[warp][8 * (k >> 1) + col + (k & 1)] = x;
+                if (lane < 4) column[quarter][8 * (k >> 1) + col + (k & 1)] = x;
             }
-            sync_128(1);
-            const int64_t part = ((int64_t)g.slot * a.head_groups + hg) * 64;
-            if (warp == 0 && lane < 4)
+            sync_128(id);
+            const int64_t part = ((int64_t)g.slot * a.head_groups + hg) * 64 + h1;
+            const int own = heads - h1;            // heads of this half
+            if (quarter == 0 && lane < 4)
 #pragma unroll
                 for (int k = 0; k < 2 * J; ++k) {
                     const int h = 8 * (k >> 1) + col + (k & 1);
-                    const float x = (sm.column[0][h] + sm.column[1][h]) + (sm.column[2][h] + sm.column[3][h]);
-                    sm.factor[h] = g.slot < 0 ? 1.f / x : 1.f;
-                    if (g.slot >= 0 && h < heads) a.part_ml[part + h] = make_float2(m[k], x);
+                    const float x = (column[0][h] + column[1][h]) + (column[2][h] + column[3][h]);
+                    factor[h] = g.slot < 0 ? 1.f / x : 1.f;
+                    if (g.slot >= 0 && h < own) a.part_ml[part + h] = make_float2(m[k], x);
                 }
             wait(&bars.pv_done, (uint32_t)(it - 1) & 1u);
-            dead = any_of_128(1, dead);
+            dead = any_of_128(id, dead);
             tc_fence_after();
 #pragma unroll 1
             for (int mb = 0; mb < nm; ++mb) {
-                const int dim = mb * 128 + 32 * warp + lane;
-                __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + g.block * a.io.o_block_stride + h0 * a.io.o_head_stride + (dim & ~1);
+                const int dim = mb * 128 + 32 * quarter + lane;
+                __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + g.block * a.io.o_block_stride + (h0 + h1) * a.io.o_head_stride + (dim & ~1);
+                constexpr int W = NH < 16 ? NH : 16;
 #pragma unroll
-                for (int c = 0; c < N; c += 16) {
-                    float v[16];
-                    tc_ld16(tmem + lanes + kColO + mb * N + c, v);
+                for (int c = 0; c < NH; c += W) {
+                    float v[W];
+                    if constexpr (W == 16) tc_ld16(tmem + lanes + kColO + mb * N + h1 + c, v);
+                    else tc_ld8(tmem + lanes + kColO + mb * N + h1 + c, v);
                     if (dead) continue;
                     if (g.slot >= 0) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (c + e < heads) a.part_o[(part + c + e) * L + dim] = v[e];
+                        for (int e = 0; e < W; ++e)
+                            if (c + e < own) a.part_o[(part + c + e) * L + dim] = v[e];
                     } else {
                         // two heads at a time: an even lane takes its own and its neighbour's element of the first, an odd one
                         // of the second
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const float x = mul_keep(v[e], sm.factor[c + e]), y = mul_keep(v[e + 1], sm.factor[c + e + 1]);
+                        for (int e = 0; e < W; e += 2) {
+                            const float x = mul_keep(v[e], factor[c + e]), y = mul_keep(v[e + 1], factor[c + e + 1]);
                             const float other = __shfl_xor_sync(0xffffffffu, (lane & 1) ? x : y, 1);
                             const uint32_t w = (lane & 1) ? bf_pack(other, y) : bf_pack(x, other);
                             const int h = c + e + (lane & 1);
-                            if (h < heads) *reinterpret_cast<uint32_t*>(o + h * a.io.o_head_stride) = w;
+                            if (h < own) *reinterpret_cast<uint32_t*>(o + h * a.io.o_head_stride) = w;
                         }
                     }
                 }
@@ -739,7 +741,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == 13) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" :: "r"(tmem) : "memory");
     }
