@@ -40,7 +40,7 @@ constexpr int kSms = 148;                       // of a B200; CTAs do not wait f
 constexpr int kSegRing = 4;
 constexpr int kMaxDecodeStages = 6;
 constexpr int kBlockCost = 1;                   // what a block costs beside its tiles, in tiles (its queries, its output)
-constexpr int kMinRange = 4;                    // cost of a CTA's share, at least
+constexpr int kMinRange = 2;                    // cost of a CTA's share, at least: a tile and its block's own (4 blocks of 96..288 tokens: 11.3 us; 14.4 with 4)
 constexpr float kLowest = -3e38f, kFirstMargin = 6.f;
 constexpr uint32_t kPBytes = kTile * 128;
 constexpr int kMaxSmem = 232448;                // 227 KB, what a CTA can have on sm_100
@@ -748,26 +748,30 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 }
 
 // ---------------------------------------------------------------- joining a cut block's parts
-// One unit = 128 elements of a (cut block, head), four per lane of a warp; factors 2^(m_k - m) of the parts' references.  Up to
-// kFewParts parts a warp takes a unit by itself, with all its loads in flight at once; if any block has more, a CTA's eight warps
-// share a unit's parts.  (Short code: it runs once, so fetching its instructions is part of its time.)
-constexpr int kJoinWarps = 8, kFewParts = 8, kJoinCtas = 8 * kSms;
-__device__ __forceinline__ void add_part(float4& v, const uint4& w, float f) {
+// One unit = 128 elements of a (cut block, head), four per lane of a warp.  Where no block has more than kFewParts parts a warp
+// takes a unit by itself, else a CTA's eight warps share a unit's parts.  (Short code: it runs once or twice per launch, so
+// fetching its instructions is part of its time.)
+constexpr int kJoinWarps = 8, kFewParts = 8, kJoinBatch = 4, kJoinPerSm = 4;
+__device__ __forceinline__ void scale_part(float4& v, float& l, float f) {
+    v.x *= f; v.y *= f; v.z *= f; v.w *= f; l *= f;
+}
+__device__ __forceinline__ void add_part(float4& v, float& l, const uint4& w, float wl, float f) {
     v.x = fmaf(f, __uint_as_float(w.x), v.x);
     v.y = fmaf(f, __uint_as_float(w.y), v.y);
     v.z = fmaf(f, __uint_as_float(w.z), v.z);
     v.w = fmaf(f, __uint_as_float(w.w), v.w);
+    l = fmaf(f, wl, l);
 }
 __device__ __forceinline__ float2 ld_f2(const float2* p) {
     float2 v;
     asm volatile("ld.global.v2.f32 {%0,%1}, [%2];\n" : "=f"(v.x), "=f"(v.y) : "l"(p));
     return v;
 }
-__global__ void __launch_bounds__(kJoinWarps * 32) latent_join_kernel(const __grid_constant__ decode_args a) {
+__global__ void __launch_bounds__(kJoinWarps * 32, kJoinPerSm) latent_join_kernel(const __grid_constant__ decode_args a) {
     __shared__ int list[3][kSms];             // block, parts, group
     __shared__ int count[kJoinWarps];
-    __shared__ float4 acc[kJoinWarps][32];
-    __shared__ float factor[kSms + 1];
+    __shared__ uint4 acc[kJoinWarps][32];
+    __shared__ float2 sums[kJoinWarps];
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -783,87 +787,71 @@ __global__ void __launch_bounds__(kJoinWarps * 32) latent_join_kernel(const __gr
         if (w < warp) at += count[w];
         n_list += count[w];
     }
-    if (cut.x >= 0) { list[0][at] = cut.x; list[1][at] = cut.y; list[2][at] = (int)threadIdx.x; }
+    if (cut.x >= 0) {
+        // (what the workspace says is not followed outside of it)
+        if (cut.x >= a.B || cut.y < 1 || cut.y > a.groups - (int)threadIdx.x) {
+            atomicCAS(a.t.header, 0, kStatusInvalid);
+            cut = make_int2(0, 0);
+        }
+        list[0][at] = cut.x;
+        list[1][at] = cut.y;
+        list[2][at] = (int)threadIdx.x;
+    }
     __syncthreads();
     const int quarters = a.L / 128, units = a.H * quarters;      // per cut block
     const int per = shared ? units : (units + kJoinWarps - 1) / kJoinWarps, n_work = n_list * per;
     for (int work = blockIdx.x; work < n_work; work += gridDim.x) {
         const int c = work / per, unit = shared ? work - c * per : (work - c * per) * kJoinWarps + warp;
         const int n = list[1][c], g0 = list[2][c];
+        if (n < 1) continue;
         const bool on = unit < units;
         const int head = on ? unit / quarters : 0, e = (on ? unit % quarters : 0) * 128 + lane * 4;
         const int hg = head / a.group_heads;
         const int64_t step = 2 * (int64_t)a.head_groups * 64, row0 = ((int64_t)(2 * g0 + 1) * a.head_groups + hg) * 64 + head - hg * a.group_heads,
                       row1 = row0 - (int64_t)a.head_groups * 64;            // part 0; part k > 0 is at row1 + k * step
-        auto row = [&](int k) { return k == 0 ? row0 : row1 + k * step; };
+        // the parts of this warp, a batch in flight at a time, with a running reference
+        const int k0 = shared ? warp : 0, dk = shared ? kJoinWarps : 1;
+        float m = kLowest, l = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        float sum = 0.f;
-        if (!shared) {
-            uint4 w[kFewParts];
+        for (int k = k0; k < n; k += kJoinBatch * dk) {
+            float2 ml[kJoinBatch];
+            uint4 w[kJoinBatch];
 #pragma unroll
-            for (int k = 0; k < kFewParts; ++k) {
-                w[k] = make_uint4(0, 0, 0, 0);
-                if (k < n) w[k] = ld_v4(a.part_o + row(k) * a.L + e);
+            for (int i = 0; i < kJoinBatch; ++i) {
+                const int at = k + i * dk;
+                ml[i] = make_float2(kLowest, 0.f);
+                w[i] = make_uint4(0, 0, 0, 0);
+                if (at < n) {
+                    const int64_t row = at == 0 ? row0 : row1 + at * step;
+                    w[i] = ld_v4(a.part_o + row * a.L + e);
+                    ml[i] = ld_f2(a.part_ml + row);
+                }
             }
-            float2 ml = make_float2(kLowest, 0.f);
-            if (lane < n) ml = ld_f2(a.part_ml + row(lane));
-            float top = ml.x;
+            float top = m;
 #pragma unroll
-            for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            top = __shfl_sync(0xffffffffu, top, 0);
-            const float f = exp2f(ml.x - top);
-            sum = lane < n ? f * ml.y : 0.f;
+            for (int i = 0; i < kJoinBatch; ++i) top = fmaxf(top, ml[i].x);
+            scale_part(v, l, exp2f(m - top));
+            m = top;
 #pragma unroll
-            for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            sum = __shfl_sync(0xffffffffu, sum, 0);
-#pragma unroll
-            for (int k = 0; k < kFewParts; ++k) {
-                const float fk = __shfl_sync(0xffffffffu, f, k);
-                if (k < n) add_part(v, w[k], fk);
-            }
-        } else {
+            for (int i = 0; i < kJoinBatch; ++i) add_part(v, l, w[i], ml[i].y, exp2f(ml[i].x - m));
+        }
+        if (shared) {
+            if (lane == 0) sums[warp] = make_float2(m, l);
+            acc[warp][lane] = make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w));
+            __syncthreads();
             if (warp == 0) {
-                float top = kLowest;
-                for (int k = lane; k < n; k += 32) top = fmaxf(top, ld_f32(&a.part_ml[row(k)].x));
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                for (int k = lane; k < n; k += 32) {
-                    const float2 ml = ld_f2(a.part_ml + row(k));
-                    factor[k] = exp2f(ml.x - top);
-                    sum += factor[k] * ml.y;
-                }
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                float top = m;
+                for (int k = 1; k < kJoinWarps; ++k) top = fmaxf(top, sums[k].x);
+                scale_part(v, l, exp2f(m - top));
+                for (int k = 1; k < kJoinWarps; ++k) add_part(v, l, acc[k][lane], sums[k].y, exp2f(sums[k].x - top));
             }
-            uint4 w[kFewParts];
-            int k0 = warp;
-            auto load = [&] {
-#pragma unroll
-                for (int k = 0; k < kFewParts; ++k)
-                    if (k0 + k * kJoinWarps < n) w[k] = ld_v4(a.part_o + row(k0 + k * kJoinWarps) * a.L + e);
-            };
-            load();
-            __syncthreads();
-            for (; k0 < n; k0 += kJoinWarps * kFewParts) {
-                if (k0 > warp) load();
-#pragma unroll
-                for (int k = 0; k < kFewParts; ++k)
-                    if (k0 + k * kJoinWarps < n) add_part(v, w[k], factor[k0 + k * kJoinWarps]);
-            }
-            acc[warp][lane] = v;
-            __syncthreads();
-            if (warp == 0)
-#pragma unroll 1
-                for (int k = 1; k < kJoinWarps; ++k) {
-                    const float4 x = acc[k][lane];
-                    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-                }
         }
         if (on && (!shared || warp == 0)) {
-            const float f = 1.f / sum;
+            const float f = 1.f / l;
             *reinterpret_cast<uint2*>((__nv_bfloat16*)a.io.o + list[0][c] * a.io.o_block_stride + head * a.io.o_head_stride + e) =
                 make_uint2(bf_pack(mul_keep(v.x, f), mul_keep(v.y, f)), bf_pack(mul_keep(v.z, f), mul_keep(v.w, f)));
         }
+        if (shared) __syncthreads();
     }
 }
 
@@ -1006,7 +994,7 @@ int decode(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tab
                    : s.n == 32 ? launch_latent<32>(map, a, st)
                                : launch_latent<64>(map, a, st);
     if (rc != CPA_OK) return rc;
-    return q8_launch(latent_join_kernel, kJoinCtas, kJoinWarps * 32, st, a);
+    return q8_launch(latent_join_kernel, kJoinPerSm * kSms, kJoinWarps * 32, st, a);
 }
 
 int check(const cpa_latent_config* cfg, const cpa_table_dims* dims, const void* d_tables, const cpa_latent_io* io,
