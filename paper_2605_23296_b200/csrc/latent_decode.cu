@@ -39,7 +39,7 @@ constexpr int kDecodeThreads = 512;
 constexpr int kSms = 148;                       // of a B200; CTAs do not wait for one another, so any device will do
 constexpr int kSegRing = 4;
 constexpr int kMaxDecodeStages = 6;
-constexpr int kBlockCost = 1;                   // what a block costs beside its tiles, in tiles (its queries, its output)
+constexpr int kBlockCost = 2;                   // what a block costs beside its tiles, in tiles (its queries, its output)
 constexpr int kMinRange = 2;                    // cost of a CTA's share, at least: a tile and its block's own (4 blocks of 96..288 tokens: 11.3 us; 14.4 with 4)
 constexpr float kLowest = -3e38f, kFirstMargin = 6.f;
 constexpr uint32_t kPBytes = kTile * 128;
