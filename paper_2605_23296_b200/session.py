@@ -354,3 +354,186 @@ class CompactionSession:
             self.close()
         except Exception:
             pass
+
+
+class Rotary:
+    """Rotary positions of one configuration on one device: the frequencies, computed once (cpa_rope_turns)."""
+
+    def __init__(self, rope_dim: int, interleaved: bool = False, base: float = 10000.0, scaling: int = B.ROPE_UNSCALED,
+                 factor: float = 1.0, trained_len: int = 0, fast: float = 32.0, slow: float = 1.0, amplitude: float = 1.0,
+                 device: str = "cuda:0"):
+        self.device = torch.device(device)
+        self.cfg = B.cpa_rope_config(rope_dim, B.ROPE_INTERLEAVED if interleaved else B.ROPE_HALF, scaling, trained_len, base, factor,
+                                     fast, slow, amplitude)
+        self.turns = torch.from_numpy(B.cpa_rope_turns(self.cfg).view(np.int64)).to(self.device)
+
+    def turn(self, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+             k_out: Optional[torch.Tensor] = None, inverse: bool = False, offset: Optional[int] = None) -> None:
+        """Turns the rows q [rows, heads, head_dim] and, if given, k to `positions` (int32 [rows]), in place or into q_out and
+        k_out; the rotated part is a head's last rope_dim elements, or those at `offset`.  On the current stream of the device."""
+        rows = q.shape[0]
+        if positions.dtype != torch.int32 or positions.device != self.turns.device or positions.shape != (rows,) or not positions.is_contiguous():
+            raise ValueError(f"positions: contiguous int32 [{rows}] on {self.turns.device} is wanted")
+        if q.device != positions.device or (k is not None and (k.device != positions.device or k.shape[0] != rows)):
+            raise ValueError(f"q and k: {rows} rows each on {positions.device} are wanted")
+        args = [B.rope_rows(q, q_out, self.cfg.rope_dim, offset), None if k is None else B.rope_rows(k, k_out, self.cfg.rope_dim, offset)]
+        with torch.cuda.device(self.device):
+            rc = B.cpa_rope(self.cfg, self.turns, positions, rows, *args, inverse, int(torch.cuda.current_stream(self.device).cuda_stream))
+        if rc != B.CPA_OK:
+            raise B.CpaError(rc, "cpa_rope")
+
+
+class LatentSession:
+    """A compaction event of a model with latent attention: one history cut into blocks, one summary sequence per block, the
+    cache one row [latent | positional key] per token for all heads.
+
+    Owns the plan of the prompts' prefill, the tables, the pool of rows and the decode's workspace.  All calls are enqueued on
+    the current torch stream of `device`.  As with CompactionSession's 8-bit cache the lengths live on the device: `lens` is
+    another tensor after every append and every step (read it anew; a captured graph that is replayed as a loop holds an even
+    number of such calls), and a block without room is left out, which status() reports.  `rope` turns queries and keys to
+    first[b] + their place in block b; without it they are taken as they are."""
+
+    def __init__(self, block_lens: Sequence[int], max_new_tokens: int, num_heads: int, free_pages: Sequence[int], num_pages: int,
+                 latent_dim: int = 512, scale: Optional[float] = None, rope: Optional[Rotary] = None,
+                 norm_weight: Optional[torch.Tensor] = None, norm_eps: float = 1e-6, first: Optional[Sequence[int]] = None,
+                 device: str = "cuda:0", poison_pools: bool = False, num_sms: int = 0):
+        self.device = torch.device(device)
+        self.plan = None
+        self.H, self.L, self.rope, self.norm_weight = num_heads, latent_dim, rope, norm_weight
+        self.B = len(block_lens)
+        self.block_lens = np.asarray(block_lens, dtype=np.int32)
+        self.total_tokens = int(self.block_lens.sum())
+        self.scale = float(scale if scale is not None else (128 + 64) ** -0.5)
+        if norm_weight is not None and (norm_weight.dtype != torch.bfloat16 or norm_weight.shape != (latent_dim,) or
+                                        not norm_weight.is_contiguous()):
+            raise ValueError(f"norm_weight: contiguous bf16 [{latent_dim}] is wanted")
+        self.cfg = B.cpa_latent_config(num_heads, latent_dim, 64, 128, 128, 16, self.scale, norm_eps, num_sms)
+        tables_cfg = B.cpa_latent_tables_config(self.cfg)
+        self.plan = B.cpa_plan_create(B.cpa_latent_plan_config(self.cfg), self.block_lens, max_new_tokens, free_pages)
+        self.dims = B.cpa_table_dims(self.B, max_new_tokens, num_pages, B.cpa_plan_param(self.plan, B.PARAM_PAGES_USED), 0)
+        on = dict(device=self.device)
+        self.index_buf = torch.empty(B.cpa_plan_param(self.plan, B.PARAM_INDEX_BYTES), dtype=torch.uint8, **on)
+        self.tables = torch.empty(B.cpa_tables_bytes(tables_cfg, self.dims), dtype=torch.uint8, **on)
+        self.pool = torch.empty((num_pages, 16, latent_dim + 64), dtype=torch.bfloat16, **on)
+        if poison_pools:   # unused slots hold NaN: the kernels must mask by index, not by value
+            self.pool.fill_(float("nan"))
+        self.workspace = torch.empty(B.cpa_latent_decode_workspace_bytes(self.cfg), dtype=torch.uint8, **on)
+        self.lens = torch.zeros(self.B, dtype=torch.int32, **on)
+        self._lens_next = torch.empty_like(self.lens)
+        start = np.zeros(self.B, dtype=np.int64) if first is None else np.asarray(first, dtype=np.int64)
+        self.first = None if first is None else torch.as_tensor(start.astype(np.int32), **on)
+        self.cu = torch.as_tensor(np.concatenate([[0], np.cumsum(self.block_lens)]).astype(np.int32), **on)
+        self.positions = torch.as_tensor(np.concatenate([s + np.arange(n) for s, n in zip(start, self.block_lens)]).astype(np.int32), **on)
+        lens, free = torch.as_tensor(self.block_lens, **on), torch.as_tensor(np.ascontiguousarray(free_pages, dtype=np.int32), **on)
+        self._call("cpa_plan_upload", self.plan, self.index_buf, self.index_buf.numel())
+        self._call("cpa_tables_build", tables_cfg, self.dims, lens, free, len(free_pages), self.tables)
+
+    def _call(self, what: str, *args) -> None:
+        with torch.cuda.device(self.device):
+            rc = getattr(B, what)(*args, int(torch.cuda.current_stream(self.device).cuda_stream))
+        if rc != B.CPA_OK:
+            raise B.CpaError(rc, what)
+
+    def _rows(self, rows: int, row: int, **tensors) -> None:
+        for name, t in tensors.items():
+            if (t.dtype != torch.bfloat16 or t.device != self.lens.device or t.shape != (rows, row) or
+                    (t.numel() and t.stride(1) != 1)):
+                raise ValueError(f"{name}: bf16 [{rows}, {row}] with whole rows on {self.lens.device} is wanted, not {t.dtype} "
+                                 f"{tuple(t.shape)} on {t.device}")
+
+    def _packed(self, **tensors) -> None:
+        for name, (t, shape) in tensors.items():
+            if t.dtype != torch.bfloat16 or t.device != self.lens.device or t.shape != shape or not t.is_contiguous():
+                raise ValueError(f"{name}: contiguous bf16 {list(shape)} on {self.lens.device} is wanted, not {t.dtype} "
+                                 f"{tuple(t.shape)} on {t.device}")
+
+    def _rope(self):
+        return (None, None) if self.rope is None else (self.rope.cfg, self.rope.turns)
+
+    def append(self, x: torch.Tensor, counts: Optional[Sequence[int]] = None, packed: bool = False) -> Optional[torch.Tensor]:
+        """New rows x [rows, latent_dim + 64] (packed block-major, any row stride), counts[b] per block or one each: normalised,
+        turned and stored behind the blocks' tokens.  With `packed` the stored rows come back too."""
+        if counts is None:
+            cu, rows = None, self.B
+        else:
+            n = np.asarray(counts, dtype=np.int64)
+            if n.shape != (self.B,) or (n < 0).any():
+                raise ValueError(f"counts: {self.B} whole numbers, none negative")
+            cu, rows = torch.as_tensor(np.concatenate([[0], np.cumsum(n)]).astype(np.int32), device=self.device), int(n.sum())
+        return self._append(x, cu, rows, packed)
+
+    def append_prefill(self, x: torch.Tensor) -> torch.Tensor:
+        """The prompts' rows x [total_tokens, latent_dim + 64] into the cache; returns the stored rows, packed, which the up
+        projections of the expanded form and prefill() read."""
+        return self._append(x, self.cu, self.total_tokens, True)
+
+    def _append(self, x, cu, rows, packed):
+        self._rows(rows, self.L + 64, x=x)
+        out = torch.empty((rows, self.L + 64), dtype=torch.bfloat16, device=self.device) if packed else None
+        self._call("cpa_latent_append", self.cfg, self.dims, self.tables, *self._rope(), x, x.stride(0) if rows > 1 else self.L + 64,
+                   self.norm_weight, cu, rows, self.first, self.lens, self._lens_next, self.pool, out)
+        self.lens, self._lens_next = self._lens_next, self.lens
+        return out
+
+    def turn_queries(self, q: torch.Tensor) -> torch.Tensor:
+        """Turns the positional part (the last 64 elements) of the prompts' queries [total_tokens, heads, 192], in place."""
+        if self.rope is not None:
+            self.rope.turn(self.positions, q)
+        return q
+
+    def prefill(self, q: torch.Tensor, kv: torch.Tensor, packed: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Expanded form, causal over every block: q [tokens, heads, 128 + 64] (turned), kv [tokens, heads, 128 + 128], and
+        append_prefill's packed rows, of which the positional keys are read.  Returns [tokens, heads, 128]."""
+        T = self.total_tokens
+        if out is None:
+            out = torch.empty((T, self.H, 128), dtype=torch.bfloat16, device=self.device)
+        self._packed(q=(q, (T, self.H, 192)), kv=(kv, (T, self.H, 256)), packed=(packed, (T, self.L + 64)), out=(out, (T, self.H, 128)))
+        self._call("cpa_latent_prefill", self.cfg, self.plan, q, kv, packed[:, self.L:], self.L + 64, out)
+        return out
+
+    def _io(self, q_latent, q_rope, out):
+        if out is None:
+            out = torch.empty((self.B, self.H, self.L), dtype=torch.bfloat16, device=self.device)
+        for name, t, e in (("q_latent", q_latent, self.L), ("q_rope", q_rope, 64), ("out", out, self.L)):
+            if t.device != self.lens.device or t.shape != (self.B, self.H, e):
+                raise ValueError(f"{name}: [{self.B}, {self.H}, {e}] on {self.lens.device} is wanted, not {tuple(t.shape)} on {t.device}")
+        return B.latent_io(q_latent, q_rope, out), out
+
+    def _active(self, active):
+        if active is not None and (active.dtype != torch.int32 or active.device != self.lens.device or active.shape != (self.B,) or
+                                   not active.is_contiguous()):
+            raise ValueError(f"active: contiguous int32 [{self.B}] on {self.lens.device} is wanted")
+        return active
+
+    def decode(self, q_latent: torch.Tensor, q_rope: torch.Tensor, out: Optional[torch.Tensor] = None, active=None) -> torch.Tensor:
+        """Absorbed form: q_latent [B, heads, latent_dim], q_rope [B, heads, 64] (turned) over the blocks' cached rows; returns
+        [B, heads, latent_dim].  Blocks whose flag in `active` (device int32 [B]) is 0 sit out."""
+        io, out = self._io(q_latent, q_rope, out)
+        self._call("cpa_latent_decode", self.cfg, self.dims, self.tables, io, self.lens, self._active(active), self.pool, self.workspace)
+        return out
+
+    def step(self, q_latent: torch.Tensor, q_rope: torch.Tensor, x: torch.Tensor, out: Optional[torch.Tensor] = None,
+             active=None) -> torch.Tensor:
+        """One decode step: x [B, latent_dim + 64] appended, q_rope turned to the new token's position, then decode()."""
+        io, out = self._io(q_latent, q_rope, out)
+        self._rows(self.B, self.L + 64, x=x)
+        self._call("cpa_latent_step", self.cfg, self.dims, self.tables, *self._rope(), io, x, x.stride(0) if self.B > 1 else self.L + 64,
+                   self.norm_weight, self.first, self.lens, self._lens_next, self._active(active), self.pool, self.workspace)
+        self.lens, self._lens_next = self._lens_next, self.lens
+        return out
+
+    def status(self) -> int:
+        stream = int(torch.cuda.current_stream(self.device).cuda_stream)
+        return B.cpa_plan_status(self.plan, stream) or B.cpa_tables_status(self.tables, stream)
+
+    def close(self) -> None:
+        if self.plan:
+            torch.cuda.synchronize(self.device)
+            B.cpa_plan_destroy(self.plan)
+            self.plan = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
