@@ -25,90 +25,26 @@
 //
 // Every mbarrier wait is bounded: when one gives up the CTA records it in the status word, stops waiting, still frees its
 // tensor memory and returns.
-#include <algorithm>
-#include <atomic>
-
-#include "latent.cuh"
-#include "cpa_tcgen05.cuh"
+#include "latent_decode.cuh"
 
 namespace {
 
-constexpr int kTile = 64;                       // tokens per tile
-constexpr int kTilePages = kTile / kPage;
-constexpr int kDecodeThreads = 512;
-constexpr int kSms = 148;                       // of a B200; CTAs do not wait for one another, so any device will do
-constexpr int kSegRing = 4;
 constexpr int kMaxDecodeStages = 6;
-constexpr int kBlockCost = 2;                   // what a block costs beside its tiles, in tiles (its queries, its output)
-constexpr int kMinRange = 2;                    // cost of a CTA's share, at least: a tile and its block's own (4 blocks of 96..288 tokens: 11.3 us; 14.4 with 4)
-constexpr float kLowest = -3e38f, kFirstMargin = 6.f;
-constexpr uint32_t kPBytes = kTile * 128;
-constexpr int kMaxSmem = 232448;                // 227 KB, what a CTA can have on sm_100
-
-struct decode_args {
-    q8_tables t;
-    cpa_latent_io io;
-    const uint64_t* turns;            // step: the query's positional part is turned; nullptr: taken as it is
-    const int32_t *first, *lens, *active;
-    // step (x given): the new token's row is made and stored first
-    const __nv_bfloat16 *x, *weight;
-    int64_t x_row;
-    int32_t* lens_out;
-    __nv_bfloat16* pool;
-    float2* part_ml;                  // [slots, head groups, 64]
-    float* part_o;                    // [slots, head groups, 64, L]
-    int2* cuts;                       // [groups] (block, parts) of the block that starts in a group and goes on behind it
-    int B, H, L, groups, head_groups, group_heads, interleaved;
-    int list_words;                   // of the page list, for a look ahead
-    float scale_log2, amplitude, eps;
-};
-
-// A block's part in a launch.
-struct block_state { int len, ip, status; bool on; };
-__device__ __forceinline__ block_state block_of(int b, const decode_args& a) {
-    block_state r;
-    const int before = ld_i32(a.lens + b), np0 = ld_i32(a.t.page_indptr + b), np1 = ld_i32(a.t.page_indptr + b + 1);
-    const bool active = a.active == nullptr || ld_i32(a.active + b) != 0;
-    const int64_t len = (int64_t)before + (a.x ? 1 : 0), room = (int64_t)(np1 - np0) * kPage;
-    r.ip = np0;
-    r.status = !active ? 0 : before < 0 ? kStatusInvalid : len > room ? kStatusNoSpace : 0;
-    r.on = active && r.status == 0;
-    r.len = r.on ? (int)len : 0;
-    return r;
-}
-
-struct segment {
-    int block, tile0, tiles, len;     // block -1: no more; tiles [tile0, tile0 + tiles) of a block of `len` tokens
-    int ip, slot;                     // its first page in the list; partial slot, -1: the whole block
-    int pad[2];
-};
-
-__device__ __forceinline__ row_recipe new_row_of(const decode_args& a) {
-    return {a.weight, a.turns, a.eps, a.amplitude, a.interleaved};
-}
-template <int L>
-__device__ __forceinline__ __nv_bfloat16* slot_of(const decode_args& a, const segment& g) {
-    const int at = g.len - 1, page = ld_i32(a.t.page_indices + g.ip + at / kPage);
-    return a.pool + ((int64_t)page * kPage + at % kPage) * (L + kRopeDim);
-}
 
 struct __align__(8) DecodeBarriers {
     uint64_t kv_full[kMaxDecodeStages], kv_empty[kMaxDecodeStages][kTilePages];
     uint64_t s_full[2], s_empty[2], p_full, pv_done, q_full, q_empty, o_empty, row_ready, drain_s, drain_p;
-    uint64_t seg_full[kSegRing], seg_empty[kSegRing];
     uint32_t tmem_base;
 };
 
 template <int N>
 struct DecodeShared {
     DecodeBarriers bars;
-    segment seg[kSegRing];
+    SegmentRing ring;
+    CutShared cut;
     float2 turn[kRopeDim / 2];
     float column[8][N / 2];           // per warp and head: maxima, sums
     float factor[N];
-    int64_t scan[kDecodeThreads / 32];
-    int64_t start_cost;
-    int start_block;
 };
 
 template <int L, int N>
@@ -124,16 +60,6 @@ struct DecodeShape {
 };
 
 // ---------------------------------------------------------------- PTX
-__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, int group, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %3}], [%4];\n"
-        :: "r"(dst), "l"(map), "r"(0), "r"(group), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map, int head, int block, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4}], [%5];\n"
-        :: "r"(dst), "l"(map), "r"(0), "r"(head), "r"(block), "r"(bar) : "memory");
-}
 // By one thread; descriptors as halves, of which the lower one holds the address.
 __device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
                                           uint32_t accumulate) {
@@ -142,25 +68,9 @@ __device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32
         " tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n}\n"
         :: "r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
 }
-// One lane of the warp, chosen in the form that lets the compiler keep the operands of what that lane runs on the uniform
-// datapath: an MMA of 64 x 64 x 16 then goes out every 32 cycles, which is what its operands take out of shared memory, and
-// every 46 under a test of the lane's number (58 with the instruction alone predicated on it).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
-    return p != 0;
-}
 __device__ __forceinline__ void tc_commit_one(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" :: "r"(bar) : "memory");
 }
-// Whether `x` holds in any of the 128 threads that meet at barrier `id`.
-__device__ __forceinline__ bool any_of_128(int id, bool x) {
-    uint32_t r;
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
-                 : "=r"(r) : "r"((uint32_t)x), "r"(id) : "memory");
-    return r != 0;
-}
-__device__ __forceinline__ void sync_128(int id) { asm volatile("barrier.cta.sync %0, 128;\n" :: "r"(id) : "memory"); }
 // Columns of 16 lanes in fragment layout: per 8 columns four words, of lane / 4 (words 0, 1) and lane / 4 + 8 (words 2, 3),
 // columns 2 (lane % 4) and the next.
 template <int N> __device__ __forceinline__ void tc_ld_frag(uint32_t taddr, float (&v)[N / 2]);
@@ -188,21 +98,6 @@ template <> __device__ __forceinline__ void tc_ld_frag<32>(uint32_t taddr, float
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
-// 16 columns of this thread's lane
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, float (&v)[16]) {
-    uint32_t r[16];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
-    tc_wait_ld();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-
-// First cost of group g's share when `total` is dealt to `groups`.
-__device__ __forceinline__ int64_t share_start(int64_t total, int g, int groups) { return (total * g + groups - 1) / groups; }
-__device__ __forceinline__ int tiles_of(int len) { return (int)(((int64_t)len + kTile - 1) / kTile); }
-
 template <int L, int N>
 __global__ void __launch_bounds__(kDecodeThreads, 1)
 latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap map_qc,
@@ -242,10 +137,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         mbar_init(bar(&bars.row_ready), 1);
         mbar_init(bar(&bars.drain_s), 1);
         mbar_init(bar(&bars.drain_p), 1);
-        for (int i = 0; i < kSegRing; ++i) {
-            mbar_init(bar(&bars.seg_full[i]), 1);
-            mbar_init(bar(&bars.seg_empty[i]), 15);      // every warp but the one that hands out
-        }
+        init_ring(sm.ring, 15);                   // every warp but the one that hands out
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     }
@@ -254,111 +146,18 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    // What every CTA reads first is brought to L2 ahead of the wait (L2 is coherent: what is written until then is seen), the
-    // lists shared out.
-    for (int64_t i = (int64_t)(threadIdx.x * gridDim.x + blockIdx.x) * 32; i < a.list_words; i += (int64_t)kDecodeThreads * gridDim.x * 32) {
-        asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.t.page_indices + i));
-        if (i < a.B) {
-            asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.lens + i));
-            asm volatile("prefetch.global.L2 [%0];\n" :: "l"(a.t.page_indptr + i));
-        }
-    }
+    look_ahead(a);
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-
-    // ---- the cut: every CTA sums the cost of all blocks and finds where its share begins
-    const int per = (a.B + kDecodeThreads - 1) / kDecodeThreads, b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
-    int64_t cost = 0;
-    for (int b = b0; b < b1; ++b) {
-        const block_state s = block_of(b, a);
-        if (s.len > 0) cost += tiles_of(s.len) + kBlockCost;
-        if (b % (int)gridDim.x == (int)blockIdx.x) {     // the blocks' books are shared out
-            if (s.status) atomicCAS(a.t.header, 0, s.status);
-            if (a.x) a.lens_out[b] = ld_i32(a.lens + b) + (s.on ? 1 : 0);
-        }
-    }
-    int64_t inc = cost;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += v;
-    }
-    if (lane == 31) sm.scan[warp] = inc;
-    if (threadIdx.x == 0) sm.start_block = a.B;
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    int64_t before = inc - cost, total = 0;
-    for (int w = 0; w < kDecodeThreads / 32; ++w) {
-        if (w < warp) before += sm.scan[w];
-        total += sm.scan[w];
-    }
-    const int used = (int)max((int64_t)1, min((int64_t)a.groups, total / kMinRange));     // groups that get a share
-    const int64_t lo = group < used ? share_start(total, group, used) : total, hi = group < used ? share_start(total, group + 1, used) : total;
-    if (cost > 0 && before <= lo && lo < before + cost) {
-        sm.start_block = b0;
-        sm.start_cost = before;
-    }
-    __syncthreads();
+    const share sh = cut_shares(a, sm.cut, group);
     const uint32_t tmem = bars.tmem_base;
     constexpr uint32_t kColO = 2 * N;
     bool dead = false;
     int32_t* const status = a.t.header;
     auto wait = [&](uint64_t* p, uint32_t parity) { mbar_wait(bar(p), parity, dead, status, kSpinLimit); };
-    // segment i of this CTA, by a whole warp
-    auto get_segment = [&](int i) {
-        wait(&bars.seg_full[i % kSegRing], (uint32_t)(i / kSegRing) & 1u);
-        dead = __any_sync(0xffffffffu, dead);
-        segment s = sm.seg[i % kSegRing];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(&bars.seg_empty[i % kSegRing]));
-        if (dead) s.block = -1;
-        return s;
-    };
+    auto get_segment = [&](int i) { return take_segment(sm.ring, i, dead, status); };
 
     if (warp == 15) {
-        // ------------------------------------------------------------ segments
-        int n = 0;
-        int2 cut = make_int2(-1, 0);
-        int64_t c = sm.start_cost;
-        auto put = [&](const segment& s) {
-            wait(&bars.seg_empty[n % kSegRing], ((uint32_t)(n / kSegRing) & 1u) ^ 1u);
-            sm.seg[n % kSegRing] = s;
-            mbar_arrive(bar(&bars.seg_full[n % kSegRing]));
-            ++n;
-        };
-        if (lo < hi)
-            for (int b = sm.start_block; b < a.B && c < hi; b += 32) {
-                block_state s{0, 0, 0, false};
-                if (b + lane < a.B) s = block_of(b + lane, a);
-                const int tiles = tiles_of(s.len);
-                const int64_t mine = s.len > 0 ? tiles + kBlockCost : 0;
-                int64_t at = mine;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int64_t v = __shfl_up_sync(0xffffffffu, at, o);
-                    if (lane >= o) at += v;
-                }
-                const int64_t first = c + at - mine + kBlockCost;      // cost at which the block's first tile lies
-                c += __shfl_sync(0xffffffffu, at, 31);
-                const int j0 = (int)min((int64_t)tiles, max((int64_t)0, lo - first)), j1 = (int)min((int64_t)tiles, max((int64_t)0, hi - first));
-                uint32_t todo = __ballot_sync(0xffffffffu, s.len > 0 && j1 > j0);
-                while (todo) {
-                    const int who = __ffs(todo) - 1;
-                    todo &= todo - 1;
-                    if (lane == who) {
-                        const bool whole = j0 == 0 && j1 == tiles;
-                        put({b + lane, j0, j1 - j0, s.len, s.ip, whole ? -1 : 2 * group + (j0 == 0 ? 1 : 0), {0, 0}});
-                        if (j0 == 0 && j1 < tiles) cut = make_int2(b + lane, (int)((first + tiles - 1) * used / total) - group + 1);
-                    }
-                    n = __shfl_sync(0xffffffffu, n, who);
-                }
-                dead = __any_sync(0xffffffffu, dead);
-                if (dead) break;
-            }
-        if (lane == 0) put({-1, 0, 0, 0, 0, 0, {0, 0}});
-        const uint32_t has = __ballot_sync(0xffffffffu, cut.x >= 0);
-        const int who = has ? __ffs(has) - 1 : 0;
-        if (hg == 0 && lane == who) a.cuts[group] = cut;
+        hand_out(a, sm.cut, sm.ring, sh, group, hg == 0, dead, status);
     } else if (warp == 12) {
         // ------------------------------------------------------------ TMA producer, a lane per page
         int it = 0, fresh = 0;
@@ -476,14 +275,13 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     } else if (warp >= 8) {
         // ------------------------------------------------------------ queries, a step's new row, rows of zeros
         // (loops are kept short: what a launch runs once or twice costs the fetching of its instructions)
-        constexpr int latent_pieces = L / 8;           // 16-byte pieces of a row's latent part
         const int tid = threadIdx.x - 256;
         auto q_at = [&](int h, int p) {                // where piece p of head h's positional part lies (swizzled)
             return reinterpret_cast<uint4*>(gen + (s_q - base) + (nc - 1) * (N * 128) + h * 128 + ((p ^ (h & 7)) << 4));
         };
         for (int i = 0;; ++i) {
             const segment g = get_segment(i);
-            if (any_of_128(3, g.block < 0)) break;
+            if (any_of_128(kLoaderBarrier, g.block < 0)) break;
             const int position = (a.first ? ld_i32(a.first + g.block) : 0) + g.len - 1;
             if (i > 0) wait(&bars.q_empty, (uint32_t)(i - 1) & 1u);
             if (warp == 9) {
@@ -497,44 +295,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 __syncwarp();
             }
             if (a.turns) {
-                // turned positional parts: a thread takes pieces r and r ^ 4 of a head, each other's partners in the half layout
-                const __nv_bfloat16* qr = (const __nv_bfloat16*)a.io.q_rope + g.block * a.io.q_rope_block_stride + h0 * a.io.q_rope_head_stride;
-                constexpr int kRounds = (N * 4 + 127) / 128;
-                const int r = tid & 3;
-                uint4 x[kRounds], y[kRounds];
-#pragma unroll
-                for (int k = 0; k < kRounds; ++k) {
-                    const int h = (tid >> 2) + 32 * k;
-                    x[k] = y[k] = make_uint4(0, 0, 0, 0);
-                    if (h < heads) {
-                        x[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * r);
-                        y[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * (r + 4));
-                    }
-                }
-                sync_128(3);
-#pragma unroll
-                for (int k = 0; k < kRounds; ++k) {
-                    const int h = (tid >> 2) + 32 * k;
-                    if (h >= N) break;
-                    uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, w[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
-                    if (a.interleaved) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            u[e] = rope_turn(u[e], sm.turn[4 * r + e]);
-                            w[e] = rope_turn(w[e], sm.turn[4 * r + 16 + e]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 c0 = sm.turn[8 * r + 2 * e], c1 = sm.turn[8 * r + 2 * e + 1];
-                            const float u0 = bf_lo(u[e]), u1 = bf_hi(u[e]), w0 = bf_lo(w[e]), w1 = bf_hi(w[e]);
-                            u[e] = bf_pack(turn_first(u0, w0, c0), turn_first(u1, w1, c1));
-                            w[e] = bf_pack(turn_second(u0, w0, c0), turn_second(u1, w1, c1));
-                        }
-                    }
-                    *q_at(h, r) = make_uint4(u[0], u[1], u[2], u[3]);
-                    *q_at(h, r + 4) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+                turn_queries<N>(a, g.block, h0, heads, tid, sm.turn, q_at);
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                 __syncwarp();
             }
@@ -548,14 +309,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 if (lane == 0) mbar_arrive(bar(&bars.row_ready));
             }
         }
-        // blocks without a token: rows of zeros
-        for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-            const block_state s = block_of(b, a);
-            if (!s.on || s.len > 0) continue;
-            __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + b * a.io.o_block_stride;
-            for (int e = tid; e < a.H * latent_pieces; e += 128)
-                *reinterpret_cast<uint4*>(o + (e / latent_pieces) * a.io.o_head_stride + 8 * (e % latent_pieces)) = make_uint4(0, 0, 0, 0);
-        }
+        write_zero_rows(a, tid);
     } else {
         // ------------------------------------------------------------ softmax and epilogue
         constexpr int NH = N / 2, J = NH / 8;  // heads of a half; groups of eight, of which this thread has two heads and two tokens
@@ -889,13 +643,13 @@ bool io_ok(const cpa_latent_io* io, int B, int H, int L) {
 
 // The pool as page-wise boxes: 64 elements x 8 tokens x column blocks x 2 groups of 8 tokens, which lands as
 // [group of 8 tokens][column block][8 rows of 128 bytes, swizzled]: uniform strides in tokens and in elements for both products.
-bool make_page_map(CUtensorMap* map, const void* pool, int64_t pages, int L) {
+bool make_page_map(CUtensorMap* map, const void* pool, int64_t pages, int L, int columns) {
     EncodeTiledFn fn = get_encode_fn();
     if (!fn) return false;
     const cuuint64_t row = (cuuint64_t)(L + kRopeDim) * 2, nc = (cuuint64_t)L / 64 + 1;
     const cuuint64_t dims[4] = {64, 8, nc, (cuuint64_t)pages * 2};
     const cuuint64_t strides[3] = {row, 128, row * 8};
-    const cuuint32_t box[4] = {64, 8, (cuuint32_t)nc, 2};
+    const cuuint32_t box[4] = {64, 8, (cuuint32_t)columns, 2};
     const cuuint32_t elem[4] = {1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, elem,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -916,16 +670,16 @@ struct workspace { int64_t ml, o, cuts, bytes; };
 workspace workspace_of(const cpa_latent_config& c) {
     const decode_shape s = shape_of(c);
     const int64_t rows = (int64_t)s.groups * 2 * s.head_groups * 64;
-    workspace w;
+    workspace w = {};
     w.ml = 0;
     w.o = rows * 8;
     w.cuts = w.o + rows * c.latent_dim * 4;
-    w.bytes = (w.cuts + s.groups * 8 + 255) / 256 * 256;
+    w.bytes = (w.cuts + s.groups * 8 + 255) / 256 * 256 + 256;       // and what its alignment may take
     return w;
 }
 
 template <int L, int N>
-int launch(const CUtensorMap (&map)[3], const decode_args& a, cudaStream_t st) {
+int launch(const CUtensorMap (&map)[4], const decode_args& a, cudaStream_t st) {
     static std::atomic<bool> configured_dev[64];
     int dev_id = 0;
     if (cudaGetDevice(&dev_id) != cudaSuccess || dev_id < 0 || dev_id >= 64) {
@@ -943,7 +697,7 @@ int launch(const CUtensorMap (&map)[3], const decode_args& a, cudaStream_t st) {
     return q8_launch_smem(latent_decode_kernel<L, N>, a.groups * a.head_groups, kDecodeThreads, smem, st, map[0], map[1], map[2], a);
 }
 template <int N>
-int launch_latent(const CUtensorMap (&map)[3], const decode_args& a, cudaStream_t st) {
+int launch_latent(const CUtensorMap (&map)[4], const decode_args& a, cudaStream_t st) {
     switch (a.L) {
         case 128: return launch<128, N>(map, a, st);
         case 256: return launch<256, N>(map, a, st);
@@ -969,7 +723,7 @@ int decode(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tab
     a.x_row = x_row;
     a.lens_out = d_lens_out;
     a.pool = (__nv_bfloat16*)const_cast<void*>(pool);
-    char* ws = (char*)d_workspace;
+    char* ws = (char*)(((uintptr_t)d_workspace + 255) & ~(uintptr_t)255);      // (the pair kernel stores 32 bytes at a time)
     a.part_ml = (float2*)(ws + w.ml);
     a.part_o = (float*)(ws + w.o);
     a.cuts = (int2*)(ws + w.cuts);
@@ -984,15 +738,17 @@ int decode(const cpa_latent_config* cfg, const cpa_table_dims* dims, void* d_tab
     a.amplitude = rope ? (float)rope->amplitude : 1.f;
     a.eps = cfg->norm_eps;
     a.list_words = dims->page_capacity;
-    CUtensorMap map[3];
-    if (!make_page_map(&map[0], pool, dims->num_pages, a.L) ||
+    CUtensorMap map[4];
+    if (!make_page_map(&map[0], pool, dims->num_pages, a.L, a.L / 64 + 1) ||
+        (s.head_groups == 2 && !make_page_map(&map[3], pool, dims->num_pages, a.L, a.L / 128)) ||
         !make_q_map(&map[1], io->q_latent, a.B, a.H, io->q_latent_block_stride, io->q_latent_head_stride, a.L / 64, s.n) ||
         !make_q_map(&map[2], io->q_rope, a.B, a.H, io->q_rope_block_stride, io->q_rope_head_stride, 1, s.n))
         return CPA_ECUDA;
     cudaStream_t st = (cudaStream_t)stream;
-    const int rc = s.n == 16   ? launch_latent<16>(map, a, st)
-                   : s.n == 32 ? launch_latent<32>(map, a, st)
-                               : launch_latent<64>(map, a, st);
+    const int rc = s.head_groups == 2 ? latent_decode_pairs(map, &a, stream)
+                   : s.n == 16        ? launch_latent<16>(map, a, st)
+                   : s.n == 32        ? launch_latent<32>(map, a, st)
+                                      : launch_latent<64>(map, a, st);
     if (rc != CPA_OK) return rc;
     return q8_launch(latent_join_kernel, kJoinPerSm * kSms, kJoinWarps * 32, st, a);
 }
