@@ -772,7 +772,8 @@ typedef struct cpa_latent_config {
 /* The cpa_config that the calls on the tables of a latent cache take.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
 CPA_API int cpa_latent_tables_config(const cpa_latent_config* cfg, cpa_config* out);
 
-/* The cpa_config that the plan of a cpa_latent_prefill is created with.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
+/* The cpa_config that the plan of a cpa_latent_prefill is created with.  Its q_tile_rows may be set to 128 where the units of 128
+ * query rows (num_heads for every 128 tokens of a block) have an SM each.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
 CPA_API int cpa_latent_plan_config(const cpa_latent_config* cfg, cpa_config* out);
 
 /*

@@ -78,7 +78,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         if (threadIdx.x == 0) atomicCAS(ix.status, 0, kStatusInvalid);
         return;
     }
-    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
     const int G = gridDim.x;
     // unit of round k, with the next rounds' schedule entry and item record in flight
     auto fetch_code = [&](int k) { return k < n_rounds ? __ldg(ix.prefill_sched + (int64_t)k * G + blockIdx.x) : -1; };
