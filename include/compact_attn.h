@@ -790,7 +790,7 @@ CPA_API int cpa_latent_plan_config(const cpa_latent_config* cfg, cpa_config* out
  *   d_lens_out    : device int32 [B], written with the tokens cached after it; not d_lens itself; may be NULL
  *   packed        : device bf16 [num_rows, latent_dim + 64], the stored rows again (what the up projections and
  *                   cpa_latent_prefill read); rows that are not stored stay as they were; 16-byte aligned; may be NULL, or x
- *                   itself where x_row_stride is latent_dim + 64
+ *                   itself where x_row_stride is latent_dim + 64 and no two blocks share a row
  * A block whose rows do not fit its pages is left out (its length stays, CPA_ENOSPC in the tables' status), as is one with a
  * bad range or a negative length (CPA_EINVAL).  The same call repeated stores the same cache.  Errors: CPA_EINVAL,
  * CPA_EUNSUPPORTED, CPA_ECUDA.
@@ -802,7 +802,7 @@ CPA_API int cpa_latent_append(const cpa_latent_config* cfg, const cpa_table_dims
 
 /* Queries and outputs of the decode calls, device bf16, strides in elements (a multiple of 8 each, pointers 16-byte aligned):
  * element e of head h of block b is at b * block_stride + h * head_stride + e.  The queries' strides are positive (those of a
- * single block or head are not looked at). */
+ * single block or head are not looked at).  o must not overlap the queries. */
 typedef struct cpa_latent_io {
     const void* q_latent;                    /* [B, num_heads, latent_dim] */
     int64_t q_latent_block_stride, q_latent_head_stride;
@@ -853,7 +853,9 @@ CPA_API int cpa_latent_step(const cpa_latent_config* cfg, const cpa_table_dims* 
  *   k_rope : device bf16, row i at k_rope + i * k_rope_row_stride (elements, a multiple of 8, >= 64): the positional keys, turned
  *            already, as they lie behind the latent part of cpa_latent_append's packed rows
  *   o      : device bf16 [total_tokens, num_heads, 128]
- * All 16-byte aligned; o must not alias the inputs.  Errors: CPA_EINVAL (also: a plan of another configuration),
+ * All 16-byte aligned; o must not alias the inputs.  Weights of later keys are zero, and what a later block holds stays there; but
+ * zero times an infinity or a NaN among the VALUES of a token reaches the earlier rows of its own block's 128-token tile (keys that
+ * are not finite do not).  Errors: CPA_EINVAL (also: a plan of another configuration),
  * CPA_EUNSUPPORTED (a plan with cached prefixes), CPA_ESTATE (not uploaded), CPA_ECUDA.
  */
 CPA_API int cpa_latent_prefill(const cpa_latent_config* cfg, const cpa_plan* plan, const void* q, const void* kv,

@@ -77,6 +77,7 @@ __global__ void __launch_bounds__(kWarps * 32) latent_append_kernel(const __grid
             // (What the search leads to grows with the row, so a block's first and last one tell.)
             if (find_block(o.c0, a.cu, a.B, lane) == b && find_block(o.c0 + o.n - 1, a.cu, a.B, lane) == b) continue;
             for (int row = o.c0; row < o.c0 + o.n; ++row) {
+                if (find_block(row, a.cu, a.B, lane) == b) continue;      // (taken where it is looked for; x may hold the packed row by now)
                 load_row<L, WIDE>(r, a.x + row * a.x_row, lane);
                 put_row<L>(r, row, (int)b, o, a, lane);
             }

@@ -635,6 +635,7 @@ bool io_ok(const cpa_latent_io* io, int B, int H, int L) {
     for (int64_t s : {B > 1 ? io->q_latent_block_stride : 8, H > 1 ? io->q_latent_head_stride : 8, B > 1 ? io->q_rope_block_stride : 8,
                       H > 1 ? io->q_rope_head_stride : 8})
         if (s <= 0 || s >= (int64_t)1 << 39) return false;
+    if (io->o == io->q_latent || io->o == io->q_rope) return false;
     // heads of the output must not share elements: blocks of heads, or heads of blocks
     const int64_t bs = B > 1 ? io->o_block_stride : INT64_MAX, hs = H > 1 ? io->o_head_stride : INT64_MAX;
     if (bs < L || hs < L) return false;

@@ -287,6 +287,21 @@ def test_append_leaves_out_what_does_not_fit_or_is_bad(B):
     assert out.tolist() == [1, 2, 3, 4]
 
 
+def test_append_packed_in_place(B):
+    rng = np.random.default_rng(9)
+    rope = Rope(B)
+    made = []
+    for in_place in (False, True):
+        c = Cache(B, [40, 0, 25], 256, seed=2, rope=rope)
+        x, _ = _bf16(np.random.default_rng(3).standard_normal((60, 320)))
+        packed, w, out = x if in_place else torch.empty_like(x), torch.ones(256, dtype=torch.bfloat16, device="cuda"), torch.empty_like(c.lens)
+        assert B.cpa_latent_append(c.cfg, c.dims, c.tables, rope.cfg, rope.turns, x, 320, w, _i32([0, 35, 35, 60]), 60, None, None, out, c.pool,
+                                   packed, _stream()) == 0
+        assert out.tolist() == [35, 0, 25] and c.status() == 0
+        made.append((packed.clone(), c.pool.clone()))
+    assert torch.equal(made[0][0], made[1][0]) and torch.equal(made[0][1].view(torch.int16), made[1][1].view(torch.int16))
+
+
 def test_append_many_blocks_and_rows_behind_the_last(B):
     rng = np.random.default_rng(8)
     counts = rng.integers(0, 4, 1500)
@@ -388,12 +403,13 @@ def test_decode_inactive_and_bad_blocks_sit_out(B):
         assert (o[0] == 9.0).all() and d.status() == word
 
 
-def test_decode_masks_by_index_not_by_value(B):
+@pytest.mark.parametrize("H,L", [(16, 512), (40, 256), (128, 512), (66, 128)])
+def test_decode_masks_by_index_not_by_value(B, H, L):
     # what lies behind a block's length may be anything: NaN (as everywhere here), infinities, the largest values
     rng = np.random.default_rng(13)
     lens = [1, 17, 63, 65, 100, 190]
     for junk in (float("inf"), float("-inf"), 3e38):
-        c = Cache(B, [256] * 6, 512, 16)
+        c = Cache(B, [256] * 6, L, H)
         c.pool.fill_(junk)
         c.fill(lens, rng)
         qc, qr, cf, rf = c.queries(rng)
@@ -417,10 +433,11 @@ def test_decode_scores_of_any_range(B, H):
         c.check(c.decode(qc, qr), cf, rf, what=f"{grow} {spread}")
 
 
-def test_decode_scores_that_are_minus_infinity_or_nan(B):
+@pytest.mark.parametrize("H", [4, 33, 100])
+def test_decode_scores_that_are_minus_infinity_or_nan(B, H):
     rng = np.random.default_rng(15)
     lens = [200, 200, 70, 128]
-    c = Cache(B, lens, 128, 4)
+    c = Cache(B, lens, 128, H)
     c.fill(lens, rng)
     flat = c.pool.view(-1, 192)
     qc, qr, cf, rf = c.queries(rng)
@@ -436,7 +453,8 @@ def test_decode_scores_that_are_minus_infinity_or_nan(B):
     assert torch.isnan(o[1]).all() and torch.isnan(o[3]).all()
 
 
-def test_decode_far_pages(B):
+@pytest.mark.parametrize("H", [16, 128])
+def test_decode_far_pages(B, H):
     # page ids on both sides of the pool's 2^32-byte line
     page = 16 * 576 * 2
     edge = 2 ** 32 // page
@@ -445,7 +463,7 @@ def test_decode_far_pages(B):
         pytest.skip("too little memory")
     ids = np.array([edge + 40, 3, edge - 1, edge, edge + 1, 0, 2 * edge // 2 + 7], dtype=np.int32)
     rng = np.random.default_rng(16)
-    c = Cache(B, [100], 512, 16, page_ids=(ids, edge + 64), rope=Rope(B))
+    c = Cache(B, [100], 512, H, page_ids=(ids, edge + 64), rope=Rope(B))
     c.fill([90], rng)
     qc, qr, cf, rf = c.queries(rng)
     c.check(c.decode(qc, qr), cf, rf, what="far pages")
@@ -454,9 +472,28 @@ def test_decode_far_pages(B):
     assert c.status() == 0
 
 
+@pytest.mark.parametrize("H", [8, 64, 96])
+def test_decode_and_step_of_many_short_blocks(B, H):
+    # several blocks to a thread of the cut, many segments to a CTA, empty and inactive ones between them
+    rng = np.random.default_rng(H)
+    lens = rng.integers(0, 90, 1300)
+    lens[rng.random(1300) < 0.2] = 0
+    c = Cache(B, lens + 1, 128, H, rope=Rope(B))
+    c.fill(list(lens), rng)
+    qc, qr, cf, rf = c.queries(rng)
+    some = sorted(rng.choice(1300, 40, replace=False))
+    o = c.decode(qc, qr)
+    assert c.status() == 0
+    c.check(o, cf, rf, some, "many")
+    assert (o[torch.as_tensor(np.flatnonzero(lens == 0), device="cuda")] == 0).all()
+    active = (rng.random(1300) < 0.7).astype(np.int32)
+    _step(c, rng, np.ones(128), rng.integers(0, 1000, 1300), _i32(active), blocks=some)
+    assert c.status() == 0
+
+
 # ------------------------------------------------------------------------------------------------ steps
 
-def _step(c, rng, weight, first, active=None, qspread=1.0):
+def _step(c, rng, weight, first, active=None, qspread=1.0, blocks=None):
     """One step of all blocks; checks rows, lengths and outputs."""
     B, r = c.B, c.rope
     x, xf = _bf16(rng.standard_normal((c.n, c.L + 64)))
@@ -482,7 +519,7 @@ def _step(c, rng, weight, first, active=None, qspread=1.0):
         rf = ol.turn(rf, pos[:, None], r.f, r.interleaved)
     # the turned query is rounded to bf16: 2^-8 of each element, times the positional key, in the score
     score = [c.scale * 2.0 ** -8 * (np.abs(rf[b]) @ np.abs(c.rows[b][:, c.L:]).T).max(1)[:, None] if len(c.rows[b]) else 0.0 for b in range(c.n)]
-    c.check(o, cf, rf, on, "step", score if r else None)
+    c.check(o, cf, rf, [b for b in on if blocks is None or b in blocks], "step", score if r else None)
     for b in range(c.n):
         if b not in on:
             assert (o[b] == 9.0).all()
@@ -612,6 +649,42 @@ def test_prefill_lengths_and_heads(B, lens, H):
 @pytest.mark.parametrize("spread,stride,num_sms", [(30.0, 64, 0), (1e-3, 72, 0), (1.0, 576, 3), (4.0, 192, 1)])
 def test_prefill_scores_strides_and_sms(B, spread, stride, num_sms):
     _prefill(B, [300, 17, 600], 3, np.random.default_rng(stride), spread, stride, num_sms)
+
+
+def test_prefill_keeps_what_is_not_finite_to_its_own(B):
+    # NaN and infinities in the next block, and in keys of the row's future, change nothing; values that are not finite reach
+    # the rows from their own on (and, of their own block, the earlier ones of their 128-token tile)
+    rng = np.random.default_rng(30)
+    lens, H = [70, 130, 200], 2
+    T = sum(lens)
+    cfg = B.cpa_latent_config(H, 512, 64, 128, 128, 16, 192 ** -0.5, 1e-6, 0)
+    plan = B.cpa_plan_create(B.cpa_latent_plan_config(cfg), lens, 0, list(range(27)))
+    index = torch.empty(B.cpa_plan_param(plan, B.PARAM_INDEX_BYTES), dtype=torch.uint8, device="cuda")
+    assert B.cpa_plan_upload(plan, index, index.numel(), _stream()) == 0
+    (q, _), (kv, _), (r, _) = _bf16(rng.standard_normal((T, H, 192))), _bf16(rng.standard_normal((T, H, 256))), _bf16(rng.standard_normal((T, 64)))
+    run = lambda: (lambda o: (B.cpa_latent_prefill(cfg, plan, q, kv, r, 64, o, _stream()), o)[1])(torch.empty(T, H, 128, dtype=torch.bfloat16, device="cuda"))
+    plain = run()
+    for bad in (float("nan"), float("inf")):
+        was = kv[70:200].clone(), r[70:200].clone()
+        kv[70:200], r[70:200] = bad, bad                       # all of block 1
+        o = run()
+        assert torch.equal(o[:70], plain[:70]) and torch.equal(o[200:], plain[200:])
+        assert not torch.isfinite(o[70:200].float()).any()
+        kv[70:200], r[70:200] = was
+        key = kv[300, 0, :128].clone()
+        kv[300, 0, :128] = bad                                 # a key of block 2: earlier rows and the other head do not see it
+        o = run()
+        assert torch.equal(o[:300], plain[:300]) and torch.equal(o[:, 1], plain[:, 1])
+        assert torch.isnan(o[300:, 0]).all() or bad != bad
+        kv[300, 0, :128] = key
+        value = kv[390, 1, 130].clone()
+        kv[390, 1, 130] = bad                                  # a value in block 2's second tile: its first tile does not see it
+        o = run()
+        assert torch.equal(o[:328], plain[:328]) and torch.equal(o[:, 0], plain[:, 0])
+        assert not torch.isfinite(o[390:, 1, 2].float()).any()
+        kv[390, 1, 130] = value
+    assert torch.equal(run(), plain)
+    B.cpa_plan_destroy(plan)
 
 
 # ------------------------------------------------------------------------------------------------ a whole event

@@ -84,7 +84,7 @@ def test_bad_latent_configurations_are_refused(cfg, want):
         with pytest.raises(B.CpaError) as e:
             call(cfg)
         assert e.value.status == want
-    io = B.cpa_latent_io(ok, 8192, 512, ok, 1024, 64, ok, 8192, 512)
+    io = B.cpa_latent_io(ok, 8192, 512, ok, 1024, 64, ok + (1 << 17), 8192, 512)
     assert B.cpa_latent_append(cfg, dims, ok, None, None, ok, 576, None, None, 4, None, ok, ok + 4, ok) == want
     assert B.cpa_latent_decode(cfg, dims, ok, io, ok, None, ok, ok) == want
     assert B.cpa_latent_step(cfg, dims, ok, None, None, io, ok, 576, None, None, ok, ok + 4, None, ok, ok) == want
@@ -102,10 +102,10 @@ def test_latent_pointers_and_strides_are_refused():
                 dict(d_turns=ok + 4), dict(d_cu_new=None, num_rows=3), dict(d_lens_out=ok + 2)):
         assert B.cpa_latent_append(cfg, dims, **dict(base, **bad)) == B.CPA_EINVAL, bad
     io = dict(q_latent=ok, q_latent_block_stride=8192, q_latent_head_stride=512, q_rope=ok, q_rope_block_stride=1024, q_rope_head_stride=64,
-              o=ok, o_block_stride=8192, o_head_stride=512)
+              o=other, o_block_stride=8192, o_head_stride=512)
     dec = dict(d_tables=ok, io=B.cpa_latent_io(**io), d_lens=ok, d_active=None, pool=ok, d_workspace=ok)
     step = dict(dec, rope=_rope(), d_turns=ok, x=ok, x_row_stride=576, norm_weight=None, d_first=None, d_lens_out=other)
-    bad_io = [dict(q_latent=0), dict(q_rope=0), dict(o=0), dict(q_latent=ok + 8), dict(q_rope=ok + 2), dict(o=ok + 8),
+    bad_io = [dict(q_latent=0), dict(q_rope=0), dict(o=0), dict(q_latent=ok + 8), dict(q_rope=ok + 2), dict(o=other + 8), dict(o=ok),
               dict(q_latent_head_stride=516), dict(q_rope_block_stride=1), dict(o_head_stride=504), dict(o_block_stride=4096),
               dict(o_head_stride=-512), dict(o_block_stride=0), dict(q_latent_head_stride=0), dict(q_rope_block_stride=-1024),
               dict(q_rope_head_stride=0), dict(q_latent_block_stride=1 << 39)]
