@@ -7,8 +7,8 @@
 // The rows are staged once (TMA, one copy per page) and serve both products: as the K-major operand of the first and the
 // MN-major operand of the second.  Tokens and latent elements are on the M side, so 16, 32 or 64 heads fill N without waste, and
 // O^T (latent_dim / 128 accumulators of 128 lanes x heads columns) leaves room in tensor memory for two score buffers at 64
-// heads; with the heads on the M side the 512-wide outputs of 128 rows would take all of it.  More than 64 heads are two groups
-// on two CTAs that walk the same tokens.
+// heads; with the heads on the M side the 512-wide outputs of 128 rows would take all of it.  More than 64 heads go to pairs of
+// CTAs (latent_decode_pair.cu).
 //
 // A CTA owns an equal share of all blocks' 64-token tiles, cut on the device from the lengths; a block that is cut leaves
 // partial sums in the workspace, which a second kernel joins.  Sixteen warps with fixed roles:
@@ -22,6 +22,14 @@
 //   15    walks the blocks and hands out the segments (block, first tile, tiles)
 // The reference m of a head stays as long as no score passes it by more than 2^8 (what it is cancels in the division); the
 // four warps of a half learn of that by one barrier with an OR, so a tile usually costs no exchange of maxima at all.
+//
+// Measured (latent parts of 512, caches larger than L2): 64 heads over 32 blocks of 1024..8192 tokens, 195 MB, 57 us (3.4 TB/s);
+// 16 heads over 192 blocks of 512..1024 with a step's new rows, 175 MB, 46 us (3.8 TB/s); 16 heads over 4 blocks of up to 288
+// tokens 9.5 us.  What bounds it: at 64 heads a tile of 74 KB takes about 2500 cycles, the operands that both products read out of
+// shared memory (240 KB at 128 bytes a cycle) with what arrives there; beside 74 KB of queries only two tiles fit, so a
+// tile's copies wait for the products of the tile before last.  At 16 heads, six blocks or so per CTA: each one's queries, first
+// tile and output, which overlap the next one's only in part.  Start, cut and join take 10 us of every call.
+// Looking ahead with L2 prefetches of pages cost 5 to 15 us (the copies queue behind them).
 //
 // Every mbarrier wait is bounded: when one gives up the CTA records it in the status word, stops waiting, still frees its
 // tensor memory and returns.
@@ -116,8 +124,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     DecodeShared<N>& sm = *reinterpret_cast<DecodeShared<N>*>(gen + (s_p + kPBytes - base));
     DecodeBarriers& bars = sm.bars;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const int group = blockIdx.x / a.head_groups, hg = blockIdx.x - group * a.head_groups;
-    const int h0 = hg * a.group_heads, heads = min(a.group_heads, a.H - h0);
+    const int group = blockIdx.x, heads = a.H;
     auto bar = [](uint64_t* p) { return smem_u32(p); };
 
     if (threadIdx.x == 0) {
@@ -157,7 +164,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     auto get_segment = [&](int i) { return take_segment(sm.ring, i, dead, status); };
 
     if (warp == 15) {
-        hand_out(a, sm.cut, sm.ring, sh, group, hg == 0, dead, status);
+        hand_out(a, sm.cut, sm.ring, sh, group, true, dead, status);
     } else if (warp == 12) {
         // ------------------------------------------------------------ TMA producer, a lane per page
         int it = 0, fresh = 0;
@@ -288,14 +295,14 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 // the latent parts, and the positional ones that do not turn; heads behind the last are filled with zeros
                 if (lane == 0 && !dead) {
                     mbar_expect_tx(bar(&bars.q_full), Sh::kQBytes - (a.turns ? N * 128 : 0));
-                    tma_load_q(s_q, &map_qc, h0, g.block, bar(&bars.q_full));
-                    if (!a.turns) tma_load_3d(s_q + (nc - 1) * (N * 128), &map_qr, 0, h0, g.block, bar(&bars.q_full));
+                    tma_load_q(s_q, &map_qc, 0, g.block, bar(&bars.q_full));
+                    if (!a.turns) tma_load_3d(s_q + (nc - 1) * (N * 128), &map_qr, 0, 0, g.block, bar(&bars.q_full));
                 }
                 if (a.turns) sm.turn[lane] = rope_cos_sin(ld_u64(a.turns + lane), position, a.amplitude);
                 __syncwarp();
             }
             if (a.turns) {
-                turn_queries<N>(a, g.block, h0, heads, tid, sm.turn, q_at);
+                turn_queries<N>(a, g.block, 0, heads, tid, sm.turn, q_at);
                 asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                 __syncwarp();
             }
@@ -445,7 +452,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 if (lane < 4) column[quarter][8 * (k >> 1) + col + (k & 1)] = x;
             }
             sync_128(id);
-            const int64_t part = ((int64_t)g.slot * a.head_groups + hg) * 64 + h1;
+            const int64_t part = (int64_t)g.slot * 64 + h1;
             const int own = heads - h1;            // heads of this half
             if (quarter == 0 && lane < 4)
 #pragma unroll
@@ -461,7 +468,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 #pragma unroll 1
             for (int mb = 0; mb < nm; ++mb) {
                 const int dim = mb * 128 + 32 * quarter + lane;
-                __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + g.block * a.io.o_block_stride + (h0 + h1) * a.io.o_head_stride + (dim & ~1);
+                __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + g.block * a.io.o_block_stride + h1 * a.io.o_head_stride + (dim & ~1);
                 constexpr int W = NH < 16 ? NH : 16;
 #pragma unroll
                 for (int c = 0; c < NH; c += W) {
@@ -502,6 +509,8 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 }
 
 // ---------------------------------------------------------------- joining a cut block's parts
+// (The last CTA of a block joining its parts itself was slower wherever blocks were cut, 83 us for 57 and 109 for 61: it reads
+// alone what here the whole device reads.)
 // One unit = 128 elements of a (cut block, head), four per lane of a warp.  Where no block has more than kFewParts parts a warp
 // takes a unit by itself, else a CTA's eight warps share a unit's parts.  (Short code: it runs once or twice per launch, so
 // fetching its instructions is part of its time.)
@@ -695,7 +704,7 @@ int launch(const CUtensorMap (&map)[4], const decode_args& a, cudaStream_t st) {
         }
         configured_dev[dev_id].store(true, std::memory_order_relaxed);
     }
-    return q8_launch_smem(latent_decode_kernel<L, N>, a.groups * a.head_groups, kDecodeThreads, smem, st, map[0], map[1], map[2], a);
+    return q8_launch_smem(latent_decode_kernel<L, N>, a.groups, kDecodeThreads, smem, st, map[0], map[1], map[2], a);
 }
 template <int N>
 int launch_latent(const CUtensorMap (&map)[4], const decode_args& a, cudaStream_t st) {

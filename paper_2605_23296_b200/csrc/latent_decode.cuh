@@ -228,14 +228,6 @@ __device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map,
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4}], [%5];\n"
         :: "r"(dst), "l"(map), "r"(0), "r"(head), "r"(block), "r"(bar) : "memory");
 }
-// One lane of the warp, chosen in the form that lets the compiler keep the operands of what that lane runs on the uniform
-// datapath: an MMA of 64 x 64 x 16 then goes out every 32 cycles, which is what its operands take out of shared memory, and
-// every 46 under a test of the lane's number (58 with the instruction alone predicated on it).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
-    return p != 0;
-}
 // Whether `x` holds in any of the 128 threads that meet at barrier `id`.
 __device__ __forceinline__ bool any_of_128(int id, bool x) {
     uint32_t r;
@@ -255,7 +247,6 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, float (&v)[16]) {
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-
 // ---------------------------------------------------------------- queries
 constexpr int kLoaderBarrier = 3;       // of the 128 threads that bring the queries
 // The turned positional parts of N query heads from h0 on (zeros behind the last of `heads`), to q_at(head, 16-byte piece), by
@@ -263,43 +254,43 @@ constexpr int kLoaderBarrier = 3;       // of the 128 threads that bring the que
 // layout.
 template <int N, class Q>
 __device__ __forceinline__ void turn_queries(const decode_args& a, int block, int h0, int heads, int tid, const float2* turn, Q&& q_at) {
-                    const __nv_bfloat16* qr = (const __nv_bfloat16*)a.io.q_rope + block * a.io.q_rope_block_stride + h0 * a.io.q_rope_head_stride;
-                    constexpr int kRounds = (N * 4 + 127) / 128;
-                    const int r = tid & 3;
-                    uint4 x[kRounds], y[kRounds];
-    #pragma unroll
-                    for (int k = 0; k < kRounds; ++k) {
-                        const int h = (tid >> 2) + 32 * k;
-                        x[k] = y[k] = make_uint4(0, 0, 0, 0);
-                        if (h < heads) {
-                            x[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * r);
-                            y[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * (r + 4));
-                        }
-                    }
-                    sync_128(kLoaderBarrier);
-    #pragma unroll
-                    for (int k = 0; k < kRounds; ++k) {
-                        const int h = (tid >> 2) + 32 * k;
-                        if (h >= N) break;
-                        uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, w[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
-                        if (a.interleaved) {
-    #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                u[e] = rope_turn(u[e], turn[4 * r + e]);
-                                w[e] = rope_turn(w[e], turn[4 * r + 16 + e]);
-                            }
-                        } else {
-    #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float2 c0 = turn[8 * r + 2 * e], c1 = turn[8 * r + 2 * e + 1];
-                                const float u0 = bf_lo(u[e]), u1 = bf_hi(u[e]), w0 = bf_lo(w[e]), w1 = bf_hi(w[e]);
-                                u[e] = bf_pack(turn_first(u0, w0, c0), turn_first(u1, w1, c1));
-                                w[e] = bf_pack(turn_second(u0, w0, c0), turn_second(u1, w1, c1));
-                            }
-                        }
-                        *q_at(h, r) = make_uint4(u[0], u[1], u[2], u[3]);
-                        *q_at(h, r + 4) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
+    const __nv_bfloat16* qr = (const __nv_bfloat16*)a.io.q_rope + block * a.io.q_rope_block_stride + h0 * a.io.q_rope_head_stride;
+    constexpr int kRounds = (N * 4 + 127) / 128;
+    const int r = tid & 3;
+    uint4 x[kRounds], y[kRounds];
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+        const int h = (tid >> 2) + 32 * k;
+        x[k] = y[k] = make_uint4(0, 0, 0, 0);
+        if (h < heads) {
+            x[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * r);
+            y[k] = ld_v4(qr + h * a.io.q_rope_head_stride + 8 * (r + 4));
+        }
+    }
+    sync_128(kLoaderBarrier);
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+        const int h = (tid >> 2) + 32 * k;
+        if (h >= N) break;
+        uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, w[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
+        if (a.interleaved) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                u[e] = rope_turn(u[e], turn[4 * r + e]);
+                w[e] = rope_turn(w[e], turn[4 * r + 16 + e]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 c0 = turn[8 * r + 2 * e], c1 = turn[8 * r + 2 * e + 1];
+                const float u0 = bf_lo(u[e]), u1 = bf_hi(u[e]), w0 = bf_lo(w[e]), w1 = bf_hi(w[e]);
+                u[e] = bf_pack(turn_first(u0, w0, c0), turn_first(u1, w1, c1));
+                w[e] = bf_pack(turn_second(u0, w0, c0), turn_second(u1, w1, c1));
+            }
+        }
+        *q_at(h, r) = make_uint4(u[0], u[1], u[2], u[3]);
+        *q_at(h, r + 4) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
 }
 
 }  // namespace
