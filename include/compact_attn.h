@@ -15,6 +15,10 @@
  * prefill in chunks beside the decode of other blocks (cpa_plan_create_chunked,
  * cpa_step_mixed), summaries of unknown length without reserved pages
  * (cpa_plan_create_dynamic) and whole events from host memory (cpa_event_host).
+ * Beside them: a cache in 8 bits on tables built on the device (cpa_tables_build,
+ * cpa_kv_append_q8, cpa_decode_q8), rotary positions (cpa_rope) and the attention of
+ * models whose keys and values come from one latent row per token
+ * (cpa_latent_append, cpa_latent_decode, cpa_latent_step, cpa_latent_prefill).
  *
  * The paper does not spell out attention; it is the textbook operation
  *     O[i,h,:] = sum_{j<=i} softmax_j(scale * q[i,h,:].k[j,g,:]) v[j,g,:],  g = h div G,
@@ -766,7 +770,7 @@ typedef struct cpa_latent_config {
     int32_t page_size;   /* 16 */
     float   scale;       /* softmax scale, normally 1 / sqrt(nope_dim + rope_dim) */
     float   norm_eps;    /* added to the mean square of a new latent part, >= 0 */
-    int32_t num_sms;     /* SMs a launch of the decode may fill, 0 = all; at most 4095 */
+    int32_t num_sms;     /* SMs a launch of the decode may fill, 0 = all; at most 4095 (more than 64 heads: two at least) */
 } cpa_latent_config;
 
 /* The cpa_config that the calls on the tables of a latent cache take.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
