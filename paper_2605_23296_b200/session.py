@@ -407,6 +407,8 @@ class LatentSession:
         if norm_weight is not None and (norm_weight.dtype != torch.bfloat16 or norm_weight.shape != (latent_dim,) or
                                         not norm_weight.is_contiguous()):
             raise ValueError(f"norm_weight: contiguous bf16 [{latent_dim}] is wanted")
+        if rope is not None and rope.cfg.rope_dim != 64:
+            raise ValueError(f"rope: 64 rotated elements are wanted, not {rope.cfg.rope_dim}")
         self.cfg = B.cpa_latent_config(num_heads, latent_dim, 64, 128, 128, 16, self.scale, norm_eps, num_sms)
         tables_cfg = B.cpa_latent_tables_config(self.cfg)
         plan_cfg = B.cpa_latent_plan_config(self.cfg)
@@ -426,6 +428,11 @@ class LatentSession:
         self.workspace = torch.empty(B.cpa_latent_decode_workspace_bytes(self.cfg), dtype=torch.uint8, **on)
         self.lens = torch.zeros(self.B, dtype=torch.int32, **on)
         self._lens_next = torch.empty_like(self.lens)
+        for name, t in (("norm_weight", norm_weight), ("rope", rope and rope.turns)):
+            if t is not None and t.device != self.lens.device:
+                B.cpa_plan_destroy(self.plan)
+                self.plan = None
+                raise ValueError(f"{name}: on {self.lens.device}, not on {t.device}")
         start = np.zeros(self.B, dtype=np.int64) if first is None else np.asarray(first, dtype=np.int64)
         self.first = None if first is None else torch.as_tensor(start.astype(np.int32), **on)
         self.cu = torch.as_tensor(np.concatenate([[0], np.cumsum(self.block_lens)]).astype(np.int32), **on)

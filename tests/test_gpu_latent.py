@@ -620,6 +620,61 @@ def test_two_caches_on_two_streams(B):
         caches[i][0].check(want[i], *caches[i][1][2:])
 
 
+@pytest.mark.parametrize("H", [64, 128])
+def test_graphs_of_two_caches_replayed_at_once(B, H):
+    # a step and the decode behind it, captured for each of two caches with tables and workspaces of their own, replayed side by side
+    rng = np.random.default_rng(H)
+    w, first = torch.ones(512, dtype=torch.bfloat16, device="cuda"), _i32([3, 0, 99])
+    rope, runs = Rope(B), []
+    for i in range(2):
+        lens = [1500, 0, 77] if i else [9, 2300, 640]
+        c = Cache(B, [n + 1 for n in lens], 512, H, seed=i, rope=rope)
+        c.fill(lens, rng)
+        qc, qr = c.queries(rng)[:2]
+        x = _bf16(rng.standard_normal((3, 576)))[0]
+        out, o, o2 = torch.empty_like(c.lens), *(torch.empty(3, H, 512, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+
+        def run(c=c, qc=qc, qr=qr, x=x, out=out, o=o, o2=o2):
+            assert B.cpa_latent_step(c.cfg, c.dims, c.tables, rope.cfg, rope.turns, B.latent_io(qc, qr, o), x, 576, w, first, c.lens, out, None,
+                                     c.pool, c.ws, _stream()) == 0
+            assert B.cpa_latent_decode(c.cfg, c.dims, c.tables, B.latent_io(qc, qr, o2), out, None, c.pool, c.ws, _stream()) == 0
+        run()                                             # (the step stores the same row again whenever it is repeated)
+        torch.cuda.synchronize()
+        want = [o.clone(), o2.clone(), out.clone()]
+        g, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(g, stream=stream):
+            run()
+        runs.append((g, stream, (o, o2, out), want, c, run))         # (run holds the graph's inputs)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for g, stream, *_ in runs:
+            with torch.cuda.stream(stream):
+                g.replay()
+    torch.cuda.synchronize()
+    for _, _, got, want, c, _ in runs:
+        assert all(torch.equal(x, y) for x, y in zip(got, want)) and c.status() == 0
+
+
+@pytest.mark.parametrize("H", [4, 72])
+def test_few_blocks_with_tokens_among_many_without(B, H):
+    rng = np.random.default_rng(H)
+    n = 6000
+    lens = np.zeros(n, dtype=np.int64)
+    lens[[0, 2700, n - 1]] = [700, 1, 130]
+    c = Cache(B, lens, 128, H)
+    c.fill(list(lens), rng)
+    q = [torch.randn(n, H, e, device="cuda").bfloat16() for e in (128, 64)]
+    o = c.decode(*q)
+    assert c.status() == 0
+    at = np.flatnonzero(lens)
+    on = torch.as_tensor(at, device="cuda")
+    cf, rf = ({b: _np(t[b]) for b in at} for t in q)
+    c.check(o, cf, rf, at, "few")
+    o[on] = 0
+    assert (o == 0).all()
+
+
 # ------------------------------------------------------------------------------------------------ expanded attention
 
 def _prefill(B, lens, H, rng, spread=1.0, stride=576, num_sms=0, scale=192 ** -0.5):

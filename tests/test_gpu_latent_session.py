@@ -191,3 +191,12 @@ def test_rotary_ahead_of_a_grouped_query_event():
     assert_attention_close(tensor_to_bits(o), oa.prefill(tensor_to_bits(q), tensor_to_bits(k), w.v, cu, w.scale), "turned prompts")
     assert s.status() == 0
     s.close()
+
+
+def test_weights_and_frequencies_elsewhere_are_refused():
+    from paper_2605_23296_b200.session import LatentSession, Rotary
+    w = torch.ones(128, dtype=torch.bfloat16)
+    for bad in (dict(norm_weight=w), dict(norm_weight=w.cuda().float()), dict(norm_weight=w[:64].cuda()), dict(rope=Rotary(64, device="cpu")),
+                dict(rope=Rotary(32))):
+        with pytest.raises(ValueError):
+            LatentSession([10], 0, 8, [0], 1, latent_dim=128, **bad)
