@@ -155,8 +155,13 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     }
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     look_ahead(a);
+    if (threadIdx.x == 12 * 32) {
+        prefetch_map(&map);
+        prefetch_map(&map_qc);
+        prefetch_map(&map_qr);
+    }
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    const share sh = cut_shares(a, sm.cut, group);
+    sum_costs(a, sm.cut);
     const uint32_t tmem = bars.tmem_base;
     constexpr uint32_t kColO = 2 * N;
     bool dead = false;
@@ -165,7 +170,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     auto get_segment = [&](int i) { return take_segment(sm.ring, i, dead, status); };
 
     if (warp == 15) {
-        hand_out(a, sm.cut, sm.ring, sh, group, true, dead, status);
+        hand_out(a, sm.cut, sm.ring, group, true, dead, status);
     } else if (warp == 12) {
         // ------------------------------------------------------------ TMA producer, a lane per page
         int it = 0, fresh = 0;
@@ -317,7 +322,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 if (lane == 0) mbar_arrive(bar(&bars.row_ready));
             }
         }
-        write_zero_rows(a, tid);
+        keep_books(a, tid);
     } else {
         // ------------------------------------------------------------ softmax and epilogue
         constexpr int NH = N / 2, J = NH / 8;  // heads of a half; groups of eight, of which this thread has two heads and two tokens

@@ -68,8 +68,6 @@ __device__ __forceinline__ __nv_bfloat16* slot_of(const decode_args& a, const se
     return a.pool + ((int64_t)page * kPage + at % kPage) * (L + kRopeDim);
 }
 
-// First cost of group g's share when `total` is dealt to `groups`.
-__device__ __forceinline__ int64_t share_start(int64_t total, int g, int groups) { return (total * g + groups - 1) / groups; }
 __device__ __forceinline__ int tiles_of(int len) { return (int)(((int64_t)len + kTile - 1) / kTile); }
 
 // What every CTA reads first is brought to L2 ahead of the wait for the launches before (L2 is coherent: what is written until
@@ -85,56 +83,42 @@ __device__ __forceinline__ void look_ahead(const decode_args& a) {
 }
 
 // ---------------------------------------------------------------- the cut
-// The tiles of all blocks in a row, each block's own cost in front of its tiles, are dealt to the groups in equal parts.
-struct share { int64_t lo, hi, total; int used; };      // costs [lo, hi) of `total`, which `used` groups have
-struct CutShared {
-    int64_t scan[kDecodeThreads / 32];
-    int64_t start_cost;               // cost in front of start_block, where the walk to the share's first tile begins
-    int start_block;
+// The tiles of all blocks in a row, each block's own cost in front of its tiles, are dealt to the groups in equal parts.  (A page
+// list has fewer than 2^31 entries, so all costs together are below 2^29 + 3 * 2^20.)
+// `total` in `used` shares of q or, the first rem ones, q + 1.
+struct shares {
+    int total, used, q, rem;
+    __device__ __forceinline__ int start(int g) const { return q * g + min(g, rem); }
+    __device__ __forceinline__ int group_of(int cost) const {
+        const int big = rem * (q + 1);
+        return cost < big ? cost / (q + 1) : rem + (cost - big) / q;
+    }
 };
-// By all threads of a CTA (two barriers).  The blocks' books (new lengths, status) are shared out to the CTAs on the way.
-__device__ __forceinline__ share cut_shares(const decode_args& a, CutShared& sm, int group) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int per = (a.B + kDecodeThreads - 1) / kDecodeThreads, b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
-    int64_t cost = 0;
+struct CutShared { int cost[kDecodeThreads / 32]; };      // of each warp's run of blocks
+__device__ __forceinline__ int blocks_per_thread(const decode_args& a) { return (a.B + kDecodeThreads - 1) / kDecodeThreads; }
+// By all threads of a CTA, with a barrier.  (What follows from the costs is left to the warp that hands the segments out: all of
+// this runs once in a launch, and takes as long as its instructions take to arrive.)
+__device__ __forceinline__ void sum_costs(const decode_args& a, CutShared& sm) {
+    const int per = blocks_per_thread(a), b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
+    int cost = 0;
+#pragma unroll 1
     for (int b = b0; b < b1; ++b) {
         const block_state s = block_of(b, a);
         if (s.len > 0) cost += tiles_of(s.len) + kBlockCost;
-        if (b % (int)gridDim.x == (int)blockIdx.x) {
-            if (s.status) atomicCAS(a.t.header, 0, s.status);
-            if (a.x) a.lens_out[b] = ld_i32(a.lens + b) + (s.on ? 1 : 0);
-        }
     }
-    int64_t inc = cost;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += v;
-    }
-    if (lane == 31) sm.scan[warp] = inc;
-    if (threadIdx.x == 0) {
-        sm.start_block = a.B;
-        sm.start_cost = 0;
-    }
+    cost = __reduce_add_sync(0xffffffffu, cost);
+    if ((threadIdx.x & 31) == 0) sm.cost[threadIdx.x >> 5] = cost;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    int64_t before = inc - cost, total = 0;
-    for (int w = 0; w < kDecodeThreads / 32; ++w) {
-        if (w < warp) before += sm.scan[w];
-        total += sm.scan[w];
+}
+__device__ __forceinline__ int inclusive_sum(int v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += x;
     }
-    share r;
-    r.total = total;
-    r.used = (int)max((int64_t)1, min((int64_t)a.groups, total / kMinRange));
-    r.lo = group < r.used ? share_start(total, group, r.used) : total;
-    r.hi = group < r.used ? share_start(total, group + 1, r.used) : total;
-    if (cost > 0 && before <= r.lo && r.lo < before + cost) {
-        sm.start_block = b0;
-        sm.start_cost = before;
-    }
-    __syncthreads();
-    return r;
+    return v;
 }
 
 // ---------------------------------------------------------------- segments
@@ -158,34 +142,37 @@ __device__ __forceinline__ segment take_segment(SegmentRing& ring, int i, bool& 
     if (dead) s.block = -1;
     return s;
 }
-// The share's segments in order, behind them one of block -1, by a whole warp; and the record of a block that goes on behind it.
-__device__ __forceinline__ void hand_out(const decode_args& a, const CutShared& sm, SegmentRing& ring, const share& sh, int group, bool record,
-                                         bool& dead, int32_t* status) {
+// The segments of group `group` in order, behind them one of block -1, by a whole warp; and the record of a block that goes on
+// behind the group's share.
+__device__ __forceinline__ void hand_out(const decode_args& a, const CutShared& sm, SegmentRing& ring, int group, bool record, bool& dead,
+                                         int32_t* status) {
     const int lane = threadIdx.x & 31;
     int n = 0;
     int2 cut = make_int2(-1, 0);
-    int64_t c = sm.start_cost;
     auto put = [&](const segment& s) {
         mbar_wait(smem_u32(&ring.empty[n % kSegRing]), ((uint32_t)(n / kSegRing) & 1u) ^ 1u, dead, status, kSpinLimit);
         ring.seg[n % kSegRing] = s;
         mbar_arrive(smem_u32(&ring.full[n % kSegRing]));
         ++n;
     };
-    if (sh.lo < sh.hi)
-        for (int b = sm.start_block; b < a.B && c < sh.hi; b += 32) {
+    const int sums = inclusive_sum(lane < kDecodeThreads / 32 ? sm.cost[lane] : 0, lane);
+    shares sh;
+    sh.total = __shfl_sync(0xffffffffu, sums, 31);
+    sh.used = max(1, min(a.groups, sh.total / kMinRange));
+    sh.q = sh.total / sh.used;
+    sh.rem = sh.total - sh.q * sh.used;
+    if (group < sh.used && sh.total > 0) {
+        const int lo = sh.start(group), hi = sh.start(group + 1);
+        const int run = __popc(__ballot_sync(0xffffffffu, sums <= lo));         // the run of blocks in which the share starts
+        int c = run ? __shfl_sync(0xffffffffu, sums, run - 1) : 0;
+        for (int b = run * 32 * blocks_per_thread(a); b < a.B && c < hi; b += 32) {
             block_state s{0, 0, 0, false};
             if (b + lane < a.B) s = block_of(b + lane, a);
-            const int tiles = tiles_of(s.len);
-            const int64_t mine = s.len > 0 ? tiles + kBlockCost : 0;
-            int64_t at = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t v = __shfl_up_sync(0xffffffffu, at, o);
-                if (lane >= o) at += v;
-            }
-            const int64_t first = c + at - mine + kBlockCost;      // cost at which the block's first tile lies
+            const int tiles = tiles_of(s.len), mine = s.len > 0 ? tiles + kBlockCost : 0;
+            const int at = inclusive_sum(mine, lane);
+            const int first = c + at - mine + kBlockCost;          // cost at which the block's first tile lies
             c += __shfl_sync(0xffffffffu, at, 31);
-            const int j0 = (int)min((int64_t)tiles, max((int64_t)0, sh.lo - first)), j1 = (int)min((int64_t)tiles, max((int64_t)0, sh.hi - first));
+            const int j0 = min(tiles, max(0, lo - first)), j1 = min(tiles, max(0, hi - first));
             uint32_t todo = __ballot_sync(0xffffffffu, s.len > 0 && j1 > j0);
             while (todo) {
                 const int who = __ffs(todo) - 1;
@@ -193,23 +180,29 @@ __device__ __forceinline__ void hand_out(const decode_args& a, const CutShared& 
                 if (lane == who) {
                     const bool whole = j0 == 0 && j1 == tiles;
                     put({b + lane, j0, j1 - j0, s.len, s.ip, whole ? -1 : 2 * group + (j0 == 0 ? 1 : 0), {0, 0}});
-                    if (j0 == 0 && j1 < tiles) cut = make_int2(b + lane, (int)((first + tiles - 1) * sh.used / sh.total) - group + 1);
+                    if (j0 == 0 && j1 < tiles) cut = make_int2(b + lane, sh.group_of(first + tiles - 1) - group + 1);
                 }
                 n = __shfl_sync(0xffffffffu, n, who);
             }
             dead = __any_sync(0xffffffffu, dead);
             if (dead) break;
         }
+    }
     if (lane == 0) put({-1, 0, 0, 0, 0, 0, {0, 0}});
     const uint32_t has = __ballot_sync(0xffffffffu, cut.x >= 0);
     const int who = has ? __ffs(has) - 1 : 0;
     if (record && lane == who) a.cuts[group] = cut;
 }
-// Blocks without a token: rows of zeros, by the 128 threads `tid` of a CTA.
-__device__ __forceinline__ void write_zero_rows(const decode_args& a, int tid) {
+// The blocks' books (status, new lengths), shared out to the CTAs, and rows of zeros for blocks without a token, by the 128 threads
+// `tid` of a CTA.
+__device__ __forceinline__ void keep_books(const decode_args& a, int tid) {
     const int pieces = a.L / 8;
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
         const block_state s = block_of(b, a);
+        if (tid == 0) {
+            if (s.status) atomicCAS(a.t.header, 0, s.status);
+            if (a.x) a.lens_out[b] = s.on ? s.len : ld_i32(a.lens + b);
+        }
         if (!s.on || s.len > 0) continue;
         __nv_bfloat16* o = (__nv_bfloat16*)a.io.o + b * a.io.o_block_stride;
         for (int e = tid; e < a.H * pieces; e += 128)
@@ -218,6 +211,7 @@ __device__ __forceinline__ void write_zero_rows(const decode_args& a, int tid) {
 }
 
 // ---------------------------------------------------------------- PTX
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];\n" :: "l"(map) : "memory"); }
 __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap* map, int group, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %3}], [%4];\n"

@@ -176,10 +176,15 @@ latent_decode_pair_kernel(const __grid_constant__ CUtensorMap map, const __grid_
     }
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     look_ahead(a);
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    const share sh = cut_shares(a, sm.cut, group);
+    if (threadIdx.x == 12 * 32) {
+        prefetch_map(&map);
+        prefetch_map(&map_half);
+        prefetch_map(&map_qc);
+        prefetch_map(&map_qr);
+    }
     cluster_sync_all();      // both CTAs' barriers are there before anything arrives at them from the other side
-    tc_fence_after();
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    sum_costs(a, sm.cut);
     const uint32_t tmem = bars.tmem_base;
     constexpr uint32_t kColO = 64;             // two score buffers of 32 columns
     bool dead = false;
@@ -191,7 +196,7 @@ latent_decode_pair_kernel(const __grid_constant__ CUtensorMap map, const __grid_
     };
 
     if (warp == 15) {
-        hand_out(a, sm.cut, sm.ring, sh, group, rank == 0, dead, status);
+        hand_out(a, sm.cut, sm.ring, group, rank == 0, dead, status);
     } else if (warp == 12) {
         // ------------------------------------------------------------ TMA producer: lanes 0-1 this CTA's pages of K, lanes 4-7 all
         // pages' halves of V
@@ -362,7 +367,7 @@ latent_decode_pair_kernel(const __grid_constant__ CUtensorMap map, const __grid_
                 ++fresh;
             }
         }
-        write_zero_rows(a, tid);
+        keep_books(a, tid);
     } else {
         // ------------------------------------------------------------ softmax and epilogue
         // This thread: head `head` (TMEM lane row + 64 * half), tokens 32 half + 16 part .. + 15 of a tile.
