@@ -150,7 +150,9 @@ extern "C" int cpa_latent_append(const cpa_latent_config* cfg, const cpa_table_d
     a.x_row = x_row_stride;
     a.B = dims->num_blocks;
     a.rows = num_rows;
-    a.at_once = num_rows > 2 * 148 * 64 ? 2 : 1;              // (two waves of warps, by one row each)
+    // two rows of a warp in flight where there are more than the device's warps (latent parts of 256: 6746 rows 5.1 us, 5.5 by one row
+    // each; 11380 rows 6.9 and 7.5; below, 2116 rows 4.1 and 3.4)
+    a.at_once = num_rows > 148 * 32 ? 2 : 1;
     a.row_ctas = (int)std::min<int64_t>(((int64_t)num_rows + kWarps * a.at_once - 1) / (kWarps * a.at_once), 1 << 20);
     const int grid = a.row_ctas + std::min((a.B + kWarps - 1) / kWarps, 1 << 16);
     const bool wide = latent_aligned(x, 16) && x_row_stride % 8 == 0;

@@ -25,10 +25,10 @@
 //
 // Measured (latent parts of 512, caches larger than L2): 64 heads over 32 blocks of 1024..8192 tokens, 195 MB, 57 us (3.4 TB/s);
 // 16 heads over 192 blocks of 512..1024 with a step's new rows, 175 MB, 46 us (3.8 TB/s); 16 heads over 4 blocks of up to 288
-// tokens 9.5 us.  What bounds it: the stream of pages runs at 5.8 TB/s once it runs (a tile of 74 KB every 3550 cycles at 64
+// tokens 8.8 us.  What bounds it: the stream of pages runs at 5.8 TB/s once it runs (a tile of 74 KB every 3550 cycles at 64
 // heads, 3150 at 16: memory's latency under that load, 3400 cycles, and the chain of a tile, twice over in two stages; beside 74 KB
 // of queries no third tile fits, and the operands of both products take 2500 cycles of shared memory's time as it is).  Around it:
-// 3.7 us from the start to the first copy (cut, segment, page list: loads that depend on one another), 3.5 us for the partials
+// 3 us from the start to the first copy (cut, segment, page list: loads that depend on one another), 3.5 us for the partials
 // (128 KB from every CTA at 64 heads, 5.5 TB/s), 3.5 us from the median CTA to the last, 1 us to the join and 5 to 7.5 us in it.
 // Looking ahead with L2 prefetches of pages cost 5 to 15 us (the copies queue behind them).
 //
