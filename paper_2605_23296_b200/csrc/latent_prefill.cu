@@ -13,11 +13,17 @@
 // one ring of eight 16 KB pieces in the order of their use: a K tile is three pieces (column blocks of 128 keys x 64 elements), a
 // V tile two (64 keys x 128 elements).  While a V tile and the next K tile are in use three pieces are under way; rings of their
 // own would hold two K tiles and one V tile, with nothing under way while the one V tile is read.
-// Tensor memory: two score buffers of 128 columns (one per sub-tile, or both for a lone one) and two outputs of 128.
+// A lone sub-tile (a block's last 128 rows, or all of a short block) takes the two sub-tiles' places in turn, and the two score
+// buffers step by step: the next unit's queries are there and its first scores are made while this one's last softmax and
+// output run.  A last tile of at most 64 keys is worked through in groups of 32, by the warps that have rows of the block and with
+// the MMAs that its keys need.  (177 blocks of 18 tokens, 20 heads: 82 us without either, 72 with the first, 42 with both.  Working every
+// last tile through in groups spares half of a diagonal's exponentials and was slower, 3.4 ms for the long prompts below: the
+// loop of whole tiles loses registers to it.  Loading only the parts of a short tile that hold rows: 63 us for 42.)
+// Tensor memory: two score buffers of 128 columns (one per sub-tile, or step by step for lone ones) and two outputs of 128.
 // Warps 0-3, 4-7 softmax + epilogue of sub-tile 0, 1; warp 8 TMA producer; warp 9 MMA issuer and owner of the tensor memory;
 // warps 10-11 idle, they complete the warpgroup whose registers go to the softmax.
-// Keys behind a block's end are the next block's: their scores are masked by index and their V rows cleared, so that what they
-// hold (infinities, NaN) stays theirs.
+// Keys behind a block's end are the next block's: their scores are masked by index and those of their V rows that an MMA reads
+// are cleared, so that what they hold (infinities, NaN) stays theirs.
 // Measured: 32 prompts of 1024..8192 tokens, 16 heads: 3.33 ms, 1.05 PFLOP/s of the products below the diagonal, in a row (under the power
 // limit; a single call 2.96 ms).  A pair of steps (both sub-tiles, one K/V tile) takes 3380 cycles, of which the tensor core is busy
 // 2560; the rest is the softmax of a sub-tile waiting for its scores: buffers for the scores of the next tile as well would fit
@@ -34,6 +40,7 @@ namespace {
 constexpr int kPieces = 8;                                    // of the ring
 constexpr uint32_t kPieceBytes = 16384;
 constexpr int kTilePieces = 5;                                // K: 3, V: 2
+constexpr int kShortKeys = 64;                                // a last tile of at most so many keys is worked through in parts
 constexpr uint32_t kQTileBytes = 3 * kPieceBytes;             // 128 rows x 192 elements
 constexpr int kV = 128;                                       // elements of a value
 constexpr uint32_t kOutCol = 256;                             // outputs behind the two score buffers
@@ -50,6 +57,15 @@ constexpr int kPrefillSmem = 2 * (int)kQTileBytes + kPieces * (int)kPieceBytes +
 // See TcWork in prefill_tc.cu: sub-tile u sees KV tiles 0 .. t0 + u, the last of which touches the diagonal.
 struct PrefillWork { int h, tok0, L, q0, t0, n_sub, n_total; bool valid; };
 
+// A count for each sub-tile, in registers where the sub-tile is known at run time only.
+struct pair_count {
+    uint32_t n0 = 0, n1 = 0;
+    __device__ __forceinline__ uint32_t of(int u) const { return u ? n1 : n0; }
+    __device__ __forceinline__ void add(int u) {
+        n0 += u ? 0u : 1u;
+        n1 += u ? 1u : 0u;
+    }
+};
 // by one thread; descriptors as halves
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -139,7 +155,8 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         if (warp == 8 && elect_one()) {
             // ------------------------------------------------------------ TMA producer
             int n = 0;                    // pieces loaded: slot n % kPieces, use n / kPieces
-            uint32_t q_loads[2] = {0, 0};
+            pair_count q_loads;
+            int lone = 0;
             PrefillWork w;
             Rec rec;
             fetch(fetch_code(0), rec);
@@ -149,14 +166,14 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 fetch(code, rec);
                 code = fetch_code(k + 2);
                 if (!w.valid) continue;
-                auto load_q = [&](int u) {
-                    tc_wait(bar(&bars.q_empty[u]), (q_loads[u] & 1u) ^ 1u, dead, ix.status);
+                auto load_q = [&](int u, int row) {
+                    tc_wait(bar(&bars.q_empty[u]), (q_loads.of(u) & 1u) ^ 1u, dead, ix.status);
                     if (dead) return;
-                    ++q_loads[u];
+                    q_loads.add(u);
                     mbar_expect_tx(bar(&bars.q_full[u]), kQTileBytes);
 #pragma unroll
                     for (int c = 0; c < 3; ++c)
-                        tma_load_2d(s_q + u * kQTileBytes + c * kPieceBytes, &tm_q, w.h * 192 + 64 * c, w.tok0 + w.q0 + u * kTileM,
+                        tma_load_2d(s_q + u * kQTileBytes + c * kPieceBytes, &tm_q, w.h * 192 + 64 * c, w.tok0 + row,
                                     bar(&bars.q_full[u]));
                 };
                 // slot of the next piece, once it is free; its barrier expects the whole piece
@@ -169,7 +186,12 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     }
                     return s;
                 };
-                for (int u = 0; u < w.n_sub; ++u) load_q(u);
+                if (w.n_sub == 2) {
+                    load_q(0, w.q0);
+                    load_q(1, w.q0 + kTileM);
+                } else {
+                    load_q(lone++ & 1, w.q0);
+                }
                 for (int j = 0; j < w.n_total && !dead; ++j) {
                     const int row = w.tok0 + j * kTileN;
 #pragma unroll
@@ -191,7 +213,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             }
             if (dead) {      // copies issued last may still be on their way into this CTA's shared memory
                 for (int u = 0; u < 2; ++u)
-                    if (q_loads[u] > 0) mbar_drain(bar(&bars.q_full[u]), (q_loads[u] - 1u) & 1u, kDrainLimit);
+                    if (q_loads.of(u) > 0) mbar_drain(bar(&bars.q_full[u]), (q_loads.of(u) - 1u) & 1u, kDrainLimit);
                 for (int t = max(0, n - kPieces); t < n; ++t)
                     mbar_drain(bar(&bars.full[t % kPieces]), (uint32_t)(t / kPieces) & 1u, kDrainLimit);
             }
@@ -201,7 +223,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             const uint64_t dk = smem_desc(0, 16, 1024), dv = smem_desc(0, kPieceBytes / 2, 1024);
             const uint32_t k_hi = (uint32_t)(dk >> 32), v_hi = (uint32_t)(dv >> 32);
             const uint32_t q_lo = (uint32_t)dk | (s_q >> 4), k_lo = (uint32_t)dk | (s_ring >> 4), v_lo = (uint32_t)dv | (s_ring >> 4);
-            uint32_t n_qk[2] = {0, 0}, n_pv[2] = {0, 0}, q_uses[2] = {0, 0};
+            pair_count n_qk, n_pv, q_uses;
             int kt0 = 0;                                    // K/V tiles of earlier units
             // piece c of tile kt: 0-2 of K, 3-4 of V
             auto slot = [](int kt, int c) { return (uint32_t)(kt * kTilePieces + c) % kPieces; };
@@ -223,28 +245,40 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 #pragma unroll
                     for (int k = 0; k < 4; ++k) mma_ss(d, a + c * (kPieceBytes >> 4) + k * 2, b + k * 2, k_hi, idesc_qk, (c | k) != 0);
                 }
-                commit(bar(&bars.s_full[u][n_qk[u] & 3u]));
-                ++n_qk[u];
+                commit(bar(&bars.s_full[u][n_qk.of(u) & 3u]));
+                n_qk.add(u);
             };
-            auto pv = [&](int u, int buf, int kt, uint32_t acc0) {   // O_u += P[buf] V[tile kt], 64 keys at a time
-                const uint32_t d = tmem + kOutCol + u * kV, a = tmem + buf * 128;
+            // O_u += P[buf] V[tile kt], 64 keys at a time, `ks` times 16 keys in all
+            auto pv = [&](int u, int buf, int kt, uint32_t acc0, int ks) {
+                const uint32_t d = tmem + kOutCol + u * kV, a = tmem + buf * 128, n = n_pv.of(u);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     wait_piece(kt, 3 + half);
-                    tc_wait(bar(half ? &bars.p_full[u][n_pv[u] & 3u] : &bars.p_half[u][n_pv[u] & 3u]), (n_pv[u] >> 2) & 1u, dead, ix.status);
+                    tc_wait(bar(half ? &bars.p_full[u][n & 3u] : &bars.p_half[u][n & 3u]), (n >> 2) & 1u, dead, ix.status);
                     if (dead) return;
                     tc_fence_after();
                     const uint32_t b = v_lo + slot(kt, 3 + half) * (kPieceBytes >> 4);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_ts(d, a + half * 32 + k * 8, b + k * (2048 >> 4), v_hi, idesc_pv, half + k > 0 ? 1u : acc0);
+                    for (int k = 0; k < 4; ++k)
+                        if (half * 4 + k < ks) mma_ts(d, a + half * 32 + k * 8, b + k * (2048 >> 4), v_hi, idesc_pv, half + k > 0 ? 1u : acc0);
                 }
                 commit(bar(&bars.pv_done[u]));
-                ++n_pv[u];
+                n_pv.add(u);
             };
+            auto steps_of = [](int keys) { return keys <= kShortKeys ? (keys + 15) / 16 : kTileN / 16; };
             auto wait_q = [&](int u) {
-                tc_wait(bar(&bars.q_full[u]), q_uses[u] & 1u, dead, ix.status);
-                ++q_uses[u];
+                tc_wait(bar(&bars.q_full[u]), q_uses.of(u) & 1u, dead, ix.status);
+                q_uses.add(u);
             };
+            // A lone sub-tile's output product waits until the scores of the step behind it are queued, the next unit's first one too.
+            struct { int u, buf, kt, acc0, ks; bool on; } last = {0, 0, 0, 0, 0, false};
+            auto finish = [&]() {
+                if (!last.on || dead) return;
+                pv(last.u, last.buf, last.kt, (uint32_t)last.acc0, last.ks);
+                release(last.kt, 3, 5);
+                last.on = false;
+            };
+            int lone = 0, lone_steps = 0;
             PrefillWork w;
             Rec rec;
             fetch(fetch_code(0), rec);
@@ -255,8 +289,9 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 code = fetch_code(rd + 2);
                 if (!w.valid) continue;
                 const int t0 = w.t0;
-                wait_q(0);
                 if (w.n_sub == 2) {
+                    finish();
+                    wait_q(0);
                     // PV of a sub-tile's step, then the scores of its next one into the buffer that PV has read; the other
                     // sub-tile's softmax runs meanwhile
                     wait_q(1);
@@ -266,35 +301,32 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     if (t0 == 0) commit(bar(&bars.q_empty[0]));
                     for (int j = 0; j <= t0 && !dead; ++j) {      // tiles both sub-tiles have; sub-tile 1 also has tile t0 + 1
                         const int kt = kt0 + j;
-                        pv(0, 0, kt, j > 0);
+                        pv(0, 0, kt, j > 0, 8);
                         if (j < t0) qk(0, 0, kt + 1);
                         if (j == t0 - 1) commit(bar(&bars.q_empty[0]));
-                        pv(1, 1, kt, j > 0);
+                        pv(1, 1, kt, j > 0, 8);
                         release(kt, 3, 5);
                         qk(1, 1, kt + 1);
                         release(kt + 1, 0, 3);
                         if (j == t0) commit(bar(&bars.q_empty[1]));
                     }
-                    if (!dead) pv(1, 1, kt0 + t0 + 1, 1u);
+                    if (!dead) pv(1, 1, kt0 + t0 + 1, 1u, steps_of(w.L - (t0 + 1) * kTileN));
                     release(kt0 + t0 + 1, 3, 5);
                 } else {
-                    // one sub-tile: the scores run one tile ahead in the other buffer
-                    qk(0, 0, kt0);
-                    release(kt0, 0, 3);
-                    if (t0 == 0) commit(bar(&bars.q_empty[0]));
+                    const int u = lone++ & 1;
+                    wait_q(u);
                     for (int j = 0; j <= t0 && !dead; ++j) {
-                        const int kt = kt0 + j;
-                        if (j < t0) {
-                            qk(0, (j + 1) & 1, kt + 1);
-                            release(kt + 1, 0, 3);
-                            if (j == t0 - 1) commit(bar(&bars.q_empty[0]));
-                        }
-                        pv(0, j & 1, kt, j > 0);
-                        release(kt, 3, 5);
+                        const int buf = lone_steps++ & 1;
+                        qk(u, buf, kt0 + j);
+                        release(kt0 + j, 0, 3);
+                        if (j == t0) commit(bar(&bars.q_empty[u]));
+                        finish();
+                        last = {u, buf, kt0 + j, j > 0, j == t0 ? steps_of(w.L - t0 * kTileN) : 8, true};
                     }
                 }
                 kt0 += w.n_total;
             }
+            finish();
             if (dead) {      // MMAs queued before may still be running; tensor memory is not freed under them
                 commit(bar(&bars.drain));
                 mbar_drain(bar(&bars.drain), 0u, kDrainLimit);
@@ -308,7 +340,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_o = tmem + lane_addr + kOutCol + u * kV;
         uint32_t n_steps = 0;
-        int kt0 = 0;
+        int kt0 = 0, lone = 0, lone_steps = 0;
         PrefillWork w;
         Rec rec;
         fetch(fetch_code(0), rec);
@@ -319,12 +351,14 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             fetch(code, rec);
             code = uniform(fetch_code(rd + 2));
             if (!w.valid) continue;
-            if (u < w.n_sub) {
-                const int n_kv = w.t0 + 1 + u;
+            if (w.n_sub == 2 || u == (lone & 1)) {
+                const int sub = w.n_sub == 2 ? u : 0;
+                const int n_kv = w.t0 + 1 + sub;
                 const int left = w.L - (n_kv - 1) * kTileN;                // keys of the last tile that are the block's
+                const int n_full = left <= kShortKeys ? n_kv - 1 : n_kv;   // tiles that are worked through whole
                 float m_used = -INFINITY, l_run = 0.f;
-                for (int j = 0; j < n_kv; ++j, ++n_steps) {
-                    const uint32_t t_s = tmem + lane_addr + (w.n_sub == 2 ? u : j & 1) * 128;
+                for (int j = 0; j < n_full; ++j, ++n_steps) {
+                    const uint32_t t_s = tmem + lane_addr + (w.n_sub == 2 ? u : (lone_steps + j) & 1) * 128;
                     tc_wait(bar(&bars.s_full[u][n_steps & 3u]), (n_steps >> 2) & 1u, dead, ix.status);
                     tc_fence_after();
                     uint32_t sv[4][32];
@@ -409,13 +443,84 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     tc_fence_before();
                     mbar_arrive(bar(&bars.p_full[u][n_steps & 3u]));
                 }
+                if (n_full < n_kv) {
+                    // ---- a last tile of few keys, and as many rows: 32 keys at a time, and only by the warps that have rows of the block (what the
+                    // others' rows come to is not stored)
+                    const int own = warp & 3, lane = r & 31, groups = (left + 31) / 32;
+                    const uint32_t t_s = tmem + lane_addr + (w.n_sub == 2 ? u : (lone_steps + n_full) & 1) * 128;
+                    tc_wait(bar(&bars.s_full[u][n_steps & 3u]), (n_steps >> 2) & 1u, dead, ix.status);
+                    tc_fence_after();
+                    if (left % 16 != 0) {      // the value rows behind the block's end that the MMA of the last 16 keys reads
+                        const uint32_t i = (uint32_t)((kt0 + n_full) * kTilePieces + 3);
+                        tc_wait(bar(&bars.full[i % kPieces]), (i / kPieces) & 1u, dead, ix.status);
+                        if (!dead)
+                            for (int e = r; e < (16 - left % 16) * 16; e += 128)
+                                *reinterpret_cast<uint4*>(smem + (s_ring - base) + (i % kPieces) * kPieceBytes + (e & 8) * (kPieceBytes / 16) +
+                                                          (left + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                    }
+                    if (own < groups) {
+                        float mx = -INFINITY;
+#pragma unroll 1
+                        for (int c = 0; c <= own; ++c) {
+                            float v[32];
+                            tc_ld32(t_s + c * 32, v);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, c == own && i > lane ? -INFINITY : v[i]);
+                        }
+                        mx *= scale_log2;
+                        float alpha = 1.f;
+                        if (mx > m_used + 8.f) {
+                            alpha = m_used == -INFINITY ? 0.f : exp2f(m_used - mx);
+                            m_used = mx;
+                        }
+                        if (n_full > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+                            tc_wait(bar(&bars.pv_done[u]), (n_steps - 1) & 1u, dead, ix.status);
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < kV / 8; ++c) {
+                                float v[8];
+                                tc_ld8(t_o + c * 8, v);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[e] *= alpha;
+                                tc_st8(t_o + c * 8, v);
+                            }
+                        }
+                        l_run *= alpha;
+                        const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
+#pragma unroll 1
+                        for (int c = 0; c < groups; ++c) {
+                            uint32_t pk[16];
+                            if (c <= own) {
+                                float v[32];
+                                tc_ld32(t_s + c * 32, v);
+#pragma unroll
+                                for (int i = 0; i < 32; i += 2) {
+                                    float x0 = c == own && i > lane ? -INFINITY : v[i], x1 = c == own && i + 1 > lane ? -INFINITY : v[i + 1];
+                                    fma_x2(x0, x1, scale_log2, neg_m);
+                                    pk[i >> 1] = pack_bf16(exp2f(x0), exp2f(x1));
+                                    add_bf16x2(l_run, pk[i >> 1]);
+                                }
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) pk[i] = 0;
+                            }
+                            tc_st16(t_s + c * 16, pk);
+                        }
+                        tc_wait_st();
+                    }
+                    tc_fence_before();
+                    mbar_arrive(bar(&bars.p_half[u][n_steps & 3u]));
+                    mbar_arrive(bar(&bars.p_full[u][n_steps & 3u]));
+                    ++n_steps;
+                }
                 // ---- epilogue: O / l; thread r owns row r.  O_u is overwritten by the next unit's first PV, which waits for
                 // this warpgroup's next weights.
                 tc_wait(bar(&bars.pv_done[u]), (n_steps - 1) & 1u, dead, ix.status);
                 tc_fence_after();
                 const float inv = 1.f / l_run;
-                const bool row_ok = !dead && r < w.L - (w.q0 + u * kTileM);     // rows behind the block's end are not stored
-                __nv_bfloat16* dst = o + ((int64_t)(w.tok0 + w.q0 + u * kTileM + r) * H + w.h) * kV;
+                const bool row_ok = !dead && r < w.L - (w.q0 + sub * kTileM);     // rows behind the block's end are not stored
+                __nv_bfloat16* dst = o + ((int64_t)(w.tok0 + w.q0 + sub * kTileM + r) * H + w.h) * kV;
 #pragma unroll
                 for (int c = 0; c < kV / 32; ++c) {
                     float v[32];
@@ -429,6 +534,10 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     }
                 }
                 tc_fence_before();
+            }
+            if (w.n_sub == 1) {
+                ++lone;
+                lone_steps += w.n_total;
             }
             kt0 += w.n_total;
         }

@@ -701,6 +701,15 @@ def test_prefill_lengths_and_heads(B, lens, H):
     _prefill(B, lens, H, np.random.default_rng(sum(lens) + H))
 
 
+@pytest.mark.parametrize("lens,H,num_sms", [([18] * 60, 5, 4), ([1, 15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 64, 65, 66], 3, 2),
+                                            ([129, 144, 145, 160, 161, 191, 192, 193, 257, 300, 320, 321], 2, 3),
+                                            ([20, 300, 64, 1, 513, 130, 7, 40, 256, 2, 383], 4, 5), ([5, 200, 3, 450] * 8, 2, 1)])
+def test_prefill_short_and_long_units_in_turn(B, lens, H, num_sms):
+    # many units to a CTA: short blocks, short ends of long ones and whole tiles follow one another through the same buffers
+    for spread in (1.0, 20.0):
+        _prefill(B, lens, H, np.random.default_rng(len(lens) + H), spread, 64, num_sms)
+
+
 @pytest.mark.parametrize("spread,stride,num_sms", [(30.0, 64, 0), (1e-3, 72, 0), (1.0, 576, 3), (4.0, 192, 1)])
 def test_prefill_scores_strides_and_sms(B, spread, stride, num_sms):
     _prefill(B, [300, 17, 600], 3, np.random.default_rng(stride), spread, stride, num_sms)
