@@ -56,7 +56,8 @@ class Rope:
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("rows,heads,kv,hd,R,offset", [
     (1, 1, 0, 64, 64, 0), (3, 32, 8, 128, 128, 0), (1200, 4, 1, 128, 32, 96), (700, 3, 3, 192, 64, 128), (7, 5, 2, 80, 20, 60),
-    (5, 2, 1, 72, 8, 16), (4, 1, 1, 256, 256, 0), (9, 7, 1, 65, 2, 31), (2000, 1, 0, 48, 48, 0), (33, 128, 0, 192, 64, 128)])
+    (5, 2, 1, 72, 8, 16), (4, 1, 1, 256, 256, 0), (9, 7, 1, 65, 2, 31), (2000, 1, 0, 48, 48, 0), (33, 128, 0, 192, 64, 128),
+    (9501, 1, 1, 32, 32, 0), (20011, 1, 0, 24, 16, 8), (18945, 1, 0, 10, 6, 1)])
 def test_rope_rows(B, rows, heads, kv, hd, R, offset, interleaved):
     rng = np.random.default_rng(rows + heads)
     rope = Rope(B, R, interleaved, "none" if rows % 2 else "parts", amplitude=1.0 if heads % 2 else 1.375)
