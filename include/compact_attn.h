@@ -80,6 +80,7 @@ typedef enum cpa_status {
     CPA_ESTATE = -6        /* call order violated (e.g. compute before cpa_plan_upload) */
 } cpa_status;
 
+enum { CPA_Q_TILE_LATENT = 1 };   /* a value of q_tile_rows */
 typedef struct cpa_config {
     int32_t num_q_heads;
     int32_t num_kv_heads;    /* must divide num_q_heads; group size G <= 8 */
@@ -88,7 +89,8 @@ typedef struct cpa_config {
     float   scale;           /* softmax scale, normally 1/sqrt(head_dim) */
     int32_t q_tile_rows;     /* query rows per prefill work item: 128, 256, or 512 (items of 512 rows run on pairs of
                                 CTAs, cta_group::2: head_dim 128, plans without cached prefixes or chunks only;
-                                measured no faster than 256, kept as an option); 0 = default (256) */
+                                measured no faster than 256, kept as an option); 0 = default (256);
+                                CPA_Q_TILE_LATENT = 128 or 256, from the lengths (for cpa_latent_prefill) */
     int32_t pages_per_split; /* KV pages per decode work item (<= 1024); 0 = chosen per block from the batch */
     int32_t num_sms;         /* SMs this plan's kernels may fill: the persistent prefill launches min(num_sms, units)
                                 CTAs (one per SM) and the decode wave is sized for 3 * num_sms CTAs; 0 = the SM
@@ -776,8 +778,9 @@ typedef struct cpa_latent_config {
 /* The cpa_config that the calls on the tables of a latent cache take.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
 CPA_API int cpa_latent_tables_config(const cpa_latent_config* cfg, cpa_config* out);
 
-/* The cpa_config that the plan of a cpa_latent_prefill is created with.  Its q_tile_rows may be set to 128 where the units of 128
- * query rows (num_heads for every 128 tokens of a block) have an SM each.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
+/* The cpa_config that the plan of a cpa_latent_prefill is created with.  Its q_tile_rows is CPA_Q_TILE_LATENT: items of 128 rows where
+ * those of 256 would leave SMs waiting for the longest ones, else 256; it may be set to either.  Errors: CPA_EINVAL,
+ * CPA_EUNSUPPORTED. */
 CPA_API int cpa_latent_plan_config(const cpa_latent_config* cfg, cpa_config* out);
 
 /*

@@ -51,6 +51,7 @@ class cpa_table_dims(ctypes.Structure):
                 ("token_capacity", ctypes.c_int32)]
 
 
+Q_TILE_LATENT = 1                                   # a value of cpa_config.q_tile_rows
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_UNSCALED, ROPE_SCALED_ALL, ROPE_SCALED_BASE, ROPE_SCALED_PARTS, ROPE_SCALED_WAVES = 0, 1, 2, 3, 4
 

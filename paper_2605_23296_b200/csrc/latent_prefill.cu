@@ -575,6 +575,7 @@ extern "C" int cpa_latent_plan_config(const cpa_latent_config* cfg, cpa_config* 
     out->page_size = cfg->page_size;
     out->scale = cfg->scale;
     out->num_sms = cfg->num_sms;
+    out->q_tile_rows = CPA_Q_TILE_LATENT;
     return CPA_OK;
 }
 

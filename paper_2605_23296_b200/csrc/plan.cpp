@@ -71,6 +71,27 @@ std::vector<int32_t> deal_prefill_units(const std::vector<int32_t>& item_cost, i
 }  // namespace
 
 namespace {
+// Query rows per item of a latent prefill: 128 where that is expected to end a tenth sooner than 256, the longest item and the mean over
+// the SMs taken for the end.  An item of two 128-row sub-tiles takes 6.7 us and 1.76 per K/V tile, of one 3.2 and 1.03 (fitted to
+// 100 blocks of 60..128 tokens up to 12 of 2048, 3 or 16 heads).  5 blocks of 755..1087 with 3 heads: 16 us by 128, 24 by 256; where
+// the two are expected within a tenth of one another they were, -3 to +8 % (9 blocks of 1..700 with 16 heads: 26.7 and 24.8).
+int32_t latent_q_tile(const std::vector<int32_t>& lens, int32_t heads, int32_t ctas) {
+    double end[2];
+    for (int k = 0; k < 2; ++k) {
+        const int32_t rows = 256 >> k;
+        double sum = 0, longest = 0;
+        for (const int32_t n : lens)
+            for (int64_t q0 = 0; q0 < n; q0 += rows) {
+                const bool two = k == 0 && n - q0 > 128;
+                const double t = two ? 6.7 + 1.76 * (double)(q0 / 128 + 2) : 3.2 + 1.03 * (double)(q0 / 128 + 1);
+                sum += t * heads;
+                longest = std::max(longest, t);
+            }
+        end[k] = std::max(longest, sum / ctas);
+    }
+    return end[1] < 0.9 * end[0] ? 128 : 256;
+}
+
 // Both layouts: `prefix_lens` == nullptr is the independent-chunks layout (no cached prefix).
 int plan_create(const cpa_config* cfg, int32_t num_blocks, const int32_t* block_lens, const int32_t* prefix_lens,
                 const int32_t* shared_pages, int32_t num_shared, int32_t max_new_tokens, const int32_t* free_pages,
@@ -86,7 +107,8 @@ int plan_create(const cpa_config* cfg, int32_t num_blocks, const int32_t* block_
     if ((cfg->head_dim != 64 && cfg->head_dim != 128) || cfg->page_size != 16 ||
         cfg->num_q_heads / cfg->num_kv_heads > 8)
         return CPA_EUNSUPPORTED;
-    if (cfg->q_tile_rows != 0 && cfg->q_tile_rows != 128 && cfg->q_tile_rows != 256 && cfg->q_tile_rows != 512)
+    if (cfg->q_tile_rows != 0 && cfg->q_tile_rows != CPA_Q_TILE_LATENT && cfg->q_tile_rows != 128 && cfg->q_tile_rows != 256 &&
+        cfg->q_tile_rows != 512)
         return CPA_EUNSUPPORTED;
     // 512-row items run on pairs of CTAs: head_dim 128, whole blocks without cached prefix or chunks
     const bool pairs_possible = cfg->head_dim == 128 && !prefix_lens && chunk_tokens == 0 &&
@@ -106,7 +128,7 @@ int plan_create(const cpa_config* cfg, int32_t num_blocks, const int32_t* block_
     p->num_sms = cfg->num_sms ? cfg->num_sms : std::min(device_sm_count(), kMaxPlanSms);
     p->B = num_blocks;
     p->T = max_new_tokens;
-    p->q_tile = cfg->q_tile_rows ? cfg->q_tile_rows : 256;
+    p->q_tile = cfg->q_tile_rows == CPA_Q_TILE_LATENT ? 256 : cfg->q_tile_rows ? cfg->q_tile_rows : 256;
     const int32_t P = cfg->page_size;
     const int32_t B = num_blocks;
     // a pool's rows (page * Hkv + head) * P + slot are 32-bit tensor-map coordinates, and a slot is page * P + offset
@@ -141,6 +163,7 @@ int plan_create(const cpa_config* cfg, int32_t num_blocks, const int32_t* block_
         own_total += own;
     }
     p->total_tokens = p->cu_seqlens[B];
+    if (cfg->q_tile_rows == CPA_Q_TILE_LATENT && !prefix_lens && chunk_tokens == 0) p->q_tile = latent_q_tile(p->block_lens, cfg->num_q_heads, p->num_sms);
     const int32_t pages_used = p->page_indptr[B];
     // Pages on demand: a block starts with the pages for its tokens plus the next one (never more than its row of
     // the table holds); the rest of the free list is the common reserve.

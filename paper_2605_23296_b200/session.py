@@ -412,12 +412,8 @@ class LatentSession:
         self.cfg = B.cpa_latent_config(num_heads, latent_dim, 64, 128, 128, 16, self.scale, norm_eps, num_sms)
         tables_cfg = B.cpa_latent_tables_config(self.cfg)
         plan_cfg = B.cpa_latent_plan_config(self.cfg)
-        # where units of 128 query rows have an SM each, they are done sooner than half as many of 256 (one block of 1024 tokens
-        # and 16 heads: 15 us for 21); with more of them every K/V tile would be read twice as often (32 blocks: 231 us for 198)
-        sms = num_sms or torch.cuda.get_device_properties(self.device).multi_processor_count
-        if num_heads * sum(-(-int(n) // 128) for n in self.block_lens) <= sms:
-            plan_cfg.q_tile_rows = 128
-        self.plan = B.cpa_plan_create(plan_cfg, self.block_lens, max_new_tokens, free_pages)
+        with torch.cuda.device(self.device):             # (whose SMs the plan counts)
+            self.plan = B.cpa_plan_create(plan_cfg, self.block_lens, max_new_tokens, free_pages)
         self.dims = B.cpa_table_dims(self.B, max_new_tokens, num_pages, B.cpa_plan_param(self.plan, B.PARAM_PAGES_USED), 0)
         on = dict(device=self.device)
         self.index_buf = torch.empty(B.cpa_plan_param(self.plan, B.PARAM_INDEX_BYTES), dtype=torch.uint8, **on)

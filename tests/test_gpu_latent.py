@@ -678,10 +678,12 @@ def test_few_blocks_with_tokens_among_many_without(B, H):
 
 # ------------------------------------------------------------------------------------------------ expanded attention
 
-def _prefill(B, lens, H, rng, spread=1.0, stride=576, num_sms=0, scale=192 ** -0.5):
+def _prefill(B, lens, H, rng, spread=1.0, stride=576, num_sms=0, scale=192 ** -0.5, rows=None):
     T = sum(lens)
     cfg = B.cpa_latent_config(H, 512, 64, 128, 128, 16, scale, 1e-6, num_sms)
-    plan = B.cpa_plan_create(B.cpa_latent_plan_config(cfg), lens, 0, list(range(sum(-(-n // 16) for n in lens))))
+    pc = B.cpa_latent_plan_config(cfg)
+    pc.q_tile_rows = rows or pc.q_tile_rows
+    plan = B.cpa_plan_create(pc, lens, 0, list(range(sum(-(-n // 16) for n in lens))))
     index = torch.empty(B.cpa_plan_param(plan, B.PARAM_INDEX_BYTES), dtype=torch.uint8, device="cuda")
     assert B.cpa_plan_upload(plan, index, index.numel(), _stream()) == 0
     (q, qf), (kv, kvf) = _bf16(spread * rng.standard_normal((T, H, 192))), _bf16(rng.standard_normal((T, H, 256)))
@@ -699,7 +701,8 @@ def _prefill(B, lens, H, rng, spread=1.0, stride=576, num_sms=0, scale=192 ** -0
 @pytest.mark.parametrize("lens,H", [([1], 1), ([1, 2, 3], 4), ([127, 128, 129], 2), ([255, 256, 257, 1], 3), ([700], 1), ([64, 63, 65, 385], 16),
                                     ([1500, 40], 2), ([30] * 40, 5), ([513, 640, 300], 20)])
 def test_prefill_lengths_and_heads(B, lens, H):
-    _prefill(B, lens, H, np.random.default_rng(sum(lens) + H))
+    for rows in (256, 128):
+        _prefill(B, lens, H, np.random.default_rng(sum(lens) + H), rows=rows)
 
 
 @pytest.mark.parametrize("lens,H,num_sms", [([18] * 60, 5, 4), ([1, 15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 64, 65, 66], 3, 2),
@@ -707,8 +710,8 @@ def test_prefill_lengths_and_heads(B, lens, H):
                                             ([20, 300, 64, 1, 513, 130, 7, 40, 256, 2, 383], 4, 5), ([5, 200, 3, 450] * 8, 2, 1)])
 def test_prefill_short_and_long_units_in_turn(B, lens, H, num_sms):
     # many units to a CTA: short blocks, short ends of long ones and whole tiles follow one another through the same buffers
-    for spread in (1.0, 20.0):
-        _prefill(B, lens, H, np.random.default_rng(len(lens) + H), spread, 64, num_sms)
+    for spread, rows in ((1.0, 256), (20.0, 256), (1.0, 128)):
+        _prefill(B, lens, H, np.random.default_rng(len(lens) + H), spread, 64, num_sms, rows=rows)
 
 
 @pytest.mark.parametrize("spread,stride,num_sms", [(30.0, 64, 0), (1e-3, 72, 0), (1.0, 576, 3), (4.0, 192, 1)])

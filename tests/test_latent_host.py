@@ -171,3 +171,18 @@ def test_oracle_turns_pairs_and_back():
         w = z * 1.25 * np.exp(1j * pos[..., None] * f)
         got = y[..., 0::2] + 1j * y[..., 1::2] if inter else y[..., :32] + 1j * y[..., 32:]
         assert np.allclose(got, w)
+
+
+@pytest.mark.parametrize("lens,H,want", [([1000], 16, 128), ([800, 900, 1000, 1050, 760], 3, 128), ([1024] * 32, 16, 256), ([8192, 4000, 1024], 64, 256),
+                                         ([5], 1, 256), ([300] * 8, 16, 256), ([300, 500], 4, 128)])
+def test_plans_of_a_latent_prefill_choose_their_items(lens, H, want):
+    # few items: as many as there are SMs; long blocks: two sub-tiles that share K and V
+    cfg = B.cpa_latent_config(H, 512, 64, 128, 128, 16, 0.07, 1e-6, 148)
+    pc = B.cpa_latent_plan_config(cfg)
+    assert pc.q_tile_rows == B.Q_TILE_LATENT
+    pages = list(range(sum(-(-n // 16) for n in lens)))
+    for rows, given in ((want, B.Q_TILE_LATENT), (128, 128), (256, 256)):
+        pc.q_tile_rows = given
+        plan = B.cpa_plan_create(pc, lens, 0, pages)
+        assert B.cpa_plan_param(plan, B.PARAM_Q_TILE_ROWS) == rows
+        B.cpa_plan_destroy(plan)
