@@ -323,6 +323,80 @@ def test_append_many_blocks_and_rows_behind_the_last(B):
     assert torch.equal(c.pool.view(-1, 192)[torch.as_tensor(slots, dtype=torch.long, device="cuda")], packed[:n])
 
 
+@pytest.mark.parametrize("cu,rows", [([0, 10, 5, 12, 5, 5], 6000), ([0, 10, 5, 12, 5, 5], 40), ([0, 4000, 3999, 4737, 4700, 5001], 5001),
+                                     ([0, 5000, 17, 18, 16, 4999], 5000), ([0, 4738, 4738, 4738, 4737, 4738], 4738),
+                                     ([7, 3, 5000, 11, 11, 13], 5000), ([0, 0, 4800, 2400, 2401, 4800], 4800)])
+def test_append_stores_every_good_range_beside_bad_ones(B, cu, rows):
+    # ranges that run backwards, so that good ones overlap: each good block has all of its rows, whatever the search of a row leads to, with
+    # one row of a warp in flight (40 rows) and with two
+    rng = np.random.default_rng(rows)
+    n = len(cu) - 1
+    c = Cache(B, [5008] * n, 128, rope=Rope(B))
+    x = torch.randn(rows, 192, device="cuda").bfloat16()
+    first, out = _i32(rng.integers(0, 10 ** 5, n)), torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    assert B.cpa_latent_append(c.cfg, c.dims, c.tables, c.rope.cfg, c.rope.turns, x, 192, None, _i32(cu), rows, first, c.lens, out, c.pool, None,
+                               _stream()) == 0
+    assert c.status() == B.CPA_EINVAL
+    lens = [max(0, cu[b + 1] - cu[b]) for b in range(n)]
+    assert out.tolist() == lens
+    for b in range(n):
+        if not lens[b]:
+            continue
+        d = Cache(B, [5008], 128, rope=c.rope)
+        part, one = x[cu[b]:cu[b + 1]].contiguous(), torch.empty(1, dtype=torch.int32, device="cuda")
+        for lo in range(0, lens[b], 1000):                                   # by calls of few rows
+            hi = min(lo + 1000, lens[b])
+            assert B.cpa_latent_append(d.cfg, d.dims, d.tables, c.rope.cfg, c.rope.turns, part[lo:hi], 192, None, _i32([0, hi - lo]), hi - lo,
+                                       first[b:b + 1].clone(), _i32([lo]), one, d.pool, None, _stream()) == 0
+        got, want = (k.pool.view(-1, 192)[torch.as_tensor(k.slots(i, 0, lens[b]), dtype=torch.long, device="cuda")] for k, i in ((c, b), (d, 0)))
+        assert torch.equal(got, want), (b, torch.nonzero((got != want).any(1)).flatten().tolist()[:4])
+
+
+@pytest.mark.parametrize("rows", [4735, 4736, 4737, 4738, 6001])
+@pytest.mark.parametrize("L,how", [(512, "apart"), (256, "odd stride"), (384, "in place"), (128, "as it is")])
+def test_append_of_many_rows_is_that_of_few(B, rows, L, how):
+    # one row of a warp in flight up to 4736 rows, two from there on: odd blocks (pairs lie across their borders), empty ones between
+    # them, one without room and one whose length is bad; the same bits as by a call for every block
+    rng = np.random.default_rng(rows + L)
+    counts = [1, 0, 33, 0, 0, 1, 700, 17, 2, 0, 1501, 3, 1]
+    counts.append(rows - 20 - sum(counts) - 96)
+    counts += [95, 1, 0]
+    cu = np.concatenate([[0], np.cumsum(counts)])                            # the last 20 rows are no block's
+    n, full, bad = len(counts), 6, 10
+    room = [k + 5 for k in counts]
+    room[full] = 600
+    rope = None if how == "as it is" else Rope(B, 64, L == 256, "parts")
+    weight = None if how == "as it is" else torch.randn(L, device="cuda").bfloat16()
+    before = rng.integers(0, 6, n)
+    before[bad] = -1
+    before = np.where(np.asarray(counts) > 0, before, 0)
+    c, stride = Cache(B, room, L, rope=rope), L + 64 + (7 if how == "odd stride" else 0)
+    x = torch.randn(rows, stride, device="cuda").bfloat16()
+    was, first, out = x.clone(), _i32(rng.integers(0, 10 ** 5, n)), torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    packed = x if how == "in place" else torch.full((rows, L + 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    assert B.cpa_latent_append(c.cfg, c.dims, c.tables, rope and rope.cfg, rope and rope.turns, x, stride, weight, _i32(cu), rows, first, _i32(before),
+                               out, c.pool, packed, _stream()) == 0
+    assert c.status() in (B.CPA_ENOSPC, B.CPA_EINVAL)
+    left_out = lambda b: b in (full, bad)
+    assert out.tolist() == [int(before[b]) if left_out(b) else int(before[b]) + counts[b] for b in range(n)]
+    stays = torch.ones(rows, dtype=torch.bool, device="cuda")
+    d = Cache(B, room, L, rope=rope)
+    for b in range(n):
+        if counts[b] == 0 or left_out(b):
+            continue
+        lens, one = np.zeros(n, dtype=np.int64), torch.empty(n, dtype=torch.int32, device="cuda")
+        lens[b] = before[b]
+        own = torch.empty(counts[b], L + 64, dtype=torch.bfloat16, device="cuda")
+        mine = np.concatenate([np.zeros(b + 1), np.full(n - b, counts[b])])
+        part = was[cu[b]:cu[b + 1]].clone()
+        assert counts[b] <= 4736 and B.cpa_latent_append(d.cfg, d.dims, d.tables, rope and rope.cfg, rope and rope.turns, part, stride, weight,
+                                                         _i32(mine), counts[b], first, _i32(lens), one, d.pool, own, _stream()) == 0
+        assert torch.equal(packed[cu[b]:cu[b + 1]], own), b
+        stays[cu[b]:cu[b + 1]] = False
+    assert torch.equal(c.pool.view(torch.int16), d.pool.view(torch.int16)) and d.status() == 0
+    assert torch.equal(packed[stays], was[stays] if how == "in place" else torch.full_like(packed[stays], 3.0))
+
+
 # ------------------------------------------------------------------------------------------------ absorbed attention
 
 EDGES = [0, 1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 200, 255, 256, 257, 1000]
