@@ -409,6 +409,10 @@ class LatentSession:
             raise ValueError(f"norm_weight: contiguous bf16 [{latent_dim}] is wanted")
         if rope is not None and rope.cfg.rope_dim != 64:
             raise ValueError(f"rope: 64 rotated elements are wanted, not {rope.cfg.rope_dim}")
+        start = np.zeros(self.B, dtype=np.int64) if first is None else np.asarray(first, dtype=np.int64)
+        # (the kernels read one position per block, and add to it in 32 bits)
+        if start.shape != (self.B,) or (start < -2 ** 31).any() or (start + self.block_lens + max_new_tokens > 2 ** 31 - 1).any():
+            raise ValueError(f"first: {self.B} positions are wanted, one per block, which stay within 32 bits for all of its tokens")
         self.cfg = B.cpa_latent_config(num_heads, latent_dim, 64, 128, 128, 16, self.scale, norm_eps, num_sms)
         tables_cfg = B.cpa_latent_tables_config(self.cfg)
         plan_cfg = B.cpa_latent_plan_config(self.cfg)
@@ -429,7 +433,6 @@ class LatentSession:
                 B.cpa_plan_destroy(self.plan)
                 self.plan = None
                 raise ValueError(f"{name}: on {self.lens.device}, not on {t.device}")
-        start = np.zeros(self.B, dtype=np.int64) if first is None else np.asarray(first, dtype=np.int64)
         self.first = None if first is None else torch.as_tensor(start.astype(np.int32), **on)
         self.cu = torch.as_tensor(np.concatenate([[0], np.cumsum(self.block_lens)]).astype(np.int32), **on)
         self.positions = torch.as_tensor(np.concatenate([s + np.arange(n) for s, n in zip(start, self.block_lens)]).astype(np.int32), **on)

@@ -186,3 +186,11 @@ def test_plans_of_a_latent_prefill_choose_their_items(lens, H, want):
         plan = B.cpa_plan_create(pc, lens, 0, pages)
         assert B.cpa_plan_param(plan, B.PARAM_Q_TILE_ROWS) == rows
         B.cpa_plan_destroy(plan)
+
+
+@pytest.mark.parametrize("first", [[], [5], [1, 2, 3], 7, [[1, 2]], [0, 2 ** 31 - 34], [-2 ** 31 - 1, 0], [2 ** 33, 0]])
+def test_sessions_refuse_first_positions_that_are_not_one_per_block(first):
+    # before anything touches a device: the kernels would read positions behind the array's end
+    session = pytest.importorskip("paper_2605_23296_b200.session")
+    with pytest.raises(ValueError, match="first"):
+        session.LatentSession([10, 30], 4, 8, list(range(8)), 8, latent_dim=128, first=first)
