@@ -779,8 +779,9 @@ typedef struct cpa_latent_config {
 CPA_API int cpa_latent_tables_config(const cpa_latent_config* cfg, cpa_config* out);
 
 /* The cpa_config that the plan of a cpa_latent_prefill is created with.  Its q_tile_rows is CPA_Q_TILE_LATENT: items of 128 rows where
- * those of 256 would leave SMs waiting for the longest ones, else 256; it may be set to either.  Errors: CPA_EINVAL,
- * CPA_EUNSUPPORTED. */
+ * those of 256 would leave SMs waiting for the longest ones, else 256; it may be set to either.  cpa_latent_prefill reads no pages: the
+ * plan may be given page 0 throughout (it bounds ids by the rows of a cache of num_heads heads; the latent cache's pages go to
+ * cpa_tables_build, which takes any of up to 2^26 - 1).  Errors: CPA_EINVAL, CPA_EUNSUPPORTED. */
 CPA_API int cpa_latent_plan_config(const cpa_latent_config* cfg, cpa_config* out);
 
 /*

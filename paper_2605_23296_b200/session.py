@@ -416,9 +416,16 @@ class LatentSession:
         self.cfg = B.cpa_latent_config(num_heads, latent_dim, 64, 128, 128, 16, self.scale, norm_eps, num_sms)
         tables_cfg = B.cpa_latent_tables_config(self.cfg)
         plan_cfg = B.cpa_latent_plan_config(self.cfg)
+        # The plan is there for the prefill's schedule, which reads no pages: it gets as many as there are, but not their ids, which
+        # it would hold against the rows of a grouped cache (num_heads times as many as a page of this one has).
+        free = np.ascontiguousarray(free_pages, dtype=np.int32)
         with torch.cuda.device(self.device):             # (whose SMs the plan counts)
-            self.plan = B.cpa_plan_create(plan_cfg, self.block_lens, max_new_tokens, free_pages)
-        self.dims = B.cpa_table_dims(self.B, max_new_tokens, num_pages, B.cpa_plan_param(self.plan, B.PARAM_PAGES_USED), 0)
+            self.plan = B.cpa_plan_create(plan_cfg, self.block_lens, max_new_tokens, np.zeros_like(free))
+        used = B.cpa_plan_param(self.plan, B.PARAM_PAGES_USED)
+        if (free[:used] < 0).any():
+            self.close()
+            raise B.CpaError(B.CPA_EINVAL, "free_pages")
+        self.dims = B.cpa_table_dims(self.B, max_new_tokens, num_pages, used, 0)
         on = dict(device=self.device)
         self.index_buf = torch.empty(B.cpa_plan_param(self.plan, B.PARAM_INDEX_BYTES), dtype=torch.uint8, **on)
         self.tables = torch.empty(B.cpa_tables_bytes(tables_cfg, self.dims), dtype=torch.uint8, **on)
@@ -436,9 +443,9 @@ class LatentSession:
         self.first = None if first is None else torch.as_tensor(start.astype(np.int32), **on)
         self.cu = torch.as_tensor(np.concatenate([[0], np.cumsum(self.block_lens)]).astype(np.int32), **on)
         self.positions = torch.as_tensor(np.concatenate([s + np.arange(n) for s, n in zip(start, self.block_lens)]).astype(np.int32), **on)
-        lens, free = torch.as_tensor(self.block_lens, **on), torch.as_tensor(np.ascontiguousarray(free_pages, dtype=np.int32), **on)
+        lens, d_free = torch.as_tensor(self.block_lens, **on), torch.as_tensor(free, **on)
         self._call("cpa_plan_upload", self.plan, self.index_buf, self.index_buf.numel())
-        self._call("cpa_tables_build", tables_cfg, self.dims, lens, free, len(free_pages), self.tables)
+        self._call("cpa_tables_build", tables_cfg, self.dims, lens, d_free, len(free), self.tables)
 
     def _call(self, what: str, *args) -> None:
         with torch.cuda.device(self.device):

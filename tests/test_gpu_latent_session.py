@@ -200,3 +200,27 @@ def test_weights_and_frequencies_elsewhere_are_refused():
                 dict(rope=Rotary(32))):
         with pytest.raises(ValueError):
             LatentSession([10], 0, 8, [0], 1, latent_dim=128, **bad)
+
+
+@pytest.mark.parametrize("H,L,far", [(128, 128, 524290), (64, 128, 1048580)])
+def test_far_pages_of_a_large_pool(H, L, far):
+    # page ids that a cache of H key heads could not have: the same event as in the first pages
+    from paper_2605_23296_b200 import binding as B
+    from paper_2605_23296_b200.session import LatentSession
+    if torch.cuda.mem_get_info()[0] < 4 * far * 16 * (L + 64):
+        pytest.skip("too little memory")
+    lens, T, made = [100, 37], 2, []
+    for at in (0, far):
+        rng = np.random.default_rng(H)
+        ids = at + rng.permutation(12)
+        s = LatentSession(lens, T, H, ids, at + 12, L)
+        packed = s.append_prefill(_bf16(rng, 137, L + 64))
+        outs = [packed, s.prefill(_bf16(rng, 137, H, 192), _bf16(rng, 137, H, 256), packed)]
+        outs += [s.step(_bf16(rng, 2, H, L), _bf16(rng, 2, H, 64), _bf16(rng, 2, L + 64)) for _ in range(T)]
+        assert s.status() == 0 and s.lens.tolist() == [102, 39]
+        made.append(outs)
+        s.close()
+        del s
+    assert all(torch.equal(a, b) for a, b in zip(*made))
+    with pytest.raises(B.CpaError):
+        LatentSession(lens, T, H, [-1] * 12, 12, L)

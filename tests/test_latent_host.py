@@ -194,3 +194,18 @@ def test_sessions_refuse_first_positions_that_are_not_one_per_block(first):
     session = pytest.importorskip("paper_2605_23296_b200.session")
     with pytest.raises(ValueError, match="first"):
         session.LatentSession([10, 30], 4, 8, list(range(8)), 8, latent_dim=128, first=first)
+
+
+def test_plans_of_a_latent_prefill_need_no_page_ids():
+    # what the header promises: page 0 throughout, whatever the cache's own ids are, and the same schedule
+    pc = B.cpa_latent_plan_config(_cfg(H=128, sms=148))
+    lens = [300, 1, 700]
+    pages = sum(-(-n // 16) for n in lens)
+    with pytest.raises(B.CpaError):
+        B.cpa_plan_create(pc, lens, 0, [1 << 25] * pages)
+    plan = B.cpa_plan_create(pc, lens, 0, [0] * pages)
+    assert B.cpa_plan_param(plan, B.PARAM_PAGES_USED) == pages
+    B.cpa_plan_destroy(plan)
+    tc = B.cpa_latent_tables_config(_cfg(H=128))
+    assert B.cpa_tables_bytes(tc, B.cpa_table_dims(4, 0, (1 << 26) - 1, 8, 0)) > 0
+    assert B.cpa_tables_bytes(tc, B.cpa_table_dims(4, 0, 1 << 26, 8, 0)) == B.CPA_EUNSUPPORTED
