@@ -26,9 +26,11 @@ struct append_args {
 
 __device__ __forceinline__ int cu_at(const int32_t* cu, int b) { return cu ? ld_i32(cu + b) : b; }
 
-// The last block that starts at or before a packed row, by a whole warp with 32 candidates per load, of `size` blocks from lo on.
-// What it leads to grows with the row, whatever cu holds.
-__device__ __forceinline__ int find_block(int row, const int32_t* cu, int lo, int size, int lane) {
+// The last block that starts at or before a packed row, by a whole warp with 32 candidates per load.  What it leads to
+// grows with the row, whatever cu holds.
+__device__ __forceinline__ int find_block(int row, const int32_t* cu, int B, int lane) {
+    if (!cu) return row;
+    int lo = 0, size = B;
     while (size > 1) {
         const int step = (size + 31) / 32, i = lane * step;
         const uint32_t below = __ballot_sync(0xffffffffu, i < size && ld_i32(cu + lo + i) <= row);
@@ -37,27 +39,6 @@ __device__ __forceinline__ int find_block(int row, const int32_t* cu, int lo, in
         size = min(step, size - skip);
     }
     return lo;
-}
-__device__ __forceinline__ int find_block(int row, const int32_t* cu, int B, int lane) {
-    return cu ? find_block(row, cu, 0, B, lane) : row;
-}
-// The same for a row and the next one, with one load as long as both go the same way.  (That the next one lies in the first one's
-// range is not enough: where ranges run backwards its search may lead elsewhere, and there it is looked for.)
-__device__ __forceinline__ int2 find_two(int row, const int32_t* cu, int B, int lane) {
-    if (!cu) return make_int2(row, row + 1);
-    int lo = 0, size = B;
-    while (size > 1) {
-        const int step = (size + 31) / 32, i = lane * step;
-        const int start = i < size ? ld_i32(cu + lo + i) : INT32_MAX;
-        const int skip = max(__popc(__ballot_sync(0xffffffffu, i < size && start <= row)) - 1, 0) * step;
-        const int next = max(__popc(__ballot_sync(0xffffffffu, i < size && start <= row + 1)) - 1, 0) * step;
-        if (skip != next)
-            return make_int2(find_block(row, cu, lo + skip, min(step, size - skip), lane),
-                             find_block(row + 1, cu, lo + next, min(step, size - next), lane));
-        lo += skip;
-        size = min(step, size - skip);
-    }
-    return make_int2(lo, lo);
 }
 
 // A block's rows: n from packed row c0 on, to position `at`; and 0, or the status of why it is left out.
@@ -80,6 +61,17 @@ __device__ __forceinline__ void put_row(row_pieces<L>& r, int row, int block, co
     if (a.packed) store_row<L>(r, a.packed + (int64_t)row * (L + kRopeDim), lane);
 }
 
+// The block that the row warps take a row for.  The second row of a pair goes with the first one's block where it lies in that one's
+// range, which is the block that its own search leads to as long as ranges run forwards.
+__device__ __forceinline__ int taken_for(int row, const append_args& a, int lane) {
+    if (a.at_once == 2 && (row & 1)) {
+        const int b = find_block(row - 1, a.cu, a.B, lane);
+        const block_rows o = rows_of(b, a);
+        if (row >= o.c0 && row < o.c0 + o.n) return b;
+    }
+    return find_block(row, a.cu, a.B, lane);
+}
+
 template <int L, bool WIDE>
 __global__ void __launch_bounds__(kWarps * 32) latent_append_kernel(const __grid_constant__ append_args a) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -94,29 +86,33 @@ __global__ void __launch_bounds__(kWarps * 32) latent_append_kernel(const __grid
                 if (a.lens_out) a.lens_out[b] = o.at + (o.status ? 0 : o.n);
             }
             if (o.status || o.n == 0 || !a.cu) continue;
-            // Where a range runs backwards the search may lead from a good block's rows elsewhere: those are taken here.
-            // (What the search leads to grows with the row, so a block's first and last one tell.)
-            if (find_block(o.c0, a.cu, a.B, lane) == b && find_block(o.c0 + o.n - 1, a.cu, a.B, lane) == b) continue;
+            // Where a range runs backwards a good block's rows may be taken for others: those are taken here.  (What the search leads
+            // to grows with the row, so a block's first and last one tell.)
+            if (taken_for(o.c0, a, lane) == b && find_block(o.c0 + o.n - 1, a.cu, a.B, lane) == b) continue;
             for (int row = o.c0; row < o.c0 + o.n; ++row) {
-                if (find_block(row, a.cu, a.B, lane) == b) continue;      // (taken where it is looked for; x may hold the packed row by now)
+                if (taken_for(row, a, lane) == b) continue;      // (x may hold the packed row by now)
                 load_row<L, WIDE>(r, a.x + row * a.x_row, lane);
                 put_row<L>(r, row, (int)b, o, a, lane);
             }
         }
         return;
     }
-    // (where there are many rows a warp has two in flight, which mostly are the same block's)
+    // (where there are many rows a warp has two in flight, which mostly are the same block's: taken_for says for whom.  A search for the second
+    // one as well in every pair cost 81 us for 78 on the prompts above.)
     row_pieces<L> r2;
     for (int64_t row = ((int64_t)blockIdx.x * kWarps + warp) * a.at_once; row < a.rows; row += (int64_t)a.row_ctas * kWarps * a.at_once) {
         const bool two = a.at_once == 2 && row + 1 < a.rows;
         load_row<L, WIDE>(r, a.x + row * a.x_row, lane);
         if (two) load_row<L, WIDE>(r2, a.x + (row + 1) * a.x_row, lane);
-        const int2 b = two ? find_two((int)row, a.cu, a.B, lane) : make_int2(find_block((int)row, a.cu, a.B, lane), 0);
-        block_rows o = rows_of(b.x, a);
-        if (!o.status && row >= o.c0 && row < o.c0 + o.n) put_row<L>(r, (int)row, b.x, o, a, lane);
+        int b = find_block((int)row, a.cu, a.B, lane);
+        block_rows o = rows_of(b, a);
+        if (!o.status && row >= o.c0 && row < o.c0 + o.n) put_row<L>(r, (int)row, b, o, a, lane);
         if (!two) continue;
-        if (b.y != b.x) o = rows_of(b.y, a);
-        if (!o.status && row + 1 >= o.c0 && row + 1 < o.c0 + o.n) put_row<L>(r2, (int)row + 1, b.y, o, a, lane);
+        if (row + 1 >= o.c0 + o.n || row + 1 < o.c0) {
+            b = find_block((int)row + 1, a.cu, a.B, lane);
+            o = rows_of(b, a);
+        }
+        if (!o.status && row + 1 >= o.c0 && row + 1 < o.c0 + o.n) put_row<L>(r2, (int)row + 1, b, o, a, lane);
     }
 }
 
