@@ -222,7 +222,8 @@ __device__ __forceinline__ void put_new_row(const __nv_bfloat16* x, const row_re
 
 // One lane of the warp, chosen in the form that lets the compiler keep the operands of what that lane runs on the uniform
 // datapath: an MMA of 64 x 64 x 16 then goes out every 32 cycles, which is what its operands take out of shared memory, and
-// every 46 under a test of the lane's number (58 with the instruction alone predicated on it).
+// every 46 under a test of the lane's number (58 with the instruction alone predicated on it).  For the same mask it is always the same
+// lane, so that a commit from it follows all of its warp's products.
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
     asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));

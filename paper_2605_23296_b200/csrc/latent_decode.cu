@@ -241,7 +241,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             dead = __any_sync(0xffffffffu, dead);
             if (dead) break;
         }
-        if (dead && lane == 0) {      // products queued before may still be running; tensor memory is not freed under them
+        if (dead && elect_one()) {      // products queued before may still be running; tensor memory is not freed under them
             tc_commit_one(bar(&bars.drain_s));
             mbar_drain(bar(&bars.drain_s), 0u, kDrainLimit);
         }
@@ -281,7 +281,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             dead = __any_sync(0xffffffffu, dead);
             if (dead) break;
         }
-        if (dead && lane == 0) {
+        if (dead && elect_one()) {
             tc_commit_one(bar(&bars.drain_p));
             mbar_drain(bar(&bars.drain_p), 0u, kDrainLimit);
         }

@@ -285,7 +285,7 @@ latent_decode_pair_kernel(const __grid_constant__ CUtensorMap map, const __grid_
             dead = __any_sync(0xffffffffu, dead);
             if (dead) break;
         }
-        if (dead && rank == 0 && lane == 0) {      // products queued before may still be running
+        if (dead && rank == 0 && elect_one()) {      // products queued before may still be running
             commit_leader(bar(&bars.drain_s));
             mbar_drain(bar(&bars.drain_s), 0u, kDrainLimit);
         }
@@ -323,7 +323,7 @@ latent_decode_pair_kernel(const __grid_constant__ CUtensorMap map, const __grid_
             dead = __any_sync(0xffffffffu, dead);
             if (dead) break;
         }
-        if (dead && rank == 0 && lane == 0) {
+        if (dead && rank == 0 && elect_one()) {
             commit_leader(bar(&bars.drain_p));
             mbar_drain(bar(&bars.drain_p), 0u, kDrainLimit);
         }

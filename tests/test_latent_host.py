@@ -1,5 +1,7 @@
 """Rotary positions and latent attention without a GPU: the frequencies against their definition, the oracle's two forms
 against one another, and what the calls refuse before they launch anything."""
+import os
+import re
 from fractions import Fraction
 
 import numpy as np
@@ -209,3 +211,14 @@ def test_plans_of_a_latent_prefill_need_no_page_ids():
     tc = B.cpa_latent_tables_config(_cfg(H=128))
     assert B.cpa_tables_bytes(tc, B.cpa_table_dims(4, 0, (1 << 26) - 1, 8, 0)) > 0
     assert B.cpa_tables_bytes(tc, B.cpa_table_dims(4, 0, 1 << 26, 8, 0)) == B.CPA_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("name", ["latent_decode.cu", "latent_decode_pair.cu"])
+def test_products_are_committed_by_the_lane_that_issues_them(name):
+    # a commit follows the products of its own thread alone: the one behind which tensor memory is freed after a wait gave up has to come from
+    # the elected lane too
+    text = open(os.path.join(os.path.dirname(B.__file__), "csrc", name)).read().splitlines()
+    drains = [i for i, line in enumerate(text) if re.search(r"commit_\w+\(bar\(&bars\.drain_", line)]
+    assert len(drains) == 2
+    for i in drains:
+        assert "elect_one()" in text[i - 1], text[i - 1]
