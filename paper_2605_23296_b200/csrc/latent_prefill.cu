@@ -412,7 +412,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                             float v[8];
                             tc_ld8(t_o + c * 8, v);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] *= alpha;
+                            for (int e = 0; e < 8; ++e) v[e] = mul_keep(v[e], alpha);
                             tc_st8(t_o + c * 8, v);
                         }
                     }
@@ -482,7 +482,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                                 float v[8];
                                 tc_ld8(t_o + c * 8, v);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) v[e] *= alpha;
+                                for (int e = 0; e < 8; ++e) v[e] = mul_keep(v[e], alpha);
                                 tc_st8(t_o + c * 8, v);
                             }
                         }
@@ -519,6 +519,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 tc_wait(bar(&bars.pv_done[u]), (n_steps - 1) & 1u, dead, ix.status);
                 tc_fence_after();
                 const float inv = 1.f / l_run;
+                auto two = [&](float x, float y) { return pack_bf16(mul_keep(x, inv), mul_keep(y, inv)); };      // (outputs below the normal range too)
                 const bool row_ok = !dead && r < w.L - (w.q0 + sub * kTileM);     // rows behind the block's end are not stored
                 __nv_bfloat16* dst = o + ((int64_t)(w.tok0 + w.q0 + sub * kTileM + r) * H + w.h) * kV;
 #pragma unroll
@@ -529,8 +530,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 #pragma unroll
                         for (int i = 0; i < 32; i += 8)
                             *reinterpret_cast<uint4*>(dst + c * 32 + i) =
-                                make_uint4(pack_bf16(v[i] * inv, v[i + 1] * inv), pack_bf16(v[i + 2] * inv, v[i + 3] * inv),
-                                           pack_bf16(v[i + 4] * inv, v[i + 5] * inv), pack_bf16(v[i + 6] * inv, v[i + 7] * inv));
+                                make_uint4(two(v[i], v[i + 1]), two(v[i + 2], v[i + 3]), two(v[i + 4], v[i + 5]), two(v[i + 6], v[i + 7]));
                     }
                 }
                 tc_fence_before();

@@ -829,6 +829,33 @@ def test_prefill_keeps_what_is_not_finite_to_its_own(B):
     B.cpa_plan_destroy(plan)
 
 
+@pytest.mark.parametrize("rows", [128, 256])
+@pytest.mark.parametrize("lens", [[1300], [129, 40, 257, 1000]])
+@pytest.mark.parametrize("spread", [2.0 ** -130, 2.0 ** -126, 2.0 ** -123])
+def test_prefill_keeps_outputs_below_the_normal_range(B, rows, lens, spread):
+    # values that small come through, the references' moves too: a key whose score lies 2^9 above the others' in a later tile
+    H, T, scale = 2, sum(lens), float(np.float32(192 ** -0.5))
+    rng = np.random.default_rng(len(lens))
+    qf, kvf, rf = np.zeros((T, H, 192)), np.zeros((T, H, 256)), np.zeros((T, 64))
+    qf[:, :, 128] = 1.0
+    kvf[..., 128:] = spread * (1 + rng.random((T, H, 128)))
+    for a, n in zip(np.cumsum([0] + lens), lens):
+        at = a + n - min(n, 30)
+        rf[at, 0], kvf[at, :, 128:] = 91.0, 0.0
+    (q, qf), (kv, kvf), (r, rf) = _bf16(qf), _bf16(kvf), _bf16(rf)
+    cfg = B.cpa_latent_config(H, 512, 64, 128, 128, 16, scale, 1e-6, 0)
+    pc = B.cpa_latent_plan_config(cfg)
+    pc.q_tile_rows = rows
+    plan = B.cpa_plan_create(pc, lens, 0, [0] * sum(-(-n // 16) for n in lens))
+    index = torch.empty(B.cpa_plan_param(plan, B.PARAM_INDEX_BYTES), dtype=torch.uint8, device="cuda")
+    assert B.cpa_plan_upload(plan, index, index.numel(), _stream()) == 0
+    o = torch.full((T, H, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+    assert B.cpa_latent_prefill(cfg, plan, q, kv, r, 64, o, _stream()) == 0 and B.cpa_plan_status(plan, _stream()) == 0
+    want, wide, shaken = ol.prefill(qf, kvf, rf, np.concatenate([[0], np.cumsum(lens)]), scale)
+    _check(o, want, ol.attention_tolerance(want, wide, shaken, 192), "tiny values")
+    B.cpa_plan_destroy(plan)
+
+
 # ------------------------------------------------------------------------------------------------ a whole event
 
 @pytest.mark.parametrize("H,L", [(8, 256), (40, 512)])
