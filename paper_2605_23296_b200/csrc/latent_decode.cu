@@ -423,7 +423,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                             float v[8];
                             tc_ld8(at, v);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] *= factor[c % NH + e];
+                            for (int e = 0; e < 8; ++e) v[e] = mul_keep(v[e], factor[c % NH + e]);
                             tc_st8(at, v);
                         }
                         tc_wait_st();
@@ -521,14 +521,16 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 // takes a unit by itself, else a CTA's eight warps share a unit's parts.  (Short code: it runs once or twice per launch, so
 // fetching its instructions is part of its time.)
 constexpr int kJoinWarps = 8, kFewParts = 8, kJoinBatch = 4, kJoinPerSm = 4;
+// (the values keep what lies below the normal range; the sums are far above it)
 __device__ __forceinline__ void scale_part(float4& v, float& l, float f) {
-    v.x *= f; v.y *= f; v.z *= f; v.w *= f; l *= f;
+    v = make_float4(mul_keep(v.x, f), mul_keep(v.y, f), mul_keep(v.z, f), mul_keep(v.w, f));
+    l *= f;
 }
 __device__ __forceinline__ void add_part(float4& v, float& l, const uint4& w, float wl, float f) {
-    v.x = fmaf(f, __uint_as_float(w.x), v.x);
-    v.y = fmaf(f, __uint_as_float(w.y), v.y);
-    v.z = fmaf(f, __uint_as_float(w.z), v.z);
-    v.w = fmaf(f, __uint_as_float(w.w), v.w);
+    v.x = fma_keep(f, __uint_as_float(w.x), v.x);
+    v.y = fma_keep(f, __uint_as_float(w.y), v.y);
+    v.z = fma_keep(f, __uint_as_float(w.z), v.z);
+    v.w = fma_keep(f, __uint_as_float(w.w), v.w);
     l = fmaf(f, wl, l);
 }
 __device__ __forceinline__ float2 ld_f2(const float2* p) {

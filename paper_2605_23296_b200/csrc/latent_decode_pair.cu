@@ -437,7 +437,7 @@ latent_decode_pair_kernel(const __grid_constant__ CUtensorMap map, const __grid_
                             float v[8];
                             tc_ld8(t_o + c, v);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] *= f;
+                            for (int e = 0; e < 8; ++e) v[e] = mul_keep(v[e], f);
                             tc_st8(t_o + c, v);
                         }
                         tc_wait_st();

@@ -491,6 +491,28 @@ def test_decode_masks_by_index_not_by_value(B, H, L):
         c.check(c.decode(qc, qr), cf, rf, what=str(junk))
 
 
+@pytest.mark.parametrize("H,L", [(16, 512), (33, 256), (64, 128), (128, 512), (70, 128)])
+@pytest.mark.parametrize("num_sms,lens", [(2, [1300, 40, 200]), (0, [5000]), (0, [1300, 40, 200, 1])])
+@pytest.mark.parametrize("spread", [2.0 ** -131, 2.0 ** -126, 2.0 ** -123])
+def test_decode_keeps_outputs_below_the_normal_range(B, H, L, num_sms, lens, spread):
+    # latent parts that small come through, moves of the references (a token whose score lies 2^14 above the first one's, late) and joins too
+    rng = np.random.default_rng(H + len(lens))
+    c = Cache(B, lens, L, H, num_sms=num_sms)
+    flat = c.pool.view(-1, L + 64)
+    for b, n in enumerate(lens):
+        x = np.zeros((n, L + 64))
+        x[:, :L] = spread * (1 + rng.random((n, L)))
+        x[n - min(n, 30), :] = 0.0
+        x[n - min(n, 30), L] = 140.0
+        x, c.rows[b] = _bf16(x)
+        flat[torch.as_tensor(c.slots(b, 0, n), dtype=torch.long, device="cuda")] = x
+    c.lens = _i32(lens)
+    qc, qr = torch.zeros(c.n, H, L, device="cuda").bfloat16(), torch.zeros(c.n, H, 64, device="cuda").bfloat16()
+    qr[:, :, 0] = 1.0
+    c.check(c.decode(qc, qr), _np(qc), _np(qr), what="tiny values")
+    assert c.status() == 0
+
+
 @pytest.mark.parametrize("H", [16, 128])
 def test_decode_scores_of_any_range(B, H):
     rng = np.random.default_rng(14)
