@@ -770,7 +770,7 @@ typedef struct cpa_latent_config {
     int32_t nope_dim;    /* expanded form: elements of a head's key without position, 128 */
     int32_t v_dim;       /* expanded form: elements of a head's value, 128 */
     int32_t page_size;   /* 16 */
-    float   scale;       /* softmax scale, normally 1 / sqrt(nope_dim + rope_dim) */
+    float   scale;       /* softmax scale, normally 1 / sqrt(nope_dim + rope_dim); 2^-100 .. 2^100 */
     float   norm_eps;    /* added to the mean square of a new latent part, >= 0 */
     int32_t num_sms;     /* SMs a launch of the decode may fill, 0 = all; at most 4095 (more than 64 heads: two at least) */
 } cpa_latent_config;

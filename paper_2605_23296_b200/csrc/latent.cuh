@@ -22,10 +22,11 @@ inline bool rope_config_ok(const cpa_rope_config* r) {
            (r->scaling != CPA_ROPE_SCALED_PARTS || r->base > 1.0);
 }
 
-// CPA_OK, or why the configuration is refused.
+// CPA_OK, or why the configuration is refused.  (The scale's range: the kernels multiply with scale * log2(e), which has to be a normal
+// number, and flush scores below 2^-126 ahead of it, which are nothing after it up to 2^100.)
 inline int latent_check(const cpa_latent_config* c) {
     if (!c || c->num_heads < 1 || c->latent_dim < 1 || c->rope_dim < 1 || c->nope_dim < 1 || c->v_dim < 1 || c->num_sms < 0 ||
-        !(c->scale > 0.f) || !(c->scale <= 3e38f) || !(c->norm_eps >= 0.f) || !(c->norm_eps <= 3e38f))
+        !(c->scale >= 0x1p-100f) || !(c->scale <= 0x1p100f) || !(c->norm_eps >= 0.f) || !(c->norm_eps <= 3e38f))
         return CPA_EINVAL;
     if (c->num_heads > kMaxLatentHeads || c->latent_dim % 128 != 0 || c->latent_dim > kMaxLatent || c->rope_dim != kRopeDim ||
         c->nope_dim != 128 || c->v_dim != 128 || c->page_size != kPage || c->num_sms > kMaxPlanSms)

@@ -222,3 +222,11 @@ def test_products_are_committed_by_the_lane_that_issues_them(name):
     assert len(drains) == 2
     for i in drains:
         assert "elect_one()" in text[i - 1], text[i - 1]
+
+
+@pytest.mark.parametrize("scale", [1e-45, 1e-40, 2.0 ** -101, 2.0 ** 101, 2.9e38])
+def test_scales_that_the_kernels_cannot_hold_are_refused(scale):
+    # times log2(e) they would be flushed to zero (all tokens alike), or infinite (NaN throughout)
+    assert B.cpa_latent_decode_workspace_bytes(_cfg(scale=scale)) == B.CPA_EINVAL
+    for fine in (2.0 ** -100, 2.0 ** 100):
+        assert B.cpa_latent_decode_workspace_bytes(_cfg(scale=fine)) > 0
