@@ -90,7 +90,8 @@ typedef struct cpa_config {
     int32_t q_tile_rows;     /* query rows per prefill work item: 128, 256, or 512 (items of 512 rows run on pairs of
                                 CTAs, cta_group::2: head_dim 128, plans without cached prefixes or chunks only;
                                 measured no faster than 256, kept as an option); 0 = default (256);
-                                CPA_Q_TILE_LATENT = 128 or 256, from the lengths (for cpa_latent_prefill) */
+                                CPA_Q_TILE_LATENT = 128 or 256, from the lengths (for cpa_latent_prefill: as many kv heads as
+                                query heads, head_dim 128) */
     int32_t pages_per_split; /* KV pages per decode work item (<= 1024); 0 = chosen per block from the batch */
     int32_t num_sms;         /* SMs this plan's kernels may fill: the persistent prefill launches min(num_sms, units)
                                 CTAs (one per SM) and the decode wave is sized for 3 * num_sms CTAs; 0 = the SM

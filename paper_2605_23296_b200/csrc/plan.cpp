@@ -110,6 +110,8 @@ int plan_create(const cpa_config* cfg, int32_t num_blocks, const int32_t* block_
     if (cfg->q_tile_rows != 0 && cfg->q_tile_rows != CPA_Q_TILE_LATENT && cfg->q_tile_rows != 128 && cfg->q_tile_rows != 256 &&
         cfg->q_tile_rows != 512)
         return CPA_EUNSUPPORTED;
+    // its choice is that of the latent prefill: every head has keys of its own, and values of 128
+    if (cfg->q_tile_rows == CPA_Q_TILE_LATENT && (cfg->num_kv_heads != cfg->num_q_heads || cfg->head_dim != 128)) return CPA_EUNSUPPORTED;
     // 512-row items run on pairs of CTAs: head_dim 128, whole blocks without cached prefix or chunks
     const bool pairs_possible = cfg->head_dim == 128 && !prefix_lens && chunk_tokens == 0 &&
                                 (cfg->num_sms == 0 || cfg->num_sms >= 2);

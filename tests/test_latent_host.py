@@ -230,3 +230,13 @@ def test_scales_that_the_kernels_cannot_hold_are_refused(scale):
     assert B.cpa_latent_decode_workspace_bytes(_cfg(scale=scale)) == B.CPA_EINVAL
     for fine in (2.0 ** -100, 2.0 ** 100):
         assert B.cpa_latent_decode_workspace_bytes(_cfg(scale=fine)) > 0
+
+
+def test_other_plans_do_not_take_the_latent_items():
+    for Hq, Hkv, D in ((8, 2, 128), (8, 4, 128), (4, 4, 64), (8, 1, 64)):
+        cfg = B.cpa_config(Hq, Hkv, D, 16, 0.1, B.Q_TILE_LATENT, 0, 148)
+        with pytest.raises(B.CpaError) as e:
+            B.cpa_plan_create(cfg, [100, 3], 0, list(range(8)))
+        assert e.value.status == B.CPA_EUNSUPPORTED
+        cfg.q_tile_rows = 0
+        B.cpa_plan_destroy(B.cpa_plan_create(cfg, [100, 3], 0, list(range(8))))
