@@ -147,7 +147,7 @@ extern "C" int cpa_latent_append(const cpa_latent_config* cfg, const cpa_table_d
         return CPA_EINVAL;
     if (rope && (!rope_config_ok(rope) || rope->rope_dim != kRopeDim)) return CPA_EINVAL;
     if (!d_cu_new && num_rows != dims->num_blocks) return CPA_EINVAL;
-    if (num_rows > 1 && x_row_stride < row) return CPA_EINVAL;
+    if (num_rows > 1 && (x_row_stride < row || (packed && packed == x && x_row_stride != row))) return CPA_EINVAL;
     append_args a = {};
     a.t = q8_view(tc, *dims, d_tables);
     a.x = (const __nv_bfloat16*)x;

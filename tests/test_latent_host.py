@@ -240,3 +240,10 @@ def test_other_plans_do_not_take_the_latent_items():
         assert e.value.status == B.CPA_EUNSUPPORTED
         cfg.q_tile_rows = 0
         B.cpa_plan_destroy(B.cpa_plan_create(cfg, [100, 3], 0, list(range(8))))
+
+
+def test_rows_are_packed_in_place_only_where_they_lie_packed():
+    # a wider row would be overwritten by the row of another token before it is read
+    cfg, dims, ok = _cfg(), B.cpa_table_dims(4, 0, 8, 8, 8), 1 << 20
+    for stride in (577, 584, 1152):
+        assert B.cpa_latent_append(cfg, dims, ok, None, None, ok, stride, None, None, 4, None, ok, ok + (1 << 16), ok, ok) == B.CPA_EINVAL
