@@ -356,13 +356,19 @@ class CompactionSession:
             pass
 
 
+def _with_index(device) -> torch.device:
+    """The device by its number: "cuda" alone would follow the current device from call to call."""
+    d = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
 class Rotary:
     """Rotary positions of one configuration on one device: the frequencies, computed once (cpa_rope_turns)."""
 
     def __init__(self, rope_dim: int, interleaved: bool = False, base: float = 10000.0, scaling: int = B.ROPE_UNSCALED,
                  factor: float = 1.0, trained_len: int = 0, fast: float = 32.0, slow: float = 1.0, amplitude: float = 1.0,
                  device: str = "cuda:0"):
-        self.device = torch.device(device)
+        self.device = _with_index(device)
         self.cfg = B.cpa_rope_config(rope_dim, B.ROPE_INTERLEAVED if interleaved else B.ROPE_HALF, scaling, trained_len, base, factor,
                                      fast, slow, amplitude)
         self.turns = torch.from_numpy(B.cpa_rope_turns(self.cfg).view(np.int64)).to(self.device)
@@ -397,7 +403,7 @@ class LatentSession:
                  latent_dim: int = 512, scale: Optional[float] = None, rope: Optional[Rotary] = None,
                  norm_weight: Optional[torch.Tensor] = None, norm_eps: float = 1e-6, first: Optional[Sequence[int]] = None,
                  device: str = "cuda:0", poison_pools: bool = False, num_sms: int = 0):
-        self.device = torch.device(device)
+        self.device = _with_index(device)
         self.plan = None
         self.H, self.L, self.rope, self.norm_weight = num_heads, latent_dim, rope, norm_weight
         self.B = len(block_lens)

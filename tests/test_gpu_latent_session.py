@@ -224,3 +224,14 @@ def test_far_pages_of_a_large_pool(H, L, far):
     assert all(torch.equal(a, b) for a, b in zip(*made))
     with pytest.raises(B.CpaError):
         LatentSession(lens, T, H, [-1] * 12, 12, L)
+
+
+def test_a_device_without_a_number_is_the_current_one_of_then():
+    from paper_2605_23296_b200.session import LatentSession, Rotary
+    here = torch.device("cuda", torch.cuda.current_device())
+    r = Rotary(64, device="cuda")
+    s = LatentSession([20], 2, 4, [0, 1], 2, 128, rope=r, device="cuda")
+    assert r.device == s.device == here
+    s.append_prefill(_bf16(np.random.default_rng(0), 20, 192))
+    assert s.status() == 0 and s.lens.tolist() == [20]
+    s.close()
