@@ -772,6 +772,102 @@ def test_few_blocks_with_tokens_among_many_without(B, H):
     assert (o == 0).all()
 
 
+# ------------------------------------------------------------------------------------------------ every token, once
+#
+# Values of zero and one show a token that is lost or taken twice at any length: element e of the output is the weight of the tokens
+# marked e over that of all, and no more than 60 tokens share a mark.  Bounds: queries score the positional part's first element k, a whole
+# number, with scale ln 2 to fp32, so that a weight is 2^k but for |k| 2^-23 at most (2^-18 for |k| <= 32, and the same again of every factor by
+# which a reference moves); rounded to bf16 it is 2^k.  Sums of such weights, two reciprocals' and products' roundings: below 2^-20.
+# The output: 2^-8.  In all |o| (2^-8 + 2^-14).  The lightest of sixty, a quarter of the heaviest, is 2^-7.1.  The last element, marked in all tokens, is one, exactly.
+
+MARKED = 2.0 ** -8 + 2.0 ** -14
+
+
+def _marks(n, m, k):
+    """[n, m + 1]: where the scores k are equal, token j has mark j % m, else stretches of equal length have one mark; and one for all."""
+    v = np.zeros((n, m + 1))
+    v[np.arange(n), np.arange(n) % m if (k == k[:1]).all() else np.arange(n) * m // max(n, 1)] = 1.0
+    v[:, m] = 1.0
+    return v
+
+
+def _scores(n, kind):
+    """Whole numbers: all alike; moving up by more than a reference allows; falling, so that the first tile's reference stays."""
+    j = np.arange(n)
+    if kind == "alike":
+        return np.zeros(n)
+    return (16.0 if kind == "rising" else -16.0) * (j >= n // 2) + (j % 3)
+
+
+def _check_marked(got, k, m, what):
+    w = 2.0 ** k
+    want = (w[:, None] * _marks(len(k), m, k)).sum(0) / w.sum()
+    _check(got, np.broadcast_to(want, got.shape), np.broadcast_to(MARKED * want, got.shape), what)
+    assert (got[..., m] == 1.0).all(), what
+
+
+@pytest.mark.parametrize("kind", ["alike", "rising", "falling"])
+@pytest.mark.parametrize("H", [16, 40, 64, 128])
+@pytest.mark.parametrize("num_sms,lens", [(0, EDGES), (0, [30000]), (0, [20011, 5, 3000, 1]), (3, [2011, 700, 64, 65]), (0, [997] * 40)])
+def test_decode_and_step_take_every_token_once(B, H, num_sms, lens, kind):
+    c = Cache(B, [n + 1 for n in lens], 512, H, num_sms=num_sms, scale=float(np.float32(np.log(2.0))))
+    rng, flat = np.random.default_rng(H), c.pool.view(-1, 576)
+    # (the tokens behind the first are what a step adds)
+    rows = [np.concatenate([_marks(n + 1, 511, _scores(n + 1, kind)), _scores(n + 1, kind)[:, None], rng.standard_normal((n + 1, 63))], 1) for n in lens]
+    for b, n in enumerate(lens):
+        if n:
+            flat[torch.as_tensor(c.slots(b, 0, n), dtype=torch.long, device="cuda")] = _bf16(rows[b][:n])[0]
+    c.lens = _i32(lens)
+    qc, qr = torch.zeros(c.n, H, 512, device="cuda").bfloat16(), torch.zeros(c.n, H, 64, device="cuda").bfloat16()
+    qr[:, :, 0] = 1.0
+    o = _np(c.decode(qc, qr))
+    for b, n in enumerate(lens):
+        if n:
+            k = _scores(n + 1, kind)
+            w, v = 2.0 ** k[:n], rows[b][:n, :512]
+            want = np.broadcast_to((w[:, None] * v).sum(0) / w.sum(), o[b].shape)
+            _check(o[b], want, MARKED * want, f"decode, block of {n}")
+            assert (o[b][:, 511] == 1.0).all()
+    x, _ = _bf16(np.stack([r[-1] for r in rows]))
+    out, o = torch.empty_like(c.lens), torch.empty(c.n, H, 512, dtype=torch.bfloat16, device="cuda")
+    assert B.cpa_latent_step(c.cfg, c.dims, c.tables, None, None, B.latent_io(qc, qr, o), x, 576, None, None, c.lens, out, None, c.pool, c.ws,
+                             _stream()) == 0
+    o = _np(o)
+    for b, n in enumerate(lens):
+        _check_marked(o[b], _scores(n + 1, kind), 511, f"step, block of {n + 1}")
+    assert out.tolist() == [n + 1 for n in lens] and c.status() == 0
+
+
+@pytest.mark.parametrize("kind", ["alike", "rising", "falling"])
+@pytest.mark.parametrize("rows", [128, 256])
+@pytest.mark.parametrize("lens,H,num_sms", [([1, 2, 15, 16, 17, 33, 63, 64, 65, 127, 128, 129], 2, 3), ([255, 256, 257, 383, 384, 385], 3, 0),
+                                            ([2500, 18, 1300], 1, 0)])
+def test_prefill_takes_every_token_once(B, lens, H, num_sms, rows, kind):
+    T, scale = sum(lens), float(np.float32(np.log(2.0)))
+    qf, kvf, rf = np.zeros((T, H, 192)), np.zeros((T, H, 256)), np.zeros((T, 64))
+    qf[:, :, 128] = 1.0
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    for a, n in zip(cu, lens):
+        k = _scores(n, kind)
+        kvf[a:a + n, :, 128:], rf[a:a + n, 0] = _marks(n, 127, k)[:, None], k
+    (q, _), (kv, _), (r, _) = _bf16(qf), _bf16(kvf), _bf16(rf)
+    cfg = B.cpa_latent_config(H, 512, 64, 128, 128, 16, scale, 1e-6, num_sms)
+    pc = B.cpa_latent_plan_config(cfg)
+    pc.q_tile_rows = rows
+    plan = B.cpa_plan_create(pc, lens, 0, [0] * sum(-(-n // 16) for n in lens))
+    index = torch.empty(B.cpa_plan_param(plan, B.PARAM_INDEX_BYTES), dtype=torch.uint8, device="cuda")
+    assert B.cpa_plan_upload(plan, index, index.numel(), _stream()) == 0
+    o = torch.full((T, H, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+    assert B.cpa_latent_prefill(cfg, plan, q, kv, r, 64, o, _stream()) == 0 and B.cpa_plan_status(plan, _stream()) == 0
+    o = _np(o)
+    for a, n in zip(cu, lens):
+        w = 2.0 ** rf[a:a + n, :1] * kvf[a:a + n, 0, 128:]
+        want = (np.cumsum(w, 0) / np.cumsum(2.0 ** rf[a:a + n, :1], 0))[:, None]
+        _check(o[a:a + n], np.broadcast_to(want, (n, H, 128)), np.broadcast_to(MARKED * want, (n, H, 128)), f"block of {n}")
+        assert (o[a:a + n, :, 127] == 1.0).all()
+    B.cpa_plan_destroy(plan)
+
+
 # ------------------------------------------------------------------------------------------------ expanded attention
 
 def _prefill(B, lens, H, rng, spread=1.0, stride=576, num_sms=0, scale=192 ** -0.5, rows=None):
