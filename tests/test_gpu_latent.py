@@ -784,9 +784,10 @@ MARKED = 2.0 ** -8 + 2.0 ** -14
 
 
 def _marks(n, m, k):
-    """[n, m + 1]: where the scores k are equal, token j has mark j % m, else stretches of equal length have one mark; and one for all."""
-    v = np.zeros((n, m + 1))
-    v[np.arange(n), np.arange(n) % m if (k == k[:1]).all() else np.arange(n) * m // max(n, 1)] = 1.0
+    """[n, m + 1]: where the scores k are equal, token j has mark j % m, else stretches of equal length in either half of the tokens (whose
+    weights are of one size) have one mark; and one for all."""
+    v, j, a, half = np.zeros((n, m + 1)), np.arange(n), n // 2, m // 2
+    v[j, j % m if (k == k[:1]).all() else np.where(j < a, j * half // max(a, 1), half + (j - a) * (m - half) // max(n - a, 1))] = 1.0
     v[:, m] = 1.0
     return v
 
