@@ -717,7 +717,8 @@ typedef struct cpa_rope_config {
 /*
  * cpa_rope_turns -- the frequencies of a configuration, host arithmetic only: turns[i], i < R/2, is f_i / (2 pi) without its
  * whole turns as a binary fraction of 64 bits.  The caller copies them to the device once.  (Position times fraction modulo
- * 2^64 is the angle of any int32 position, reduced exactly; the fraction is off by 2^-64 turns at most.)
+ * 2^64 is the angle of any int32 position, reduced exactly; the fraction is off by 2^-64 turns at most where f_i is at most 1,
+ * as it is for base >= 1 and factor >= 1.)
  * Errors: CPA_EINVAL.
  */
 CPA_API int cpa_rope_turns(const cpa_rope_config* cfg, uint64_t* turns);
@@ -738,9 +739,10 @@ typedef struct cpa_rope_rows {
  *   d_turns     : device uint64 [R/2], from cpa_rope_turns of the same configuration
  *   d_positions : device int32 [num_rows]; negative ones turn the other way
  *   inverse     : 0, or 1 to turn back by the same angles (and amplitude)
- * Angles are exact to 2^-32 turns, products in fp32, outputs rounded once.  16-byte aligned tensors with strides, offset and
- * head_dim of whole 8 elements and R of whole 16 (interleaved: 8) move in 16-byte pieces, others by element.  A tensor of no
- * heads and a call of no rows do nothing.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED (more than 2^24 elements a row), CPA_ECUDA.
+ * An angle is reduced to half a turn without error and then rounded to fp32 (by 2^-26 turns at most); products in fp32, outputs
+ * rounded once.  16-byte aligned tensors with strides, offset and head_dim of whole 8 elements and R of whole 16 (interleaved: 8)
+ * move in 16-byte pieces, others by element (both tensors of a call where one of them has to).  A tensor of no heads and a call of
+ * no rows do nothing.  Errors: CPA_EINVAL, CPA_EUNSUPPORTED (more than 2^24 elements a row), CPA_ECUDA.
  */
 CPA_API int cpa_rope(const cpa_rope_config* cfg, const uint64_t* d_turns, const int32_t* d_positions, int32_t num_rows,
                      const cpa_rope_rows* q, const cpa_rope_rows* k, int inverse, void* stream);

@@ -47,7 +47,7 @@ inline bool latent_aligned(const void* p, unsigned n) { return (reinterpret_cast
 // The angle of a pair at a position.  `turns` holds the pair's frequency in turns per position as a 64-bit binary fraction,
 // so position * turns modulo 2^64 is the angle's fractional part with no error but the fraction's own (2^-64 turns, times the
 // position): any int32 position, negative ones too, is reduced exactly by the product's wrap-around.  32 bits of it, as a
-// signed fraction of half a turn, go to the sine and cosine.
+// signed fraction of half a turn, are rounded to fp32 (off by 2^-26 turns at most) and go to the sine and cosine.
 __device__ __forceinline__ float2 rope_cos_sin(uint64_t turns, int32_t position, float amplitude) {
     const uint64_t a = (uint64_t)(int64_t)position * turns;
     const int32_t t = (int32_t)(uint32_t)((a + 0x80000000ull) >> 32);
