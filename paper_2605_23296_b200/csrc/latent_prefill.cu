@@ -372,16 +372,15 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 if (c * 32 + i > r) sv[c][i] = 0xff800000u;
-                        if (left < kTileN) {
-                            for (int half = left < 64 ? 0 : 1; half < 2; ++half) {
-                                const uint32_t i = (uint32_t)((kt0 + j) * kTilePieces + 3 + half);
-                                tc_wait(bar(&bars.full[i % kPieces]), (i / kPieces) & 1u, dead, ix.status);
-                                const int first = max(left - 64 * half, 0);
-                                if (!dead)
-                                    for (int e = r; e < (64 - first) * 16; e += 128)
-                                        *reinterpret_cast<uint4*>(smem + (s_ring - base) + (i % kPieces) * kPieceBytes + (e & 8) * (kPieceBytes / 16) +
-                                                                  (first + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
-                            }
+                        if (left < kTileN) {      // (more than kShortKeys, so only rows of the second piece)
+                            static_assert(kShortKeys == 64, "a last tile that is worked through whole reaches into its second V piece");
+                            const uint32_t i = (uint32_t)((kt0 + j) * kTilePieces + 4);
+                            tc_wait(bar(&bars.full[i % kPieces]), (i / kPieces) & 1u, dead, ix.status);
+                            const int first = left - 64;
+                            if (!dead)
+                                for (int e = r; e < (64 - first) * 16; e += 128)
+                                    *reinterpret_cast<uint4*>(smem + (s_ring - base) + (i % kPieces) * kPieceBytes + (e & 8) * (kPieceBytes / 16) +
+                                                              (first + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
                             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
                         }
                     }
