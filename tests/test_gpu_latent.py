@@ -898,6 +898,11 @@ def test_prefill_lengths_and_heads(B, lens, H):
         _prefill(B, lens, H, np.random.default_rng(sum(lens) + H), rows=rows)
 
 
+@pytest.mark.parametrize("lens,H", [([40, 131], 128), ([260, 1, 64], 65), ([385], 40)])
+def test_prefill_of_many_heads(B, lens, H):
+    _prefill(B, lens, H, np.random.default_rng(H))
+
+
 @pytest.mark.parametrize("lens,H,num_sms", [([18] * 60, 5, 4), ([1, 15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 64, 65, 66], 3, 2),
                                             ([129, 144, 145, 160, 161, 191, 192, 193, 257, 300, 320, 321], 2, 3),
                                             ([20, 300, 64, 1, 513, 130, 7, 40, 256, 2, 383], 4, 5), ([5, 200, 3, 450] * 8, 2, 1)])
