@@ -23,7 +23,7 @@
 // The reference m of a head stays as long as no score passes it by more than 2^8 (what it is cancels in the division); the
 // four warps of a half learn of that by one barrier with an OR, so a tile usually costs no exchange of maxima at all.
 //
-// Measured (latent parts of 512, caches larger than L2): 64 heads over 32 blocks of 1024..8192 tokens, 195 MB, 57 us (3.4 TB/s);
+// Measured (latent parts of 512, caches larger than L2): 64 heads over 32 blocks of 1024..8192 tokens, 195 MB, 57 us (3.4 TB/s) in a row;
 // 16 heads over 192 blocks of 512..1024 with a step's new rows, 175 MB, 46 us (3.8 TB/s); 16 heads over 4 blocks of up to 288
 // tokens 8.8 us.  What bounds it: the stream of pages runs at 5.8 TB/s once it runs (a tile of 74 KB every 3550 cycles at 64
 // heads, 3150 at 16: memory's latency under that load, 3400 cycles, and the chain of a tile, twice over in two stages; beside 74 KB

@@ -96,7 +96,8 @@ struct shares {
 };
 struct CutShared { int cost[kDecodeThreads / 32]; };      // of each warp's run of blocks
 __device__ __forceinline__ int blocks_per_thread(const decode_args& a) { return (a.B + kDecodeThreads - 1) / kDecodeThreads; }
-// By all threads of a CTA, with a barrier.  (What follows from the costs is left to the warp that hands the segments out: all of
+// By all threads of a CTA, with a barrier; a thread takes its blocks one behind the other, which shows from some thousand blocks on (16 heads,
+// blocks of 64 tokens: 192 blocks 12 us, 2000 46, 20000 425).  (What follows from the costs is left to the warp that hands the segments out: all of
 // this runs once in a launch, and takes as long as its instructions take to arrive.)
 __device__ __forceinline__ void sum_costs(const decode_args& a, CutShared& sm) {
     const int per = blocks_per_thread(a), b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);

@@ -11,11 +11,11 @@
 // in lanes 0-63 of its tensor memory with the first half of an instruction's columns and in lanes 64-127 with the second: scores
 // take 32 columns, outputs latent_dim / 2, lanes below 64 holding the first half of the latent elements.
 //
-// Measured (128 heads, latent parts of 512): one block of 131072 tokens, 151 MB and 36.5 GFLOP, 54.5 us (65 with a one-CTA group per 64
-// heads); a step of 16 blocks of 8192 tokens 58.6 us (69).  Bound by the chain within a tile of 64 tokens, 2180 cycles where the
-// operands take 1750: scores, softmax and outputs alternate over two tiles in shared memory, beside 74 KB of queries.  Arrivals in
-// the leader at cluster scope (release.cluster) cost over 1000 cycles each; CTA-scope ones order what these barriers hand over,
-// since data goes between the CTAs through the tensor cores and copies alone.
+// Measured (128 heads, latent parts of 512): one block of 131072 tokens, 151 MB and 36.5 GFLOP, 54.6 us in a row, 55.5 to 62 by single
+// calls (65 with a one-CTA group per 64 heads); a step of 16 blocks of 8192 tokens 59 us, 60 to 67 (69).  Bound by the chain within a
+// tile of 64 tokens, 2180 cycles where the operands take 1750: scores, softmax and outputs alternate over two tiles in shared memory,
+// beside 74 KB of queries.  Arrivals in the leader at cluster scope (release.cluster) cost over 1000 cycles each; CTA-scope ones order
+// what these barriers hand over, since data goes between the CTAs through the tensor cores and copies alone.
 //
 // Shares, segments, partials and the joining kernel are those of latent_decode.cu (a pair is a group, a CTA a head group).
 // Per CTA: warps 0-7 softmax and epilogue (thread = head, half of the tokens by lane, half of those by warpgroup), 8-11 queries, new

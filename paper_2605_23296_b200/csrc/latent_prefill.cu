@@ -24,11 +24,12 @@
 // warps 10-11 idle, they complete the warpgroup whose registers go to the softmax.
 // Keys behind a block's end are the next block's: their scores are masked by index and those of their V rows that an MMA reads
 // are cleared, so that what they hold (infinities, NaN) stays theirs.
-// Measured: 32 prompts of 1024..8192 tokens, 16 heads: 3.33 ms, 1.05 PFLOP/s of the products below the diagonal, in a row (under the power
-// limit; a single call 2.96 ms).  A pair of steps (both sub-tiles, one K/V tile) takes 3380 cycles, of which the tensor core is busy
-// 2560; the rest is the softmax of a sub-tile waiting for its scores: buffers for the scores of the next tile as well would fit
-// with the weights in place of the oldest scores only, and were slower (3.48 ms: both softmaxes then run at once and slow one another
-// down).  9 odd blocks of 1..700 tokens, 16 heads: 22-25 us, mostly the longest block's chain of tiles.
+// Measured: 32 prompts of 1024..8192 tokens, 16 heads: 3.33 ms, 1.05 PFLOP/s of the products below the diagonal, in a row (3.20 to 3.35,
+// under the power limit; a single call 2.96 ms).  A pair of steps (both sub-tiles, one K/V tile) takes 3380 cycles, of which the
+// tensor core is busy 2560; the rest is the softmax of a sub-tile waiting for its scores: buffers for the scores of the next tile as
+// well would fit with the weights in place of the oldest scores only, and were slower (3.48 ms: both softmaxes then run at once and
+// slow one another down).  9 odd blocks of 1..700 tokens, 16 heads: 24-25 us, the work of all items with their fixed part (the longest
+// block, 592 tokens, alone 14.4; the other eight 24.3).
 // Every mbarrier wait is bounded (see prefill_tc.cu).
 #include <atomic>
 

@@ -75,6 +75,8 @@ namespace {
 // the SMs taken for the end.  An item of two 128-row sub-tiles takes 6.7 us and 1.76 per K/V tile, of one 3.2 and 1.03 (fitted to
 // 100 blocks of 60..128 tokens up to 12 of 2048, 3 or 16 heads).  5 blocks of 755..1087 with 3 heads: 16 us by 128, 24 by 256; where
 // the two are expected within a tenth of one another they were, -3 to +8 % (9 blocks of 1..700 with 16 heads: 26.7 and 24.8).
+// (Fitted to items that follow one another.  Lone sub-tiles overlap since then and are cheaper than this: 8 blocks of 171..567 with 16 heads, 21.2 us
+// by 128, 24.3 by 256 as chosen here.)
 int32_t latent_q_tile(const std::vector<int32_t>& lens, int32_t heads, int32_t ctas) {
     double end[2];
     for (int k = 0; k < 2; ++k) {

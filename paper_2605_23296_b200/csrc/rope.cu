@@ -2,8 +2,10 @@
 //     (u, v) -> (u cos a - v sin a, v cos a + u sin a),     a = position * f_i,
 // in fp32 from bf16 inputs, rounded once.  A row's R/2 sines and cosines serve all of its heads, so a CTA computes those of a
 // tile of rows into shared memory and walks the tile's 16-byte pieces with them.  Bound by memory: two bytes read and two
-// written per element.  Measured: 32 + 8 heads of 128 over 32 prompts of 1024..8192 tokens, 2.5 GB, 398 us = 96 % of the
-// copy rate; one token for each of 192 blocks 2.8 us on the device.
+// written per element.  Measured: 32 + 8 heads of 128 over 32 prompts of 1024..8192 tokens, 2.5 GB, 398 us in a row = 96 % of the
+// copy rate (403 to 433 by single calls); one token for each of 192 blocks 2.8 us on the device.  By element, which only shapes that
+// hold no 16-byte pieces need, 32 + 8 heads of 80 with 20 rotated elements over the same prompts: 1.23 ms, 1.3 TB/s (16 of 80 by
+// pieces 321 us).
 #include <algorithm>
 #include <cmath>
 

@@ -477,7 +477,8 @@ class LatentSession:
 
     def append(self, x: torch.Tensor, counts: Optional[Sequence[int]] = None, packed: bool = False) -> Optional[torch.Tensor]:
         """New rows x [rows, latent_dim + 64] (packed block-major, any row stride), counts[b] per block or one each: normalised,
-        turned and stored behind the blocks' tokens.  With `packed` the stored rows come back too."""
+        turned and stored behind the blocks' tokens.  With `packed` the stored rows come back too.  (Their queries meet the
+        cache through decode() and step() alone, a token per block at a time; prefill() is over the prompts themselves.)"""
         if counts is None:
             cu, rows = None, self.B
         else:
