@@ -3,9 +3,8 @@
 // in fp32, rounded once to bf16, to the token's slot and, where asked for, to a packed row.  Bound by memory: 2 (L + 64) bytes
 // read and as many (or twice as many) written per token.  One warp takes a row: lane i holds the 16-byte pieces i, i + 32 and
 // i + 64 of it, so the sum of squares is a warp's sum, and each lane computes one of the 32 sines and cosines.  Measured: 32 prompts
-// of 1024..8192 tokens, latent parts of 512, packed rows as well, 473 MB, 77.5 us = 93 % of the copy rate
-// in a row, 78 to 83 by single calls; one row for each of
-// 192 blocks 3.4 us on the device (latency).
+// of 1024..8192 tokens, latent parts of 512, packed rows as well, 473 MB, 77.5 us in a row = 93 % of the copy rate (78 to 83 by single
+// calls); one row for each of 192 blocks 3.4 us on the device (latency).
 #include <algorithm>
 
 #include "latent.cuh"
