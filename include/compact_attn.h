@@ -812,8 +812,8 @@ CPA_API int cpa_latent_append(const cpa_latent_config* cfg, const cpa_table_dims
                               const int32_t* d_lens, int32_t* d_lens_out, void* pool, void* packed, void* stream);
 
 /* Queries and outputs of the decode calls, device bf16, strides in elements (a multiple of 8 each, pointers 16-byte aligned):
- * element e of head h of block b is at b * block_stride + h * head_stride + e.  The queries' strides are positive (those of a
- * single block or head are not looked at).  o must not overlap the queries. */
+ * element e of head h of block b is at b * block_stride + h * head_stride + e.  The queries' strides are positive; those of a
+ * single block or head are not looked at, here and in o.  o must not overlap the queries. */
 typedef struct cpa_latent_io {
     const void* q_latent;                    /* [B, num_heads, latent_dim] */
     int64_t q_latent_block_stride, q_latent_head_stride;

@@ -645,13 +645,13 @@ bool io_ok(const cpa_latent_io* io, int B, int H, int L) {
     if (!io || !io->q_latent || !io->q_rope || !io->o || !latent_aligned(io->q_latent, 16) || !latent_aligned(io->q_rope, 16) ||
         !latent_aligned(io->o, 16))
         return false;
-    for (int64_t s : {io->q_latent_block_stride, io->q_latent_head_stride, io->q_rope_block_stride, io->q_rope_head_stride,
-                      io->o_block_stride, io->o_head_stride})
-        if (s % 8 != 0) return false;
-    // queries are read through tensor maps: strides that count are positive and below 2^40 bytes
+    // (strides of a single block or head are not looked at)
     for (int64_t s : {B > 1 ? io->q_latent_block_stride : 8, H > 1 ? io->q_latent_head_stride : 8, B > 1 ? io->q_rope_block_stride : 8,
-                      H > 1 ? io->q_rope_head_stride : 8})
-        if (s <= 0 || s >= (int64_t)1 << 39) return false;
+                      H > 1 ? io->q_rope_head_stride : 8}) {
+        // queries are read through tensor maps: whole pieces, and positive below 2^40 bytes
+        if (s % 8 != 0 || s <= 0 || s >= (int64_t)1 << 39) return false;
+    }
+    if ((B > 1 && io->o_block_stride % 8 != 0) || (H > 1 && io->o_head_stride % 8 != 0)) return false;
     if (io->o == io->q_latent || io->o == io->q_rope) return false;
     // heads of the output must not share elements: blocks of heads, or heads of blocks
     const int64_t bs = B > 1 ? io->o_block_stride : INT64_MAX, hs = H > 1 ? io->o_head_stride : INT64_MAX;

@@ -397,6 +397,27 @@ def test_append_of_many_rows_is_that_of_few(B, rows, L, how):
     assert torch.equal(packed[stays], was[stays] if how == "in place" else torch.full_like(packed[stays], 3.0))
 
 
+@pytest.mark.parametrize("n", [4735, 4737, 5001])
+def test_append_one_row_for_each_of_many_blocks(B, n):
+    rng = np.random.default_rng(n)
+    c = Cache(B, [1 + b % 3 for b in range(n)], 128, rope=Rope(B))
+    was = rng.integers(0, 3, n)                                              # some have no room left
+    x, xf = _bf16(rng.standard_normal((n, 192)))
+    first, out, packed = _i32(np.arange(n)), torch.empty_like(c.lens), torch.full((n, 192), 3.0, dtype=torch.bfloat16, device="cuda")
+    was[::7] = 16
+    assert B.cpa_latent_append(c.cfg, c.dims, c.tables, c.rope.cfg, c.rope.turns, x, 192, None, None, n, first, _i32(was), out, c.pool, packed,
+                               _stream()) == 0
+    fits = was < 16
+    assert out.tolist() == (was + fits).tolist() and c.status() == B.CPA_ENOSPC
+    want = ol.new_rows(xf, 128, None, 0, np.arange(n) + was, c.rope.f)
+    got = _np(packed)
+    _check(got[fits], want[fits], ol.rows_tolerance(xf, want, 128)[fits])
+    assert (got[~fits] == 3.0).all()
+    at = np.array([c.slots(b, was[b], was[b] + 1)[0] for b in np.flatnonzero(fits)])
+    assert np.array_equal(_np(c.pool.view(-1, 192)[torch.as_tensor(at, dtype=torch.long, device="cuda")]), got[fits])
+    assert int((~torch.isnan(c.pool.view(-1, 192)[:, 0])).sum()) == fits.sum()
+
+
 # ------------------------------------------------------------------------------------------------ absorbed attention
 
 EDGES = [0, 1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 200, 255, 256, 257, 1000]
@@ -455,6 +476,25 @@ def test_decode_takes_strided_queries_and_outputs(B):
     o = c.decode(hq, wide[..., 128:], out=out[..., :L].transpose(0, 1))
     c.check(o, cf, rf, what="strided")
     assert (out[..., L:] == 4.0).all()
+
+
+@pytest.mark.parametrize("lens,H", [([300], 24), ([300], 100), ([70, 3, 200], 1), ([1], 1)])
+def test_strides_of_a_single_block_or_head_do_not_matter(B, lens, H):
+    rng = np.random.default_rng(H)
+    c = Cache(B, [n + 1 for n in lens], 256, H)
+    c.fill(lens, rng)
+    qc, qr, cf, rf = c.queries(rng)
+    io = lambda o, f: B.cpa_latent_io(qc.data_ptr(), *f(qc.stride()), qr.data_ptr(), *f(qr.stride()), o.data_ptr(), *f(o.stride()))
+    odd = lambda s: (13 if c.n == 1 else s[0], -5 if H == 1 else s[1])
+    made = []
+    for f in (lambda s: s[:2], odd):
+        o, o2, out = torch.full_like(qc, 9.0), torch.full_like(qc, 9.0), torch.empty_like(c.lens)
+        assert B.cpa_latent_decode(c.cfg, c.dims, c.tables, io(o, f), c.lens, None, c.pool, c.ws, _stream()) == 0
+        x = torch.ones(c.n, 320, device="cuda").bfloat16()
+        assert B.cpa_latent_step(c.cfg, c.dims, c.tables, None, None, io(o2, f), x, 320, None, None, c.lens, out, None, c.pool, c.ws, _stream()) == 0
+        made.append((o, o2))
+    c.check(made[0][0], cf, rf)
+    assert c.status() == 0 and all(torch.equal(a, b) for a, b in zip(*made))
 
 
 def test_decode_inactive_and_bad_blocks_sit_out(B):
