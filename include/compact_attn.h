@@ -711,7 +711,7 @@ typedef struct cpa_rope_config {
     double  base;        /* > 0, at most 1e30 */
     double  factor;      /* > 0, at most 1e6 */
     double  fast, slow;  /* turns, 0 < slow < fast <= 1e9 */
-    double  amplitude;   /* multiplies sines and cosines; 1 for none (0 < amplitude <= 1e4) */
+    double  amplitude;   /* multiplies sines and cosines; 1 for none (1e-30 .. 1e4) */
 } cpa_rope_config;
 
 /*

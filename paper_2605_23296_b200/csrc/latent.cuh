@@ -12,7 +12,7 @@ constexpr int kMaxLatentHeads = 128;
 inline bool rope_config_ok(const cpa_rope_config* r) {
     if (!r || r->rope_dim < 2 || r->rope_dim > 256 || r->rope_dim % 2 != 0) return false;
     if (r->layout != CPA_ROPE_HALF && r->layout != CPA_ROPE_INTERLEAVED) return false;
-    if (!(r->base > 0.0) || !(r->base <= 1e30) || !(r->amplitude > 0.0) || !(r->amplitude <= 1e4)) return false;
+    if (!(r->base > 0.0) || !(r->base <= 1e30) || !(r->amplitude >= 1e-30) || !(r->amplitude <= 1e4)) return false;
     if (r->scaling == CPA_ROPE_UNSCALED) return true;
     if (!(r->factor > 0.0) || !(r->factor <= 1e6)) return false;
     if (r->scaling == CPA_ROPE_SCALED_ALL) return true;

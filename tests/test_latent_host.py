@@ -247,3 +247,10 @@ def test_rows_are_packed_in_place_only_where_they_lie_packed():
     cfg, dims, ok = _cfg(), B.cpa_table_dims(4, 0, 8, 8, 8), 1 << 20
     for stride in (577, 584, 1152):
         assert B.cpa_latent_append(cfg, dims, ok, None, None, ok, stride, None, None, 4, None, ok, ok + (1 << 16), ok, ok) == B.CPA_EINVAL
+
+
+@pytest.mark.parametrize("amplitude", [1e-300, 1e-45, 1e-38, 9e-31])
+def test_amplitudes_that_fp32_sines_cannot_hold_are_refused(amplitude):
+    # they would come out as zeros
+    assert B.cpa_rope_turns(_rope(amplitude=amplitude), check=False)[0] == B.CPA_EINVAL
+    assert B.cpa_rope_turns(_rope(amplitude=1e-30), check=False)[0] == B.CPA_OK
